@@ -242,7 +242,7 @@ def prepare(case, seed):
         from paper_2602_02108_amd import api
         if c["op"] == "kv4_attn":
             desc = api.make_rows_desc(s["q"], s["k_pool"], table, s["max_len"], 1.0 / math.sqrt(D), max_rows=c["rows"])
-            s["ws"] = torch.empty(max(256, api.rows_workspace_bytes(desc, _lists(c) if c["top_k"] else -1)), dtype=torch.uint8, device=dev)
+            s["ws"] = torch.empty(max(256, api.kvq_workspace_bytes(desc, _lists(c) if c["top_k"] else -1)), dtype=torch.uint8, device=dev)
         else:
             s["rope"] = api.Rope(s["cos"], s["sin"], interleaved=c["interleaved"])
     return s
