@@ -377,6 +377,119 @@ oomb_status oomb_check_inputs(const oomb_attn_desc* desc, const int32_t* page_ta
                               const int32_t* sel_count, int32_t sel_stride, int32_t lists_per_head, int32_t* violations,
                               void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/*
+ * Rows of any number of sequences (prompts of any length, single tokens in generation) on their way into paged caches, with the
+ * position rotation of their queries and keys, the backward of that, and attention over a cache held in 4 bits.
+ *
+ * Row tensors are packed, [n_rows][heads][D] with strides of their own (views of a packed projection are fine).  Sequence b
+ * has the rows row_starts[b] .. row_starts[b + 1] - 1 (row_starts == NULL: n_rows / n_seqs rows each) and seq_lens[b]
+ * tokens (NULL: max_len), the rows' own among them: the rows are its last tokens, and row i of its n stands at position
+ * seq_lens[b] - n + i.  A sequence may have no rows, or no tokens; rows past row_starts[n_seqs] belong to none, and no entry point reads or
+ * writes them.  Sequence b's logical page l is physical page page_tables[b][l]; pages may be shared by sequences as long as no
+ * row is appended to them.
+ * All of these arrays are read on the device (a captured graph follows them from replay to replay); what the host gives are bounds: no sequence has more than
+ * max_rows rows or max_len tokens.  Rows beyond max_rows are left out, and lengths are cut to max_len.  A row of a
+ * sequence shorter than its rows (a position below 0) does not exist: the appends and their backward leave it alone, for attention it sees nothing.  A physical page outside [0, num_phys_pages)
+ * holds nothing: rows are not written there (their gradients and read values are 0) and attention does not see it.
+ */
+typedef struct {
+  int32_t n_q_heads, n_kv_heads; /* Hq, Hkv; Hkv divides Hq */
+  int32_t head_dim;              /* D: 64 or 128 */
+  int32_t page_size;             /* P: power of two, 16..128 */
+  int32_t dtype;                 /* oomb_dtype of the row tensors (and of K / V pools) */
+  int32_t n_seqs, n_rows;        /* > 0 */
+  int32_t max_rows;              /* 1 .. n_rows */
+  float sm_scale;                /* attention: logits = sm_scale * <q, k>; > 0 */
+  int32_t reserved;              /* 0 */
+  int64_t max_len;               /* 1 .. table_stride * P, below 2^31 - 256 */
+  int64_t table_stride;          /* entries of a row of page_tables */
+  int64_t num_phys_pages;
+  int64_t pool_page_stride, pool_head_stride, pool_tok_stride; /* elements; 4-bit pools: bytes, pool_tok_stride unused */
+} oomb_rows_desc;
+
+/* one row tensor: element strides; D contiguous, every D-row 16-byte aligned */
+typedef struct {
+  void* data;
+  int64_t tok_stride, head_stride;
+} oomb_rows;
+
+/* device arrays: page_tables [n_seqs][table_stride], seq_lens [n_seqs] or NULL, row_starts [n_seqs + 1] or NULL */
+typedef struct {
+  const int32_t* page_tables;
+  const int32_t* seq_lens;
+  const int32_t* row_starts;
+} oomb_seqs;
+
+/* The rotation: cos and sin [n_pos][rot_dim / 2] float, device, n_pos >= max_len: pair i of a row at position p turns by
+ * the angle whose cosine and sine are cos[p][i] and sin[p][i]:
+ *   y1 = x1 cos - x2 sin,  y2 = x2 cos + x1 sin
+ * Pairs are dims (i, rot_dim / 2 + i), or with interleaved != 0 (2 i, 2 i + 1); dims from rot_dim on stay as they are.  rot_dim: a
+ * multiple of 16, at most D.  With rot_dim 0, or a NULL oomb_rope, nothing turns. */
+typedef struct {
+  const float* cos;
+  const float* sin;
+  int64_t n_pos;
+  int32_t rot_dim;
+  int32_t interleaved;
+} oomb_rope;
+
+/*
+ * oomb_kv_append_rope: the rows' keys, rotated, and values go to their pages, the queries are rotated.
+ *   q, q_out [n_rows][Hq][D]   in, out (both or neither; may be the same tensor; otherwise they must not overlap)
+ *   k, v     [n_rows][Hkv][D]  in
+ *   k_pool, v_pool [n_phys][Hkv][P][D]  in/out: the row at position t of sequence b goes to
+ *            pool[page_tables[b][t / P]][g][t % P]; nothing else is written
+ *   kbar_cache [n_seqs][table_stride][Hkv][D] float or NULL, in/out: for every page that the rows fill to its last token
+ *            the mean of its P keys, as oomb_page_means computes it
+ * Keys are rotated in 64 bits and rounded to float, then to their type; queries in float (two rounded products, one rounded sum).
+ *
+ * oomb_kv_append_rope_bwd: its backward.  d_q is the gradient with respect to q_out; dk_pool / dv_pool (element type grad_dtype,
+ * the descriptor's pool strides) hold the gradients with respect to the pages:
+ *   d_q_out = d_q rotated back (d_q and d_q_out: both or neither, may be the same)
+ *   d_k, d_v [n_rows][Hkv][D] = the rows' gradients in the pools, d_k rotated back
+ * in float, rounded once to the rows' type.  The pools are left as they are.
+ */
+oomb_status oomb_kv_append_rope(const oomb_rows_desc* desc, const oomb_seqs* seqs, const oomb_rope* rope, const oomb_rows* q,
+                                const oomb_rows* q_out, const oomb_rows* k, const oomb_rows* v, void* k_pool, void* v_pool,
+                                float* kbar_cache, void* hip_stream);
+oomb_status oomb_kv_append_rope_bwd(const oomb_rows_desc* desc, const oomb_seqs* seqs, const oomb_rope* rope,
+                                    const oomb_rows* d_q, const oomb_rows* d_q_out, const void* dk_pool, const void* dv_pool,
+                                    int32_t grad_dtype, const oomb_rows* d_k, const oomb_rows* d_v, void* hip_stream);
+
+/*
+ * A cache held in 4 bits ("kvq").  A pool is bytes [n_phys][Hkv][tile], tile = P * (D / 2 + D / 32): the codes [P][D / 2] of
+ * a page's tokens (dim 2 i in the low half of byte i), then the scales [D / 32][P], one byte per block of 32 dims and token.  A code
+ * is a sign bit over {0, 0.5, 1, 1.5, 2, 3, 4, 6} (e2m1), a scale byte s stands for 2^(s - 127), and 255 for NaN.
+ * What a token takes is 68 bytes per head at D = 128, against 256 in bf16.
+ *
+ * oomb_kvq_append_rope: oomb_kv_append_rope into such pools.  A block's scale is the smallest power of two, 2^-125 .. 2^125, of
+ * which its largest magnitude is at most 7 times; a value is rounded to the nearest of the codes, ties to the even code, beyond 6 to 6.  A block
+ * that holds a value that is not finite becomes NaN throughout.  Rotated keys are quantised from 64 bits, without a rounding
+ * to their type in between.  kbar_cache receives the means of the values that the cache holds.
+ *
+ * oomb_kvq_read: the values of the rows as the cache holds them, k_out, v_out [n_rows][Hkv][D]
+ * (exact in either type).  To read a whole sequence, let its rows be all its tokens.
+ *
+ * oomb_paged_attn_fwd_kvq: attention of the rows over such a cache.  Row r of query head h at position p sees the tokens
+ * t <= p of its sequence whose page is listed for KV head g = h / G:
+ *   O[r,h,:] = sum_t exp(s_t - LSE) V[t],  LSE[h][r] = log sum_t exp(s_t),  s_t = sm_scale <Q[r,h], K[t]>
+ *   q, o [n_rows][Hq][D] (o must not overlap q);  lse [Hq][n_rows] float
+ *   sel_pages [n_seqs][Hkv][sel_stride] int32 logical pages, ascending, distinct, and sel_count [n_seqs][Hkv]; NULL: every page
+ * A row that sees no token gets O = 0 and LSE = -infinity.  A value that is not finite reaches the rows that see its token, and no
+ * other.  fp32 rows: products in three bf16 terms per value (the cache's values are exact in one), sums in fp32.
+ * Results do not depend on scheduling.  Workspace: oomb_kvq_workspace_bytes(desc, sel_stride), sel_stride < 0 for every page (with
+ * less than that, OOMB_ERR_WORKSPACE; it may be 0); calls that overlap in time need workspaces of their own.
+ */
+oomb_status oomb_kvq_append_rope(const oomb_rows_desc* desc, const oomb_seqs* seqs, const oomb_rope* rope, const oomb_rows* q,
+                                 const oomb_rows* q_out, const oomb_rows* k, const oomb_rows* v, void* k_pool, void* v_pool,
+                                 float* kbar_cache, void* hip_stream);
+oomb_status oomb_kvq_read(const oomb_rows_desc* desc, const oomb_seqs* seqs, const void* k_pool, const void* v_pool,
+                          const oomb_rows* k_out, const oomb_rows* v_out, void* hip_stream);
+size_t oomb_kvq_workspace_bytes(const oomb_rows_desc* desc, int32_t sel_stride);
+oomb_status oomb_paged_attn_fwd_kvq(const oomb_rows_desc* desc, const oomb_seqs* seqs, const oomb_rows* q, const void* k_pool,
+                                    const void* v_pool, const int32_t* sel_pages, const int32_t* sel_count, int32_t sel_stride,
+                                    const oomb_rows* o, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 const char* oomb_status_string(int32_t status);
 
 /* major * 10000 + minor * 100 + patch */

@@ -29,7 +29,8 @@ EXPORTS = ["oomb_workspace_bytes", "oomb_page_score_topk", "oomb_paged_attn_fwd"
            "oomb_page_pool_reset", "oomb_page_pool_alloc", "oomb_page_pool_release",
            "oomb_paged_attn_fwd_qp", "oomb_paged_attn_bwd_qp", "oomb_page_vote_topk",
            "oomb_offload_plan", "oomb_offload_fetch", "oomb_offload_writeback", "oomb_check_inputs",
-           "oomb_page_score_topk_noalloc"]
+           "oomb_page_score_topk_noalloc", "oomb_kv_append_rope", "oomb_kv_append_rope_bwd",
+           "oomb_kvq_append_rope", "oomb_kvq_read", "oomb_kvq_workspace_bytes", "oomb_paged_attn_fwd_kvq"]
 
 
 class AttnDesc(ctypes.Structure):
@@ -42,6 +43,29 @@ class AttnDesc(ctypes.Structure):
                 ("pool_tok_stride", ctypes.c_int64),
                 ("q_tok_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
                 ("num_phys_pages", ctypes.c_int64)]
+
+
+class RowsDesc(ctypes.Structure):
+    _fields_ = [("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("n_seqs", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("max_rows", ctypes.c_int32),
+                ("sm_scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+                ("max_len", ctypes.c_int64), ("table_stride", ctypes.c_int64), ("num_phys_pages", ctypes.c_int64),
+                ("pool_page_stride", ctypes.c_int64), ("pool_head_stride", ctypes.c_int64),
+                ("pool_tok_stride", ctypes.c_int64)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("tok_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class Seqs(ctypes.Structure):
+    _fields_ = [("page_tables", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("row_starts", ctypes.c_void_p)]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("n_pos", ctypes.c_int64),
+                ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
 
 
 class OombError(RuntimeError):
@@ -114,6 +138,18 @@ def lib():
         l.oomb_page_pool_release.argtypes = [i64, vp, ctypes.POINTER(i64), vp, i64]
         l.oomb_calibrate.restype = i32
         l.oomb_calibrate.argtypes = [i32, vp, u64, ctypes.POINTER(ctypes.c_double), vp]
+        rd, rw, sq, rp = (ctypes.POINTER(t) for t in (RowsDesc, Rows, Seqs, RopeDesc))
+        for f in (l.oomb_kv_append_rope, l.oomb_kvq_append_rope):
+            f.restype = i32
+            f.argtypes = [rd, sq, rp, rw, rw, rw, rw, vp, vp, vp, vp]
+        l.oomb_kv_append_rope_bwd.restype = i32
+        l.oomb_kv_append_rope_bwd.argtypes = [rd, sq, rp, rw, rw, vp, vp, i32, rw, rw, vp]
+        l.oomb_kvq_read.restype = i32
+        l.oomb_kvq_read.argtypes = [rd, sq, vp, vp, rw, rw, vp]
+        l.oomb_kvq_workspace_bytes.restype = u64
+        l.oomb_kvq_workspace_bytes.argtypes = [rd, i32]
+        l.oomb_paged_attn_fwd_kvq.restype = i32
+        l.oomb_paged_attn_fwd_kvq.argtypes = [rd, sq, rw, vp, vp, vp, vp, i32, rw, vp, vp, u64, vp]
         _lib = l
     return _lib
 
@@ -571,3 +607,214 @@ def local_page_list(desc: AttnDesc, window_pages: int, device, sel_pages=None, s
     if st != OK:
         raise _refused("oomb_local_page_list") if st < 0 else OombError(st, "oomb_local_page_list")
     return sel_pages, sel_count
+
+
+# ---- packed rows of any number of sequences: rotation and append, their backward, a cache held in 4 bits (include/oomb.h) ----
+
+class Rope:
+    """Tables of a position rotation: cos, sin [positions][rot_dim / 2] float32; pairs in halves, or neighbours."""
+    __slots__ = ("cos", "sin", "interleaved")
+
+    def __init__(self, cos, sin, interleaved: bool = False):
+        self.cos, self.sin, self.interleaved = cos, sin, bool(interleaved)
+
+
+def rope_tables(n_pos: int, rot_dim: int, theta: float = 10000.0, interleaved: bool = False, device="cuda") -> Rope:
+    """Rope with the angles p * theta^(-2 i / rot_dim), taken in 64 bits (far positions), held in 32."""
+    half = rot_dim // 2
+    freq = float(theta) ** (-torch.arange(half, dtype=torch.float64) / half)
+    angle = torch.arange(n_pos, dtype=torch.float64)[:, None] * freq
+    return Rope(angle.cos().float().to(device), angle.sin().float().to(device), interleaved)
+
+
+def kvq_tile_bytes(page_size: int, head_dim: int) -> int:
+    """Bytes of one page of one KV head in a pool of 4-bit codes."""
+    return page_size * (head_dim // 2 + head_dim // 32)
+
+
+def kvq_pool(n_phys: int, n_kv_heads: int, page_size: int, head_dim: int, device="cuda") -> torch.Tensor:
+    """A pool of 4-bit codes, uint8 [n_phys][Hkv][tile]."""
+    return torch.zeros((n_phys, n_kv_heads, kvq_tile_bytes(page_size, head_dim)), dtype=torch.uint8, device=device)
+
+
+def make_rows_desc(q: torch.Tensor, pool: torch.Tensor, page_tables: torch.Tensor, max_len: int, sm_scale: float = 1.0,
+                   max_rows: Optional[int] = None) -> RowsDesc:
+    """Descriptor from packed rows [n_rows][Hq][D], a pool ([n_phys][Hkv][P][D], or a kvq_pool) and page tables ([n_seqs][pages], or
+    [pages] of one sequence).  max_rows: most rows of one sequence (default: all rows)."""
+    desc = RowsDesc()
+    if (_nb or _native()).make_rows_desc(desc, q, pool, page_tables, max_len, sm_scale, max_rows or 0) != 0:
+        raise OombError(ERR_INVALID_ARG, "make_rows_desc: q must be [n_rows][Hq][D] float32 or bfloat16, pool [n_phys][Hkv][P][D] or a kvq_pool "
+                                         "of that head dim, page_tables [n_seqs][pages] or [pages]")
+    return desc
+
+
+def means_desc(q: torch.Tensor, n_kv_heads: int, page_size: int, ctx_len: int, sm_scale: float) -> AttnDesc:
+    """AttnDesc for the calls that pick pages from cached means (page_score_topk_cached, page_vote_topk, local_page_list) where
+    there is no K pool of q's type to make it from: a chunk [C][Hq][D] of whole pages over a cache held in 4 bits."""
+    C, Hq, D = q.shape
+    return AttnDesc(Hq, n_kv_heads, D, page_size, C, _dt(q.dtype), F32, float(sm_scale), int(ctx_len), n_kv_heads * page_size * D, page_size * D, D,
+                    q.stride(0), q.stride(1), ctx_len // page_size)
+
+
+def _rows_refused(where: str, desc: RowsDesc, rows, pools, page_tables, seq_lens, row_starts, rope=None, kbar_cache=None, others=()):
+    """The error of a call whose tensors the native module did not take: which of them does not fit the descriptor."""
+    def bad(what):
+        return OombError(ERR_INVALID_ARG, f"{where}: {what}")
+
+    dt = torch.bfloat16 if desc.dtype == BF16 else torch.float32
+    kvq_shape = (desc.num_phys_pages, desc.n_kv_heads, kvq_tile_bytes(desc.page_size, desc.head_dim))
+    pages = -(-desc.max_len // max(desc.page_size, 1))
+    tensors = []
+    for name, t, heads in rows:
+        want = (desc.n_rows, heads, desc.head_dim)
+        if not isinstance(t, torch.Tensor) or tuple(t.shape) != want or t.dtype != dt or t.stride(2) != 1:
+            return bad(f"{name} must be {list(want)}, {dt}, its last dim contiguous")
+        tensors.append((name, t))
+    for name, t, kind in pools:
+        want = kvq_shape if kind is torch.uint8 else (desc.num_phys_pages, desc.n_kv_heads, desc.page_size, desc.head_dim)
+        strides = (desc.pool_page_stride, desc.pool_head_stride) + (() if kind is torch.uint8 else (desc.pool_tok_stride,)) + (1,)
+        if not isinstance(t, torch.Tensor) or tuple(t.shape) != want or tuple(t.stride()) != strides or t.dtype != kind:
+            return bad(f"{name} must be {list(want)}, {kind}, with the strides {list(strides)} of the descriptor's pool")
+        tensors.append((name, t))
+    t = page_tables
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or (t.dim() == 1 and desc.n_seqs != 1) or t.dim() not in (1, 2) or \
+            (t.dim() == 2 and (t.shape[0] != desc.n_seqs or (desc.n_seqs > 1 and t.stride(0) != desc.table_stride))) or t.shape[-1] < pages or \
+            (t.shape[-1] > 1 and t.stride(-1) != 1):
+        return bad(f"page_tables must be int32 [{desc.n_seqs}][>= {pages}] with the descriptor's row stride")
+    tensors.append(("page_tables", t))
+    for name, t, n in (("seq_lens", seq_lens, desc.n_seqs), ("row_starts", row_starts, desc.n_seqs + 1)):
+        if t is not None and (not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or tuple(t.shape) != (n,) or not t.is_contiguous()):
+            return bad(f"{name} must be contiguous int32 [{n}]")
+        tensors.append((name, t))
+    if rope is not None:
+        for name in ("cos", "sin"):
+            t = getattr(rope, name)
+            if not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or t.dim() != 2 or not t.is_contiguous() or t.shape != rope.cos.shape:
+                return bad("rope.cos and rope.sin must be contiguous float32 [positions][rot_dim / 2]")
+            tensors.append((name, t))
+    if kbar_cache is not None:
+        t = kbar_cache
+        if not isinstance(t, torch.Tensor) or t.dtype != torch.float32 or not t.is_contiguous() or t.dim() not in (3, 4) or \
+                tuple(t.shape[-2:]) != (desc.n_kv_heads, desc.head_dim) or (t.dim() == 3 and desc.n_seqs != 1) or \
+                (t.dim() == 4 and (t.shape[0] != desc.n_seqs or (desc.n_seqs > 1 and t.shape[1] != desc.table_stride))) or t.shape[-3] < pages:
+            return bad("kbar_cache must be contiguous float32 [n_seqs][table stride][Hkv][D] ([pages][Hkv][D] for one sequence)")
+        tensors.append(("kbar_cache", t))
+    tensors += list(others)
+    devices = {t.device for _, t in tensors if t is not None}
+    if len(devices) > 1 or any(x.type != "cuda" for x in devices):
+        return bad(f"the tensors must lie on one GPU (got {sorted(str(x) for x in devices)})")
+    return _refused(where)
+
+
+def _rows_like(q, heads, row_starts):
+    """A new row tensor; rows that belong to no sequence are written by no call and start at zero."""
+    make = torch.empty if row_starts is None else torch.zeros
+    return make((q.shape[0], heads, q.shape[2]), dtype=q.dtype, device=q.device)
+
+
+def _rope(rope):
+    return (None, None, False) if rope is None else (rope.cos, rope.sin, rope.interleaved)
+
+
+def _append_rope(where, native, pool_dtype, desc, k, v, page_tables, k_pool, v_pool, q, q_out, rope, kbar_cache, seq_lens, row_starts):
+    if q is not None and q_out is None:
+        q_out = _rows_like(q, desc.n_q_heads, row_starts)
+    st = native(desc, *_rope(rope), q, q_out, k, v, page_tables, seq_lens, row_starts, k_pool, v_pool, kbar_cache)
+    if st < 0:
+        rows = [("k", k, desc.n_kv_heads), ("v", v, desc.n_kv_heads)]
+        if q is not None or q_out is not None:
+            rows += [("q", q, desc.n_q_heads), ("q_out", q_out, desc.n_q_heads)]
+        raise _rows_refused(where, desc, rows, [("k_pool", k_pool, pool_dtype), ("v_pool", v_pool, pool_dtype)], page_tables, seq_lens, row_starts, rope,
+                            kbar_cache)
+    if st != OK:
+        raise OombError(st, where)
+    return q_out
+
+
+def kv_append_rope(desc: RowsDesc, k, v, page_tables, k_pool, v_pool, q=None, q_out=None, rope: Optional[Rope] = None, kbar_cache=None, seq_lens=None,
+                   row_starts=None):
+    """oomb_kv_append_rope: the rows' keys, rotated, and values into their pages (+ the means of the pages they fill into kbar_cache).
+    Returns q rotated (q_out, a new tensor unless given; None without q)."""
+    return _append_rope("oomb_kv_append_rope", (_nb or _native()).kv_append_rope, torch.bfloat16 if desc.dtype == BF16 else torch.float32, desc, k, v,
+                        page_tables, k_pool, v_pool, q, q_out, rope, kbar_cache, seq_lens, row_starts)
+
+
+def kvq_append_rope(desc: RowsDesc, k, v, page_tables, k_pool, v_pool, q=None, q_out=None, rope: Optional[Rope] = None, kbar_cache=None, seq_lens=None,
+                    row_starts=None):
+    """oomb_kvq_append_rope: kv_append_rope into pools of 4-bit codes (kvq_pool)."""
+    return _append_rope("oomb_kvq_append_rope", (_nb or _native()).kvq_append_rope, torch.uint8, desc, k, v, page_tables, k_pool, v_pool, q, q_out, rope,
+                        kbar_cache, seq_lens, row_starts)
+
+
+def kv_append_rope_bwd(desc: RowsDesc, dk_pool, dv_pool, page_tables, d_q=None, rope: Optional[Rope] = None, d_q_out=None, d_k=None, d_v=None,
+                       seq_lens=None, row_starts=None):
+    """oomb_kv_append_rope_bwd: the gradients with respect to the rows that kv_append_rope took, from d_q (of its q_out) and the gradient pools
+    (float32 or bfloat16; desc made with one of them as the pool).  Returns (d_q_out, d_k, d_v), d_q_out None without d_q."""
+    dt = torch.bfloat16 if desc.dtype == BF16 else torch.float32
+    make = torch.empty if row_starts is None else torch.zeros
+    def new(heads):
+        return make((desc.n_rows, heads, desc.head_dim), dtype=dt, device=dk_pool.device)
+    if d_q is not None and d_q_out is None:
+        d_q_out = new(desc.n_q_heads)
+    if d_k is None:
+        d_k = new(desc.n_kv_heads)
+    if d_v is None:
+        d_v = new(desc.n_kv_heads)
+    st = (_nb or _native()).kv_append_rope_bwd(desc, *_rope(rope), d_q, d_q_out, d_k, d_v, page_tables, seq_lens, row_starts, dk_pool, dv_pool)
+    if st < 0:
+        rows = [("d_k", d_k, desc.n_kv_heads), ("d_v", d_v, desc.n_kv_heads)]
+        if d_q is not None or d_q_out is not None:
+            rows += [("d_q", d_q, desc.n_q_heads), ("d_q_out", d_q_out, desc.n_q_heads)]
+        gdt = dk_pool.dtype if dk_pool.dtype == torch.bfloat16 else torch.float32
+        raise _rows_refused("oomb_kv_append_rope_bwd", desc, rows, [("dk_pool", dk_pool, gdt), ("dv_pool", dv_pool, gdt)], page_tables, seq_lens, row_starts, rope)
+    if st != OK:
+        raise OombError(st, "oomb_kv_append_rope_bwd")
+    return d_q_out, d_k, d_v
+
+
+def kvq_read(desc: RowsDesc, k_pool, v_pool, page_tables, k_out=None, v_out=None, seq_lens=None, row_starts=None):
+    """oomb_kvq_read: the rows' values as a cache of 4-bit codes holds them.  Returns (k [n_rows][Hkv][D], v)."""
+    dt = torch.bfloat16 if desc.dtype == BF16 else torch.float32
+    make = torch.empty if row_starts is None else torch.zeros
+    k_out, v_out = (make((desc.n_rows, desc.n_kv_heads, desc.head_dim), dtype=dt, device=k_pool.device) if t is None else t for t in (k_out, v_out))
+    st = (_nb or _native()).kvq_read(desc, page_tables, seq_lens, row_starts, k_pool, v_pool, k_out, v_out)
+    if st < 0:
+        raise _rows_refused("oomb_kvq_read", desc, [("k_out", k_out, desc.n_kv_heads), ("v_out", v_out, desc.n_kv_heads)],
+                            [("k_pool", k_pool, torch.uint8), ("v_pool", v_pool, torch.uint8)], page_tables, seq_lens, row_starts)
+    if st != OK:
+        raise OombError(st, "oomb_kvq_read")
+    return k_out, v_out
+
+
+def kvq_workspace_bytes(desc: RowsDesc, sel_stride: int = -1) -> int:
+    """oomb_kvq_workspace_bytes: what paged_attn_fwd_kvq needs with lists of this row stride (-1: every page); may be 0."""
+    return int(lib().oomb_kvq_workspace_bytes(ctypes.byref(desc), int(sel_stride)))
+
+
+def paged_attn_fwd_kvq(desc: RowsDesc, q, k_pool, v_pool, page_tables, sel_pages=None, sel_count=None, o=None, lse=None, workspace=None, seq_lens=None,
+                       row_starts=None):
+    """oomb_paged_attn_fwd_kvq: attention of the rows over a cache of 4-bit codes, every page or lists [n_seqs][Hkv][stride] ([Hkv][stride] for
+    one sequence).  Returns (O [n_rows][Hq][D], LSE [Hq][n_rows] float32)."""
+    if o is None:
+        o = _rows_like(q, desc.n_q_heads, row_starts)
+    if lse is None:
+        lse = (torch.empty if row_starts is None else torch.zeros)((desc.n_q_heads, desc.n_rows), dtype=torch.float32, device=q.device)
+    if workspace is None:
+        need = kvq_workspace_bytes(desc, -1 if sel_pages is None else int(sel_pages.shape[-1]))
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    st = (_nb or _native()).attn_fwd_kvq(desc, q, k_pool, v_pool, page_tables, seq_lens, row_starts, sel_pages, sel_count, o, lse, workspace)
+    if st < 0:
+        where = "oomb_paged_attn_fwd_kvq"
+        lists = desc.n_seqs * desc.n_kv_heads
+        if lse.dtype != torch.float32 or tuple(lse.shape) != (desc.n_q_heads, desc.n_rows) or not lse.is_contiguous():
+            raise OombError(ERR_INVALID_ARG, f"{where}: lse must be contiguous float32 [{desc.n_q_heads}][{desc.n_rows}]")
+        if sel_pages is not None and (sel_count is None or sel_pages.dtype != torch.int32 or sel_count.dtype != torch.int32 or sel_pages.dim() < 2 or
+                                      not sel_pages.is_contiguous() or not sel_count.is_contiguous() or sel_count.numel() != lists or
+                                      sel_pages.numel() != lists * sel_pages.shape[-1]):
+            raise OombError(ERR_INVALID_ARG, f"{where}: sel_pages must be contiguous int32 [n_seqs][Hkv][stride], sel_count [n_seqs][Hkv]")
+        raise _rows_refused(where, desc, [("q", q, desc.n_q_heads), ("o", o, desc.n_q_heads)],
+                            [("k_pool", k_pool, torch.uint8), ("v_pool", v_pool, torch.uint8)], page_tables, seq_lens, row_starts,
+                            others=[("sel_pages", sel_pages), ("sel_count", sel_count), ("lse", lse), ("workspace", workspace)])
+    if st != OK:
+        raise OombError(st, "oomb_paged_attn_fwd_kvq")
+    return o, lse

@@ -1,0 +1,536 @@
+// Attention of packed rows over a cache of 4-bit codes (layouts: include/oomb.h, rows.h).
+//
+// S^T = K Q^T and O^T += V^T P^T with v_mfma_f32_16x16x32_bf16; a wave holds RT tiles of 16 query rows and walks units of 32
+// tokens (two tiles of 16, each inside a page).  The G query heads of a KV head share its cache: query row r of a sequence and KV head is
+// token r / G, head r % G.
+//   A operand: lane l holds A[l % 16][8 (l / 16) + 0..7], B alike with columns; C/D: lane l, register r holds C[4 (l / 16) + r][l % 16]
+// With lane = 16 kg + m the operands come straight from memory, no LDS and no exchange of lanes:
+//   K   lane (m, kg) reads the codes of dims D/4 kg .. of token m in one load (at D = 128 one block of 32 dims, one scale) and converts a word at a
+//       time into the operands of the steps c; Q is laid out to match: k index 8 kg + j of step c is dim D/4 kg + 8 c + j
+//   P   a lane's accumulators are tokens 4 kg + 0..3 of both tiles of query m: in this order they are the B operand of P^T
+//   V   lane (m, kg) reads those eight tokens' codes of dims D/16 m .. and converts each with its own scale; pairs of tokens are
+//       put together with byte permutes, operand j of O^T holds dims D/16 m + j
+// Conversions are v_cvt_scalef32_pk_bf16_fp4 (two values each, scale applied, exact); every value of the cache is exact in bf16.
+//
+// Softmax in one pass: the running reference of a row moves only when a logit exceeds it by 2^8, which
+// leaves probabilities of at most 256 and sums far inside a float.  Rows of the type bf16 take P in PT terms, fp32 rows Q and P in three (24 bits).
+//
+// Few rows: the four waves of a workgroup share a row block and split its tokens, S workgroups split them further, and
+// kvq_combine adds the parts up (fixed order).  Many rows: every wave has a row block of its own.
+#include "common.h"
+#include "launch.h"
+#include "mfma_common.h"
+#include "rows.h"
+#include "rowsum.h"
+
+namespace oomb {
+
+namespace {
+
+constexpr int WAVES = 4;
+constexpr int THREADS = 64 * WAVES;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float SLACK = 8.0f;            // log2 of how far a logit may exceed the reference
+constexpr int NO_TOKEN = 0x7fffff00;     // position of the tokens of a tile that does not exist
+constexpr int PAD = 4;                   // floats between the rows of a merge buffer: conflict-free for 16-byte accesses
+
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
+__device__ __forceinline__ f32x4 mfma16(const uint4& a, const uint4& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a), as_bf16x8(b), c, 0, 0, 0);
+}
+template <int SEL> __device__ __forceinline__ uint32_t cvt2(uint32_t codes, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, SEL));
+}
+__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+
+// what is left of a and b after their bf16 roundings, packed as `w`
+__device__ __forceinline__ void less(float& a, float& b, uint32_t w) {
+  a -= __uint_as_float(w << 16);
+  b -= __uint_as_float(w & 0xffff0000u);
+}
+
+struct AttnArgs {
+  int splits, row_blocks;      // workgroups along the tokens, row blocks per (sequence, KV head)
+  int share;                   // the waves of a workgroup share a row block and split its tokens
+  float* part;                 // [workgroup][row of the block][D] sums and [workgroup][row][2] (reference, sum), with splits > 1
+  float* part_ml;
+};
+
+// Codes and scales of a unit as a lane reads them.
+template <int D> struct Raw {
+  uint32_t k[2][D / 32];
+  uint32_t ks[2];
+  uint32_t v[2][4];
+  uint32_t vs[2];
+};
+
+template <int D> __device__ __forceinline__ void load_tile(const unsigned char* kt, const unsigned char* vt, int P, int off, int m, int kg, Raw<D>& r, int i) {
+  const int t = off + m;
+  const unsigned char* kc = kt + t * (D / 2) + kg * (D / 8);
+  if constexpr (D == 128) {
+    const uint4 x = *reinterpret_cast<const uint4*>(kc);
+    r.k[i][0] = x.x; r.k[i][1] = x.y; r.k[i][2] = x.z; r.k[i][3] = x.w;
+  } else {
+    const uint2 x = *reinterpret_cast<const uint2*>(kc);
+    r.k[i][0] = x.x; r.k[i][1] = x.y;
+  }
+  const int kb = D == 128 ? kg : kg >> 1, vb = D == 128 ? m >> 2 : m >> 3;
+  r.ks[i] = kt[P * (D / 2) + kb * P + t];
+  const unsigned char* vc = vt + (off + 4 * kg) * (D / 2) + m * (D / 32);
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    r.v[i][j] = D == 128 ? *reinterpret_cast<const uint32_t*>(vc + j * (D / 2)) : *reinterpret_cast<const uint16_t*>(vc + j * (D / 2));
+  r.vs[i] = *reinterpret_cast<const uint32_t*>(vt + P * (D / 2) + vb * P + off + 4 * kg);
+}
+
+// One workgroup's row block: sequence, KV head, rows, and what a wave keeps of it.
+template <typename T, int D, int RT, int PT>
+__global__ __launch_bounds__(THREADS) void attn_kvq_kernel(RowsParams p, AttnArgs a) {
+  extern __shared__ __align__(16) float merge[];
+  constexpr int QT = sizeof(T) == 2 ? 1 : 3, NC = D / 32, NJ = D / 16, ROWS = 16 * RT;
+  const int lane = threadIdx.x & 63, m = lane & 15, kg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int x = blockIdx.x;
+  const int split = x % a.splits;
+  x /= a.splits;
+  const int block = x % a.row_blocks;
+  x /= a.row_blocks;
+  const int g = x % p.Hkv, b = x / p.Hkv;
+  const Seq s = seq_of(p, b);
+  const int n_rows = s.n * p.G;
+  const int r0 = a.share ? block * ROWS : (block * WAVES + wave) * ROWS;
+  if (r0 >= n_rows) return;      // (a workgroup that shares its rows leaves as a whole; the others have no barrier)
+  const int r_last = min(r0 + ROWS, n_rows) - 1;
+  const int min_pos = s.pos + r0 / p.G, max_pos = s.pos + r_last / p.G;
+
+  // queries: row 16 rt + m of the block
+  uint4 q[RT][QT][NC];
+  int pos[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int r = min(r0 + 16 * rt + m, r_last), i = r / p.G, h = g * p.G + (r - i * p.G);
+    pos[rt] = s.pos + i;
+    const T* src = (const T*)p.q.data + (int64_t)(s.row + i) * p.q.tok_stride + (int64_t)h * p.q.head_stride + kg * (D / 4);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      if constexpr (QT == 1) {
+        q[rt][0][c] = *reinterpret_cast<const uint4*>(src + 8 * c);
+      } else {
+        float f[8];
+        Vec16<float>::unpack(reinterpret_cast<const uint4*>(src + 8 * c)[0], f);
+        Vec16<float>::unpack(reinterpret_cast<const uint4*>(src + 8 * c)[1], f + 4);
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+          uint32_t w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            w[e] = pack2_bf16(f[2 * e], f[2 * e + 1]);
+            less(f[2 * e], f[2 * e + 1], w[e]);
+          }
+          q[rt][t][c] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      }
+    }
+  }
+
+  // the tiles that some row sees: entries of the list up to the last row's page
+  const int log_tpp = p.log2_p - 4, n_pages = (p.max_len + p.P - 1) >> p.log2_p;
+  const int32_t* list = p.sel ? p.sel + ((int64_t)b * p.Hkv + g) * p.sel_stride : nullptr;
+  int n_entries = 0, n_tiles = 0;
+  if (max_pos >= 0) {
+    if (list) {
+      int e = min(max(p.sel_count[b * p.Hkv + g], 0), p.sel_stride);
+      while (e > 0) {      // (ascending: the last entry that begins at or before max_pos is near the end)
+        const int base = max(e - 64, 0), at = base + lane;
+        const int id = at < e ? list[at] : -1;
+        const uint64_t seen = __ballot(id >= 0 && id <= (max_pos >> p.log2_p));
+        if (seen) {
+          n_entries = base + 64 - __builtin_clzll(seen);
+          break;
+        }
+        e = base;
+      }
+      n_tiles = n_entries << log_tpp;
+    } else {
+      n_tiles = (max_pos >> 4) + 1;
+      n_entries = (max_pos >> p.log2_p) + 1;
+    }
+  }
+  const int n_units = (n_tiles + 1) >> 1;
+  const int parts = a.share ? a.splits * WAVES : a.splits, part = a.share ? split * WAVES + wave : split;
+  int u = (int)((int64_t)n_units * part / parts);
+  const int u_end = (int)((int64_t)n_units * (part + 1) / parts);
+
+  f32x4 acc[RT][NJ];
+  float ref[RT], sum[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    ref[rt] = -INFINITY;
+    sum[rt] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[rt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float scale = p.sm_scale * LOG2E;
+
+  // pages of 64 consecutive entries, one per lane; tile -> (page pointers, position of its first token)
+  int win = -128, w_log = 0, w_phys = -1;
+  auto window = [&](int e0) __attribute__((always_inline)) {
+    win = e0;
+    const int e = e0 + lane;
+    w_log = e < n_entries ? (list ? list[e] : e) : -1;
+    w_phys = w_log >= 0 && w_log < n_pages ? page_of(p, b, w_log) : -1;
+  };
+  const unsigned char* kbase = (const unsigned char*)p.k_pool + (int64_t)g * p.pool_head_stride;
+  const unsigned char* vbase = (const unsigned char*)p.v_pool + (int64_t)g * p.pool_head_stride;
+  struct Tile { const unsigned char *k, *v; int off, t0; };
+  auto tile_at = [&](int t) __attribute__((always_inline)) {
+    const int e = t >> log_tpp, off = (t & ((1 << log_tpp) - 1)) << 4;
+    if (t >= n_tiles) return Tile{kbase, vbase, 0, NO_TOKEN};
+    const int phys = __builtin_amdgcn_readlane(w_phys, e - win), page = __builtin_amdgcn_readlane(w_log, e - win);
+    if (phys < 0) return Tile{kbase, vbase, 0, NO_TOKEN};
+    return Tile{kbase + (int64_t)phys * p.pool_page_stride, vbase + (int64_t)phys * p.pool_page_stride, off, (page << p.log2_p) + off};
+  };
+  Raw<D> raw;
+  Tile tile[2];
+  auto fetch = [&](int unit, Raw<D>& r, Tile (&tl)[2]) __attribute__((always_inline)) {
+    const int e0 = (2 * unit) >> log_tpp, e1 = (2 * unit + 1) >> log_tpp;
+    if (e1 - win >= 64 || win < 0) window(e0);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      tl[i] = tile_at(2 * unit + i);
+      load_tile<D>(tl[i].k, tl[i].v, p.P, tl[i].off, m, kg, r, i);
+    }
+  };
+
+  if (u < u_end) fetch(u, raw, tile);
+  while (u < u_end) {
+    Raw<D> next;
+    Tile next_tile[2];
+    if (u + 1 < u_end) fetch(u + 1, next, next_tile);
+    const bool masked = max(tile[0].t0, tile[1].t0) + 15 > min_pos;
+
+    // S^T
+    f32x4 st[RT][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float ks = kvq_scale(raw.ks[i]);
+      uint4 kf[NC];
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        kf[c] = make_uint4(cvt2<0>(raw.k[i][c], ks), cvt2<1>(raw.k[i][c], ks), cvt2<2>(raw.k[i][c], ks), cvt2<3>(raw.k[i][c], ks));
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        st[rt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int t = QT - 1; t >= 0; --t)
+#pragma unroll
+          for (int c = 0; c < NC; ++c) st[rt][i] = mfma16(kf[c], q[rt][t][c], st[rt][i]);
+      }
+    }
+
+    // Tokens that not every row sees.  Their V is zero where nothing of it is seen (it may be anything) and where it is NaN: a
+    // weight of zero does not stop a NaN, so the rows that do see it get theirs below.
+    bool nan_seen = false;
+    if (masked) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int t = tile[i].t0 + 4 * kg + j;
+          const bool partly = t > min_pos, unseen = t > max_pos, bad = ((raw.vs[i] >> (8 * j)) & 255) == 255;
+          if (partly && (unseen || bad)) {
+            raw.v[i][j] = 0;
+            raw.vs[i] = (raw.vs[i] & ~(255u << (8 * j))) | (127u << (8 * j));
+          }
+          nan_seen |= partly && !unseen && bad;
+        }
+      }
+    }
+
+    uint4 pf[RT][PT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float z[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] = st[rt][e >> 2][e & 3] * scale;
+      if (masked) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = tile[e >> 2].t0 + 4 * kg + (e & 3) <= pos[rt] ? z[e] : -INFINITY;
+      }
+      float top = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
+      if (__any(top > ref[rt] + SLACK)) {
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float to = fmaxf(ref[rt], top);
+        const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref[rt] - to);
+        ref[rt] = to;
+        sum[rt] *= f;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[rt][j] *= f;
+      }
+      const float from = ref[rt] == -INFINITY ? 0.0f : ref[rt];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        z[e] = __builtin_amdgcn_exp2f(z[e] - from);
+        sum[rt] += z[e];
+      }
+#pragma unroll
+      for (int t = 0; t < PT; ++t) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          w[e] = pack2_bf16(z[2 * e], z[2 * e + 1]);
+          if (t + 1 < PT) less(z[2 * e], z[2 * e + 1], w[e]);
+        }
+        pf[rt][t] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+
+    // V: pairs of tokens (i, 2 y), (i, 2 y + 1) -> word 2 i + y of the operands
+    uint32_t vf[NJ][4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const float sa = kvq_scale((raw.vs[i] >> (16 * y)) & 255), sb = kvq_scale((raw.vs[i] >> (16 * y + 8)) & 255);
+        const uint32_t ca = raw.v[i][2 * y], cb = raw.v[i][2 * y + 1];
+        uint32_t xa[4], xb[4];
+        xa[0] = cvt2<0>(ca, sa); xb[0] = cvt2<0>(cb, sb);
+        xa[1] = cvt2<1>(ca, sa); xb[1] = cvt2<1>(cb, sb);
+        if constexpr (D == 128) {
+          xa[2] = cvt2<2>(ca, sa); xb[2] = cvt2<2>(cb, sb);
+          xa[3] = cvt2<3>(ca, sa); xb[3] = cvt2<3>(cb, sb);
+        }
+#pragma unroll
+        for (int j = 0; j < NJ / 2; ++j) {
+          vf[2 * j][2 * i + y] = low_halves(xa[j], xb[j]);
+          vf[2 * j + 1][2 * i + y] = high_halves(xa[j], xb[j]);
+        }
+      }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const uint4 va = make_uint4(vf[j][0], vf[j][1], vf[j][2], vf[j][3]);
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int t = PT - 1; t >= 0; --t) acc[rt][j] = mfma16(va, pf[rt][t], acc[rt][j]);
+    }
+
+    if (__any(nan_seen)) {
+      const int vb = D == 128 ? kg : kg >> 1;      // this lane's output dims are D/4 kg .. + D/4 - 1
+      for (int i = 0; i < 2; ++i)
+        for (int t = 0; t < 16; ++t) {
+          const int at = tile[i].t0 + t;
+          if (at <= min_pos || at > max_pos) continue;
+          if (tile[i].v[p.P * (D / 2) + vb * p.P + tile[i].off + t] != 255) continue;
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt)
+            if (at <= pos[rt]) {
+#pragma unroll
+              for (int j = 0; j < NJ; ++j) acc[rt][j] = f32x4{NAN, NAN, NAN, NAN};
+            }
+        }
+    }
+    raw = next;
+    tile[0] = next_tile[0];
+    tile[1] = next_tile[1];
+    ++u;
+  }
+
+  // lane (m, kg): query m, dims D/4 kg + D/16 i + j of acc[.][j][i]
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    sum[rt] += __shfl_xor(sum[rt], 16, 64);
+    sum[rt] += __shfl_xor(sum[rt], 32, 64);
+  }
+  auto put = [&](int r, int d, const float* y, float ref_r, float sum_r, bool first) __attribute__((always_inline)) {   // four dims of row r of the block
+    const int row = r0 + r;
+    if (row >= n_rows) return;
+    if (a.splits > 1) {
+      const int64_t at = (int64_t)blockIdx.x * ROWS + r;
+      *reinterpret_cast<float4*>(a.part + at * D + d) = make_float4(y[0], y[1], y[2], y[3]);
+      if (first) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(ref_r, sum_r);
+      return;
+    }
+    const int i = row / p.G, h = g * p.G + (row - i * p.G);
+    const float f = sum_r == 0.0f ? 0.0f : 1.0f / sum_r;
+    T* dst = (T*)p.q_out.data + (int64_t)(s.row + i) * p.q_out.tok_stride + (int64_t)h * p.q_out.head_stride + d;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(pack2_bf16(y[0] * f, y[1] * f), pack2_bf16(y[2] * f, y[3] * f));
+    else *reinterpret_cast<float4*>(dst) = make_float4(y[0] * f, y[1] * f, y[2] * f, y[3] * f);
+    if (first) p.lse[(int64_t)h * p.n_rows + s.row + i] = sum_r == 0.0f ? -INFINITY : (ref_r + __builtin_amdgcn_logf(sum_r)) * LN2;
+  };
+
+  if (!a.share) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; j += 4) {
+          const float y[4] = {acc[rt][j][i], acc[rt][j + 1][i], acc[rt][j + 2][i], acc[rt][j + 3][i]};
+          put(16 * rt + m, (D / 4) * kg + NJ * i + j, y, ref[rt], sum[rt], i == 0 && j == 0 && kg == 0);
+        }
+    return;
+  }
+
+  // the four waves' sums, one row tile at a time: [wave][16][D + PAD] floats, [wave][16][2] references and sums
+  float* ml = merge + WAVES * 16 * (D + PAD);
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    if (rt) __syncthreads();
+    if (kg == 0) *reinterpret_cast<float2*>(ml + (wave * 16 + m) * 2) = make_float2(ref[rt], sum[rt]);
+    __syncthreads();
+    float to = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) to = fmaxf(to, ml[(w * 16 + m) * 2]);
+    const float f = ref[rt] == to ? 1.0f : __builtin_amdgcn_exp2f(ref[rt] - to);
+    float* mine = merge + (wave * 16 + m) * (D + PAD) + (D / 4) * kg;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; j += 4)
+        *reinterpret_cast<float4*>(mine + NJ * i + j) = make_float4(acc[rt][j][i] * f, acc[rt][j + 1][i] * f, acc[rt][j + 2][i] * f, acc[rt][j + 3][i] * f);
+    __syncthreads();
+    for (int e = threadIdx.x; e < 16 * (D / 4); e += THREADS) {
+      const int r = e / (D / 4), d = (e - r * (D / 4)) * 4;
+      float y[4] = {0.f, 0.f, 0.f, 0.f}, ref_r = -INFINITY, sum_r = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) ref_r = fmaxf(ref_r, ml[(w * 16 + r) * 2]);
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        const float4 v = *reinterpret_cast<const float4*>(merge + (w * 16 + r) * (D + PAD) + d);
+        const float rw = ml[(w * 16 + r) * 2], sw = ml[(w * 16 + r) * 2 + 1];
+        sum_r += sw * (rw == ref_r ? 1.0f : __builtin_amdgcn_exp2f(rw - ref_r));
+        y[0] += v.x; y[1] += v.y; y[2] += v.z; y[3] += v.w;
+      }
+      put(16 * rt + r, d, y, ref_r, sum_r, d == 0);
+    }
+  }
+}
+
+// The parts of a row, in order: a workgroup per row of a row block, its threads in groups of D / 4 that take every
+// (256 / (D / 4))-th part each.
+template <typename T, int D>
+__global__ __launch_bounds__(THREADS) void kvq_combine_kernel(RowsParams p, AttnArgs a, int rows) {
+  constexpr int LANES = D / 4, GROUPS = THREADS / LANES;
+  __shared__ __align__(16) float lds[GROUPS][D + PAD];
+  __shared__ float lds_ml[GROUPS][2];
+  int x = blockIdx.x;
+  const int r = x % rows;
+  x /= rows;
+  const int tile = x;
+  const int block = x % a.row_blocks;
+  x /= a.row_blocks;
+  const int g = x % p.Hkv, b = x / p.Hkv;
+  const Seq s = seq_of(p, b);
+  const int row = block * rows + r;
+  if (row >= s.n * p.G) return;
+  const int grp = threadIdx.x / LANES, d = (threadIdx.x - grp * LANES) * 4;
+  float ref = -INFINITY, sum = 0.0f, y[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int k = grp; k < a.splits; k += GROUPS) {
+    const int64_t at = ((int64_t)tile * a.splits + k) * rows + r;
+    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
+    const float4 v = *reinterpret_cast<const float4*>(a.part + at * D + d);
+    const float to = fmaxf(ref, ml.x);
+    const float f0 = ref == to ? 1.0f : __builtin_amdgcn_exp2f(ref - to), f1 = ml.x == to ? 1.0f : __builtin_amdgcn_exp2f(ml.x - to);
+    ref = to;
+    sum = sum * f0 + ml.y * f1;
+    y[0] = y[0] * f0 + v.x * f1; y[1] = y[1] * f0 + v.y * f1; y[2] = y[2] * f0 + v.z * f1; y[3] = y[3] * f0 + v.w * f1;
+  }
+  *reinterpret_cast<float4*>(&lds[grp][d]) = make_float4(y[0], y[1], y[2], y[3]);
+  if (d == 0) { lds_ml[grp][0] = ref; lds_ml[grp][1] = sum; }
+  __syncthreads();
+  if (grp) return;
+  float top = -INFINITY, total = 0.0f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < GROUPS; ++k) top = fmaxf(top, lds_ml[k][0]);
+#pragma unroll
+  for (int k = 0; k < GROUPS; ++k) {
+    const float f = lds_ml[k][0] == top ? 1.0f : __builtin_amdgcn_exp2f(lds_ml[k][0] - top);
+    const float4 v = *reinterpret_cast<const float4*>(&lds[k][d]);
+    total += lds_ml[k][1] * f;
+    o[0] += v.x * f; o[1] += v.y * f; o[2] += v.z * f; o[3] += v.w * f;
+  }
+  const int i = row / p.G, h = g * p.G + (row - i * p.G);
+  const float f = total == 0.0f ? 0.0f : 1.0f / total;
+  T* dst = (T*)p.q_out.data + (int64_t)(s.row + i) * p.q_out.tok_stride + (int64_t)h * p.q_out.head_stride + d;
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(pack2_bf16(o[0] * f, o[1] * f), pack2_bf16(o[2] * f, o[3] * f));
+  else *reinterpret_cast<float4*>(dst) = make_float4(o[0] * f, o[1] * f, o[2] * f, o[3] * f);
+  if (d == 0) p.lse[(int64_t)h * p.n_rows + s.row + i] = total == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * LN2;
+}
+
+// How a call is cut: row tiles per wave, whether waves share rows, row blocks and splits.
+struct Plan {
+  int rt, share, row_blocks, splits;   // (splits > 1 only with share)
+};
+Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
+  Plan c{};
+  const int64_t rows = (int64_t)p.max_rows * p.G, heads = (int64_t)p.n_seqs * p.Hkv;
+  const int most = is_bf16 ? 4 : 2;
+  c.rt = rows <= 16 ? 1 : rows <= 32 || most == 2 ? 2 : 4;
+  const int64_t own = (rows + 16 * c.rt * WAVES - 1) / (16 * c.rt * WAVES);
+  c.share = own * heads < 256;
+  c.row_blocks = (int)(c.share ? (rows + 16 * c.rt - 1) / (16 * c.rt) : own);
+  c.splits = 1;
+  if (c.share) {
+    int64_t tokens = p.max_len;
+    if (sel_stride >= 0 && (int64_t)sel_stride * p.P < tokens) tokens = (int64_t)sel_stride * p.P;
+    const int64_t wgs = heads * c.row_blocks, most_splits = tokens / (32 * WAVES * 4);
+    int64_t want = 512 / (wgs ? wgs : 1);
+    if (want > most_splits) want = most_splits;
+    c.splits = (int)(want < 1 ? 1 : want);
+  }
+  return c;
+}
+
+template <typename T, int D, int RT, int PT> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
+  AttnArgs a{c.splits, c.row_blocks, c.share, nullptr, nullptr};
+  const int64_t blocks = (int64_t)p.n_seqs * p.Hkv * c.row_blocks;
+  if (c.splits > 1) {
+    a.part = (float*)ws;
+    a.part_ml = a.part + blocks * c.splits * 16 * RT * D;
+  }
+  {
+    ProfScope prof_("attn_kvq", st);
+    const size_t lds = c.share ? (size_t)(WAVES * 16 * (D + PAD) + WAVES * 16 * 2) * sizeof(float) : 0;
+    attn_kvq_kernel<T, D, RT, PT><<<dim3((unsigned)(blocks * c.splits)), dim3(THREADS), lds, st>>>(p, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || c.splits == 1) return e;
+  }
+  ProfScope prof_("kvq_combine", st);
+  kvq_combine_kernel<T, D><<<dim3((unsigned)(blocks * 16 * RT)), dim3(THREADS), 0, st>>>(p, a, 16 * RT);
+  return hipGetLastError();
+}
+template <typename T, int D> hipError_t attn(const RowsParams& p, void* ws, hipStream_t st) {
+  constexpr bool BF = sizeof(T) == 2;
+  const Plan c = plan_of(p, BF, p.sel ? p.sel_stride : -1);
+  if constexpr (BF) {
+    if (c.rt == 1) return run<T, D, 1, 2>(p, c, ws, st);
+    if (c.rt == 2) return run<T, D, 2, 2>(p, c, ws, st);
+    return run<T, D, 4, 1>(p, c, ws, st);
+  } else {
+    return c.rt == 1 ? run<T, D, 1, 3>(p, c, ws, st) : run<T, D, 2, 3>(p, c, ws, st);
+  }
+}
+
+}  // namespace
+
+size_t kvq_attn_workspace_bytes(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
+  const Plan c = plan_of(p, is_bf16, sel_stride);
+  if (c.splits == 1) return 0;
+  return (size_t)p.n_seqs * p.Hkv * c.row_blocks * c.splits * 16 * c.rt * (p.D + 2) * sizeof(float);
+}
+int64_t kvq_attn_blocks(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
+  const Plan c = plan_of(p, is_bf16, sel_stride);
+  const int64_t blocks = (int64_t)p.n_seqs * p.Hkv * c.row_blocks;
+  return blocks * (c.splits > 16 * c.rt ? c.splits : 16 * c.rt);
+}
+
+hipError_t launch_attn_kvq(const RowsParams& p, bool is_bf16, void* ws, hipStream_t st) {
+  if (is_bf16) return p.D == 128 ? attn<bf16_t, 128>(p, ws, st) : attn<bf16_t, 64>(p, ws, st);
+  return p.D == 128 ? attn<float, 128>(p, ws, st) : attn<float, 64>(p, ws, st);
+}
+
+}  // namespace oomb
