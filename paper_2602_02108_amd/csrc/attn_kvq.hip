@@ -1,22 +1,28 @@
 // Attention of packed rows over a cache of 4-bit codes (layouts: include/oomb.h, rows.h).
 //
-// S^T = K Q^T and O^T += V^T P^T with v_mfma_f32_16x16x32_bf16; a wave holds RT tiles of 16 query rows and walks units of 32
-// tokens (two tiles of 16, each inside a page).  The G query heads of a KV head share its cache: query row r of a sequence and KV head is
-// token r / G, head r % G.
-//   A operand: lane l holds A[l % 16][8 (l / 16) + 0..7], B alike with columns; C/D: lane l, register r holds C[4 (l / 16) + r][l % 16]
-// With lane = 16 kg + m the operands come straight from memory, no LDS and no exchange of lanes:
-//   K   lane (m, kg) reads the codes of dims D/4 kg .. of token m in one load (at D = 128 one block of 32 dims, one scale) and converts a word at a
-//       time into the operands of the steps c; Q is laid out to match: k index 8 kg + j of step c is dim D/4 kg + 8 c + j
-//   P   a lane's accumulators are tokens 4 kg + 0..3 of both tiles of query m: in this order they are the B operand of P^T
-//   V   lane (m, kg) reads those eight tokens' codes of dims D/16 m .. and converts each with its own scale; pairs of tokens are
-//       put together with byte permutes, operand j of O^T holds dims D/16 m + j
-// Conversions are v_cvt_scalef32_pk_bf16_fp4 (two values each, scale applied, exact); every value of the cache is exact in bf16.
+// A wave holds RT tiles of 16 query rows and walks units of 32 tokens (two tiles of 16, each inside a page); the G query heads of
+// a KV head share its cache: query row r of a sequence and KV head is token r / G, head r % G.  Operands come straight from
+// memory, no LDS and no exchange of lanes.  With lane = 16 kg + m:
+//   v_mfma_f32_16x16x32_bf16: lane l holds A[l % 16][8 (l / 16) + 0..7], B alike with columns, C[4 (l / 16) + r][l % 16] in register r
+//   S^T = K Q^T: lane (m, kg) reads the codes of dims D/4 kg .. of token m in one load (at D = 128 one block of 32 dims, one scale)
+//       and converts a word at a time into the operands of the steps c; the queries are laid out to match: k index 8 kg + j of step c is dim
+//       D/4 kg + 8 c + j
+//   O^T += V^T P^T: a lane's accumulators of S^T are tokens 4 kg + 0..3 of both tiles of query m: in this order they are the B operand.
+//       For the A operand lane (m, kg) reads those eight tokens' codes of dims D/16 m .., converts each with its own scale and puts pairs of tokens
+//       together with byte permutes; operand j holds dims D/16 m + j
+// Conversions are v_cvt_scalef32_pk_bf16_fp4 (two values each, scale applied, exact); every value of the cache is exact in bf16.  fp32
+// rows: Q and P in three bf16 terms (24 bits).  bf16 rows: P in two (16 bits) where that is free, in one with 64 rows to a wave.  (The codes
+// could be a matrix operand as they are, v_mfma_scale_f32_16x16x128_f8f6f4 against e4m3 terms of the queries: its sums were off by
+// 2^-16 of the largest product, 2^-24 here.)
 //
-// Softmax in one pass: the running reference of a row moves only when a logit exceeds it by 2^8, which
-// leaves probabilities of at most 256 and sums far inside a float.  Rows of the type bf16 take P in PT terms, fp32 rows Q and P in three (24 bits).
+// Softmax in one pass: weights are taken against a reference of the row that moves only when the eight weights of a lane in a unit
+// exceed 2^9 together; so no maximum is formed on the way, and sums stay far inside a float.
 //
-// Few rows: the four waves of a workgroup share a row block and split its tokens, S workgroups split them further, and
-// kvq_combine adds the parts up (fixed order).  Many rows: every wave has a row block of its own.
+// Few rows: the waves of a workgroup share a row block and split its tokens; long caches are cut into parts of equal work over
+// workgroups, counted on the device from the lengths as they are, and kvq_combine adds a row's parts in their order.  Many rows: every wave has a row
+// block of its own.
+#include <type_traits>
+
 #include "common.h"
 #include "launch.h"
 #include "mfma_common.h"
@@ -27,12 +33,12 @@ namespace oomb {
 
 namespace {
 
-constexpr int WAVES = 4;
-constexpr int THREADS = 64 * WAVES;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr float SLACK = 8.0f;            // log2 of how far a logit may exceed the reference
+constexpr float MOST = 512.0f;           // of a lane's weights of a unit, before the reference moves
 constexpr int NO_TOKEN = 0x7fffff00;     // position of the tokens of a tile that does not exist
 constexpr int PAD = 4;                   // floats between the rows of a merge buffer: conflict-free for 16-byte accesses
+constexpr int COMBINE_THREADS = 256;
+constexpr int WGS = 512;                 // workgroups that a call is cut into
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 
@@ -52,10 +58,13 @@ __device__ __forceinline__ void less(float& a, float& b, uint32_t w) {
 }
 
 struct AttnArgs {
-  int splits, row_blocks;      // workgroups along the tokens, row blocks per (sequence, KV head)
+  int row_blocks;              // per (sequence, KV head)
   int share;                   // the waves of a workgroup share a row block and split its tokens
-  float* part;                 // [workgroup][row of the block][D] sums and [workgroup][row][2] (reference, sum), with splits > 1
-  float* part_ml;
+  int split;                   // parts over workgroups (else one part per (sequence, KV head))
+  int target, min_units;       // parts to aim at; units of a part at least
+  int2* parts;                 // [sequence * Hkv + KV head]: first part, number of parts
+  float* part;                 // [part][row block][row of the block][D] sums
+  float* part_ml;              // [part][row block][row][2]: reference, sum
 };
 
 // Codes and scales of a unit as a lane reads them.
@@ -85,22 +94,89 @@ template <int D> __device__ __forceinline__ void load_tile(const unsigned char* 
   r.vs[i] = *reinterpret_cast<const uint32_t*>(vt + P * (D / 2) + vb * P + off + 4 * kg);
 }
 
-// One workgroup's row block: sequence, KV head, rows, and what a wave keeps of it.
-template <typename T, int D, int RT, int PT>
-__global__ __launch_bounds__(THREADS) void attn_kvq_kernel(RowsParams p, AttnArgs a) {
+// This lane's D / 4 dims of a query row, as operands of the steps and terms.
+template <typename T, int D, int QT> __device__ __forceinline__ void query_terms(const T* row, uint4 (&q)[QT][D / 32]) {
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) {
+    if constexpr (QT == 1) {
+      q[0][c] = *reinterpret_cast<const uint4*>(row + 8 * c);
+    } else {
+      float f[8];
+      Vec16<float>::unpack(reinterpret_cast<const uint4*>(row + 8 * c)[0], f);
+      Vec16<float>::unpack(reinterpret_cast<const uint4*>(row + 8 * c)[1], f + 4);
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          w[e] = pack2_bf16(f[2 * e], f[2 * e + 1]);
+          less(f[2 * e], f[2 * e + 1], w[e]);
+        }
+        q[t][c] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+  }
+}
+
+// ---- the parts of a call ------------------------------------------------------------------------------------------------
+// A bound of the units that the rows of (sequence, KV head) e see, -1 if it has no rows.
+__device__ __forceinline__ int units_of(const RowsParams& p, int e) {
+  const int b = e / p.Hkv;
+  const Seq s = seq_of(p, b);
+  if (s.n == 0) return -1;
+  const int64_t tokens = p.sel ? (int64_t)min(max(p.sel_count[e], 0), p.sel_stride) * p.P : s.len;
+  return (int)((min(tokens, (int64_t)p.max_len) + 31) >> 5);
+}
+struct Part { int e, first, index, count; };   // (sequence, KV head), its first part, this one of it, its number of parts
+// Part x of the call, by every lane of a wave; e < 0: there are fewer.
+__device__ __forceinline__ Part part_at(const RowsParams& p, const AttnArgs& a, int x, int lane) {
+  const int n = p.n_seqs * p.Hkv;
+  if (!a.split) return {x, x, 0, 1};
+  float total = 0.0f;
+  int mine = -1;
+  for (int e = lane; e < n; e += 64) {
+    mine = units_of(p, e);
+    total += (float)max(mine, 0);
+  }
+#pragma unroll
+  for (int w = 1; w < 64; w *= 2) total += __shfl_xor(total, w, 64);
+  const int per = max(a.min_units, (int)(total / (float)a.target) + 1);   // (the same sum in every wave of both kernels)
+  int before = 0;
+  for (int e0 = 0; e0 < n; e0 += 64) {
+    const int e = e0 + lane;
+    const int units = n <= 64 ? mine : e < n ? units_of(p, e) : -1;
+    const int parts = units < 0 ? 0 : max(1, (units + per - 1) / per);
+    int upto = parts;
+#pragma unroll
+    for (int w = 1; w < 64; w *= 2) {
+      const int y = __shfl_up(upto, w, 64);
+      if (lane >= w) upto += y;
+    }
+    const uint64_t past = __ballot(before + upto > x);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      const int count = __builtin_amdgcn_readlane(parts, l), first = before + __builtin_amdgcn_readlane(upto, l) - count;
+      return {e0 + l, first, x - first, count};
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return {-1, 0, 0, 0};
+}
+
+template <typename T, int D, int RT, int PT, int W>
+__global__ __launch_bounds__(64 * W, RT == 4 ? 1 : 2) void attn_kvq_kernel(RowsParams p, AttnArgs a) {
   extern __shared__ __align__(16) float merge[];
   constexpr int QT = sizeof(T) == 2 ? 1 : 3, NC = D / 32, NJ = D / 16, ROWS = 16 * RT;
   const int lane = threadIdx.x & 63, m = lane & 15, kg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int x = blockIdx.x;
-  const int split = x % a.splits;
-  x /= a.splits;
-  const int block = x % a.row_blocks;
-  x /= a.row_blocks;
-  const int g = x % p.Hkv, b = x / p.Hkv;
+  const int px = blockIdx.x / a.row_blocks, block = blockIdx.x - px * a.row_blocks;
+  const Part part = part_at(p, a, px, lane);
+  if (part.e < 0) return;
+  const int b = part.e / p.Hkv, g = part.e - b * p.Hkv;
   const Seq s = seq_of(p, b);
+  if (a.split && part.index == 0 && block == 0 && threadIdx.x == 0) a.parts[part.e] = make_int2(part.first, part.count);
   const int n_rows = s.n * p.G;
-  const int r0 = a.share ? block * ROWS : (block * WAVES + wave) * ROWS;
+  const int r0 = a.share ? block * ROWS : (block * W + wave) * ROWS;
   if (r0 >= n_rows) return;      // (a workgroup that shares its rows leaves as a whole; the others have no barrier)
   const int r_last = min(r0 + ROWS, n_rows) - 1;
   const int min_pos = s.pos + r0 / p.G, max_pos = s.pos + r_last / p.G;
@@ -112,36 +188,16 @@ __global__ __launch_bounds__(THREADS) void attn_kvq_kernel(RowsParams p, AttnArg
   for (int rt = 0; rt < RT; ++rt) {
     const int r = min(r0 + 16 * rt + m, r_last), i = r / p.G, h = g * p.G + (r - i * p.G);
     pos[rt] = s.pos + i;
-    const T* src = (const T*)p.q.data + (int64_t)(s.row + i) * p.q.tok_stride + (int64_t)h * p.q.head_stride + kg * (D / 4);
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      if constexpr (QT == 1) {
-        q[rt][0][c] = *reinterpret_cast<const uint4*>(src + 8 * c);
-      } else {
-        float f[8];
-        Vec16<float>::unpack(reinterpret_cast<const uint4*>(src + 8 * c)[0], f);
-        Vec16<float>::unpack(reinterpret_cast<const uint4*>(src + 8 * c)[1], f + 4);
-#pragma unroll
-        for (int t = 0; t < QT; ++t) {
-          uint32_t w[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            w[e] = pack2_bf16(f[2 * e], f[2 * e + 1]);
-            less(f[2 * e], f[2 * e + 1], w[e]);
-          }
-          q[rt][t][c] = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-      }
-    }
+    query_terms<T, D, QT>((const T*)p.q.data + (int64_t)(s.row + i) * p.q.tok_stride + (int64_t)h * p.q.head_stride + kg * (D / 4), q[rt]);
   }
 
   // the tiles that some row sees: entries of the list up to the last row's page
   const int log_tpp = p.log2_p - 4, n_pages = (p.max_len + p.P - 1) >> p.log2_p;
-  const int32_t* list = p.sel ? p.sel + ((int64_t)b * p.Hkv + g) * p.sel_stride : nullptr;
+  const int32_t* list = p.sel ? p.sel + (int64_t)part.e * p.sel_stride : nullptr;
   int n_entries = 0, n_tiles = 0;
   if (max_pos >= 0) {
     if (list) {
-      int e = min(max(p.sel_count[b * p.Hkv + g], 0), p.sel_stride);
+      int e = min(max(p.sel_count[part.e], 0), p.sel_stride);
       while (e > 0) {      // (ascending: the last entry that begins at or before max_pos is near the end)
         const int base = max(e - 64, 0), at = base + lane;
         const int id = at < e ? list[at] : -1;
@@ -159,9 +215,9 @@ __global__ __launch_bounds__(THREADS) void attn_kvq_kernel(RowsParams p, AttnArg
     }
   }
   const int n_units = (n_tiles + 1) >> 1;
-  const int parts = a.share ? a.splits * WAVES : a.splits, part = a.share ? split * WAVES + wave : split;
-  int u = (int)((int64_t)n_units * part / parts);
-  const int u_end = (int)((int64_t)n_units * (part + 1) / parts);
+  const int parts = a.share ? part.count * W : 1, mine = a.share ? part.index * W + wave : 0;
+  int u = (int)((int64_t)n_units * mine / parts);
+  const int u_end = (int)((int64_t)n_units * (mine + 1) / parts);
 
   f32x4 acc[RT][NJ];
   float ref[RT], sum[RT];
@@ -192,8 +248,6 @@ __global__ __launch_bounds__(THREADS) void attn_kvq_kernel(RowsParams p, AttnArg
     if (phys < 0) return Tile{kbase, vbase, 0, NO_TOKEN};
     return Tile{kbase + (int64_t)phys * p.pool_page_stride, vbase + (int64_t)phys * p.pool_page_stride, off, (page << p.log2_p) + off};
   };
-  Raw<D> raw;
-  Tile tile[2];
   auto fetch = [&](int unit, Raw<D>& r, Tile (&tl)[2]) __attribute__((always_inline)) {
     const int e0 = (2 * unit) >> log_tpp, e1 = (2 * unit + 1) >> log_tpp;
     if (e1 - win >= 64 || win < 0) window(e0);
@@ -204,13 +258,8 @@ __global__ __launch_bounds__(THREADS) void attn_kvq_kernel(RowsParams p, AttnArg
     }
   };
 
-  if (u < u_end) fetch(u, raw, tile);
-  while (u < u_end) {
-    Raw<D> next;
-    Tile next_tile[2];
-    if (u + 1 < u_end) fetch(u + 1, next, next_tile);
+  auto unit = [&](Raw<D>& raw, const Tile (&tile)[2]) __attribute__((always_inline)) {
     const bool masked = max(tile[0].t0, tile[1].t0) + 15 > min_pos;
-
     // S^T
     f32x4 st[RT][2];
 #pragma unroll
@@ -221,13 +270,13 @@ __global__ __launch_bounds__(THREADS) void attn_kvq_kernel(RowsParams p, AttnArg
       for (int c = 0; c < NC; ++c)
         kf[c] = make_uint4(cvt2<0>(raw.k[i][c], ks), cvt2<1>(raw.k[i][c], ks), cvt2<2>(raw.k[i][c], ks), cvt2<3>(raw.k[i][c], ks));
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        st[rt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int rt = 0; rt < RT; ++rt) st[rt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int t = QT - 1; t >= 0; --t)
+      for (int t = QT - 1; t >= 0; --t)
 #pragma unroll
-          for (int c = 0; c < NC; ++c) st[rt][i] = mfma16(kf[c], q[rt][t][c], st[rt][i]);
-      }
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) st[rt][i] = mfma16(kf[c], q[rt][t][c], st[rt][i]);
     }
 
     // Tokens that not every row sees.  Their V is zero where nothing of it is seen (it may be anything) and where it is NaN: a
@@ -249,18 +298,31 @@ __global__ __launch_bounds__(THREADS) void attn_kvq_kernel(RowsParams p, AttnArg
       }
     }
 
-    uint4 pf[RT][PT];
+    float z[RT][8], all[RT];
+    auto weights = [&](int rt) __attribute__((always_inline)) {
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      float z[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] = st[rt][e >> 2][e & 3] * scale;
+      for (int e = 0; e < 8; ++e) z[rt][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[rt][e >> 2][e & 3], scale, -ref[rt]));
       if (masked) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) z[e] = tile[e >> 2].t0 + 4 * kg + (e & 3) <= pos[rt] ? z[e] : -INFINITY;
+        for (int e = 0; e < 8; ++e) z[rt][e] = tile[e >> 2].t0 + 4 * kg + (e & 3) <= pos[rt] ? z[rt][e] : 0.0f;
       }
-      float top = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
-      if (__any(top > ref[rt] + SLACK)) {
+      all[rt] = ((z[rt][0] + z[rt][1]) + (z[rt][2] + z[rt][3])) + ((z[rt][4] + z[rt][5]) + (z[rt][6] + z[rt][7]));
+    };
+    float most = 0.0f;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      weights(rt);
+      most = fmaxf(most, all[rt]);
+    }
+    if (__any(most > MOST)) {   // (the first unit of a row: its reference is -infinity)
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const bool seen = !masked || tile[e >> 2].t0 + 4 * kg + (e & 3) <= pos[rt];
+          top = fmaxf(top, seen ? st[rt][e >> 2][e & 3] * scale : -INFINITY);
+        }
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
         const float to = fmaxf(ref[rt], top);
@@ -269,53 +331,56 @@ __global__ __launch_bounds__(THREADS) void attn_kvq_kernel(RowsParams p, AttnArg
         sum[rt] *= f;
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[rt][j] *= f;
+        weights(rt);
       }
-      const float from = ref[rt] == -INFINITY ? 0.0f : ref[rt];
+    }
+    uint4 pf[RT][PT];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        z[e] = __builtin_amdgcn_exp2f(z[e] - from);
-        sum[rt] += z[e];
-      }
+    for (int rt = 0; rt < RT; ++rt) {
+      sum[rt] += all[rt];
 #pragma unroll
       for (int t = 0; t < PT; ++t) {
         uint32_t w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          w[e] = pack2_bf16(z[2 * e], z[2 * e + 1]);
-          if (t + 1 < PT) less(z[2 * e], z[2 * e + 1], w[e]);
+          w[e] = pack2_bf16(z[rt][2 * e], z[rt][2 * e + 1]);
+          if (t + 1 < PT) less(z[rt][2 * e], z[rt][2 * e + 1], w[e]);
         }
         pf[rt][t] = make_uint4(w[0], w[1], w[2], w[3]);
       }
     }
 
-    // V: pairs of tokens (i, 2 y), (i, 2 y + 1) -> word 2 i + y of the operands
-    uint32_t vf[NJ][4];
+    // V: dims 2 x and 2 x + 1 of this lane's; tokens (i, 2 y), (i, 2 y + 1) make word 2 i + y of an operand
+    float vsf[2][4];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        const float sa = kvq_scale((raw.vs[i] >> (16 * y)) & 255), sb = kvq_scale((raw.vs[i] >> (16 * y + 8)) & 255);
-        const uint32_t ca = raw.v[i][2 * y], cb = raw.v[i][2 * y + 1];
-        uint32_t xa[4], xb[4];
-        xa[0] = cvt2<0>(ca, sa); xb[0] = cvt2<0>(cb, sb);
-        xa[1] = cvt2<1>(ca, sa); xb[1] = cvt2<1>(cb, sb);
-        if constexpr (D == 128) {
-          xa[2] = cvt2<2>(ca, sa); xb[2] = cvt2<2>(cb, sb);
-          xa[3] = cvt2<3>(ca, sa); xb[3] = cvt2<3>(cb, sb);
+      for (int j = 0; j < 4; ++j) vsf[i][j] = kvq_scale((raw.vs[i] >> (8 * j)) & 255);
+    auto dims = [&](auto sel) __attribute__((always_inline)) {
+      constexpr int X = decltype(sel)::value;
+      uint32_t lo[4], hi[4];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const uint32_t va = cvt2<X>(raw.v[i][2 * y], vsf[i][2 * y]), vb = cvt2<X>(raw.v[i][2 * y + 1], vsf[i][2 * y + 1]);
+          lo[2 * i + y] = low_halves(va, vb);
+          hi[2 * i + y] = high_halves(va, vb);
         }
 #pragma unroll
-        for (int j = 0; j < NJ / 2; ++j) {
-          vf[2 * j][2 * i + y] = low_halves(xa[j], xb[j]);
-          vf[2 * j + 1][2 * i + y] = high_halves(xa[j], xb[j]);
-        }
+      for (int k = 0; k < 2; ++k) {
+        const uint4 va = k ? make_uint4(hi[0], hi[1], hi[2], hi[3]) : make_uint4(lo[0], lo[1], lo[2], lo[3]);
+#pragma unroll
+        for (int t = PT - 1; t >= 0; --t)
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) acc[rt][2 * X + k] = mfma16(va, pf[rt][t], acc[rt][2 * X + k]);
       }
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const uint4 va = make_uint4(vf[j][0], vf[j][1], vf[j][2], vf[j][3]);
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int t = PT - 1; t >= 0; --t) acc[rt][j] = mfma16(va, pf[rt][t], acc[rt][j]);
+    };
+    dims(std::integral_constant<int, 0>{});
+    dims(std::integral_constant<int, 1>{});
+    if constexpr (D == 128) {
+      dims(std::integral_constant<int, 2>{});
+      dims(std::integral_constant<int, 3>{});
     }
 
     if (__any(nan_seen)) {
@@ -333,9 +398,17 @@ __global__ __launch_bounds__(THREADS) void attn_kvq_kernel(RowsParams p, AttnArg
             }
         }
     }
-    raw = next;
-    tile[0] = next_tile[0];
-    tile[1] = next_tile[1];
+  };
+
+  Raw<D> raw[2];
+  Tile tile[2][2];
+  if (u < u_end) fetch(u, raw[0], tile[0]);
+  while (u < u_end) {
+    if (u + 1 < u_end) fetch(u + 1, raw[1], tile[1]);
+    unit(raw[0], tile[0]);
+    raw[0] = raw[1];
+    tile[0][0] = tile[1][0];
+    tile[0][1] = tile[1][1];
     ++u;
   }
 
@@ -348,7 +421,7 @@ __global__ __launch_bounds__(THREADS) void attn_kvq_kernel(RowsParams p, AttnArg
   auto put = [&](int r, int d, const float* y, float ref_r, float sum_r, bool first) __attribute__((always_inline)) {   // four dims of row r of the block
     const int row = r0 + r;
     if (row >= n_rows) return;
-    if (a.splits > 1) {
+    if (part.count > 1) {
       const int64_t at = (int64_t)blockIdx.x * ROWS + r;
       *reinterpret_cast<float4*>(a.part + at * D + d) = make_float4(y[0], y[1], y[2], y[3]);
       if (first) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(ref_r, sum_r);
@@ -375,8 +448,8 @@ __global__ __launch_bounds__(THREADS) void attn_kvq_kernel(RowsParams p, AttnArg
     return;
   }
 
-  // the four waves' sums, one row tile at a time: [wave][16][D + PAD] floats, [wave][16][2] references and sums
-  float* ml = merge + WAVES * 16 * (D + PAD);
+  // the waves' sums, one row tile at a time: [wave][16][D + PAD] floats, [wave][16][2] references and sums
+  float* ml = merge + W * 16 * (D + PAD);
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     if (rt) __syncthreads();
@@ -384,7 +457,7 @@ __global__ __launch_bounds__(THREADS) void attn_kvq_kernel(RowsParams p, AttnArg
     __syncthreads();
     float to = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) to = fmaxf(to, ml[(w * 16 + m) * 2]);
+    for (int w = 0; w < W; ++w) to = fmaxf(to, ml[(w * 16 + m) * 2]);
     const float f = ref[rt] == to ? 1.0f : __builtin_amdgcn_exp2f(ref[rt] - to);
     float* mine = merge + (wave * 16 + m) * (D + PAD) + (D / 4) * kg;
 #pragma unroll
@@ -393,13 +466,14 @@ __global__ __launch_bounds__(THREADS) void attn_kvq_kernel(RowsParams p, AttnArg
       for (int j = 0; j < NJ; j += 4)
         *reinterpret_cast<float4*>(mine + NJ * i + j) = make_float4(acc[rt][j][i] * f, acc[rt][j + 1][i] * f, acc[rt][j + 2][i] * f, acc[rt][j + 3][i] * f);
     __syncthreads();
-    for (int e = threadIdx.x; e < 16 * (D / 4); e += THREADS) {
+    for (int e = threadIdx.x; e < 16 * (D / 4); e += 64 * W) {
       const int r = e / (D / 4), d = (e - r * (D / 4)) * 4;
+      if (r0 + 16 * rt + r >= n_rows) break;
       float y[4] = {0.f, 0.f, 0.f, 0.f}, ref_r = -INFINITY, sum_r = 0.0f;
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) ref_r = fmaxf(ref_r, ml[(w * 16 + r) * 2]);
+      for (int w = 0; w < W; ++w) ref_r = fmaxf(ref_r, ml[(w * 16 + r) * 2]);
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) {
+      for (int w = 0; w < W; ++w) {
         const float4 v = *reinterpret_cast<const float4*>(merge + (w * 16 + r) * (D + PAD) + d);
         const float rw = ml[(w * 16 + r) * 2], sw = ml[(w * 16 + r) * 2 + 1];
         sum_r += sw * (rw == ref_r ? 1.0f : __builtin_amdgcn_exp2f(rw - ref_r));
@@ -413,24 +487,24 @@ __global__ __launch_bounds__(THREADS) void attn_kvq_kernel(RowsParams p, AttnArg
 // The parts of a row, in order: a workgroup per row of a row block, its threads in groups of D / 4 that take every
 // (256 / (D / 4))-th part each.
 template <typename T, int D>
-__global__ __launch_bounds__(THREADS) void kvq_combine_kernel(RowsParams p, AttnArgs a, int rows) {
-  constexpr int LANES = D / 4, GROUPS = THREADS / LANES;
+__global__ __launch_bounds__(COMBINE_THREADS) void kvq_combine_kernel(RowsParams p, AttnArgs a, int rows) {
+  constexpr int LANES = D / 4, GROUPS = COMBINE_THREADS / LANES;
   __shared__ __align__(16) float lds[GROUPS][D + PAD];
   __shared__ float lds_ml[GROUPS][2];
   int x = blockIdx.x;
   const int r = x % rows;
   x /= rows;
-  const int tile = x;
-  const int block = x % a.row_blocks;
-  x /= a.row_blocks;
-  const int g = x % p.Hkv, b = x / p.Hkv;
+  const int block = x % a.row_blocks, e = x / a.row_blocks;
+  const int b = e / p.Hkv, g = e - b * p.Hkv;
   const Seq s = seq_of(p, b);
   const int row = block * rows + r;
   if (row >= s.n * p.G) return;
+  const int2 parts = a.parts[e];
+  if (parts.y <= 1) return;
   const int grp = threadIdx.x / LANES, d = (threadIdx.x - grp * LANES) * 4;
   float ref = -INFINITY, sum = 0.0f, y[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int k = grp; k < a.splits; k += GROUPS) {
-    const int64_t at = ((int64_t)tile * a.splits + k) * rows + r;
+  for (int k = grp; k < parts.y; k += GROUPS) {
+    const int64_t at = ((int64_t)(parts.x + k) * a.row_blocks + block) * rows + r;
     const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
     const float4 v = *reinterpret_cast<const float4*>(a.part + at * D + d);
     const float to = fmaxf(ref, ml.x);
@@ -461,47 +535,65 @@ __global__ __launch_bounds__(THREADS) void kvq_combine_kernel(RowsParams p, Attn
   if (d == 0) p.lse[(int64_t)h * p.n_rows + s.row + i] = total == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * LN2;
 }
 
-// How a call is cut: row tiles per wave, whether waves share rows, row blocks and splits.
+// How a call is cut.
 struct Plan {
-  int rt, share, row_blocks, splits;   // (splits > 1 only with share)
+  int rt, waves, share, row_blocks, split, target, min_units;
+  int64_t parts;   // at most
 };
 Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   Plan c{};
   const int64_t rows = (int64_t)p.max_rows * p.G, heads = (int64_t)p.n_seqs * p.Hkv;
   const int most = is_bf16 ? 4 : 2;
   c.rt = rows <= 16 ? 1 : rows <= 32 || most == 2 ? 2 : 4;
-  const int64_t own = (rows + 16 * c.rt * WAVES - 1) / (16 * c.rt * WAVES);
+  c.waves = 4;
+  const int64_t own = (rows + 16 * c.rt * 4 - 1) / (16 * c.rt * 4);
   c.share = own * heads < 256;
   c.row_blocks = (int)(c.share ? (rows + 16 * c.rt - 1) / (16 * c.rt) : own);
-  c.splits = 1;
+  c.min_units = 32;
+  c.target = 1;
+  c.parts = heads;
   if (c.share) {
     int64_t tokens = p.max_len;
     if (sel_stride >= 0 && (int64_t)sel_stride * p.P < tokens) tokens = (int64_t)sel_stride * p.P;
-    const int64_t wgs = heads * c.row_blocks, most_splits = tokens / (32 * WAVES * 4);
-    int64_t want = 512 / (wgs ? wgs : 1);
-    if (want > most_splits) want = most_splits;
-    c.splits = (int)(want < 1 ? 1 : want);
+    const int64_t units = (tokens + 31) / 32, each = (units + c.min_units - 1) / c.min_units;
+    const int64_t target = WGS / c.row_blocks;
+    c.target = (int)(target < 1 ? 1 : target);
+    c.split = each > 1 && target > 1;
+    if (c.split) c.parts = heads * each < c.target + heads ? heads * each : c.target + heads;
+    else c.waves = c.rt < 4 ? 8 : 4;
   }
   return c;
 }
 
-template <typename T, int D, int RT, int PT> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
-  AttnArgs a{c.splits, c.row_blocks, c.share, nullptr, nullptr};
-  const int64_t blocks = (int64_t)p.n_seqs * p.Hkv * c.row_blocks;
-  if (c.splits > 1) {
+template <typename T, int D, int RT, int PT, int W> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
+  AttnArgs a{c.row_blocks, c.share, c.split, c.target, c.min_units, nullptr, nullptr, nullptr};
+  const int64_t heads = (int64_t)p.n_seqs * p.Hkv, blocks = c.parts * c.row_blocks;
+  if (c.split) {
     a.part = (float*)ws;
-    a.part_ml = a.part + blocks * c.splits * 16 * RT * D;
+    a.part_ml = a.part + blocks * 16 * RT * D;
+    a.parts = (int2*)(a.part_ml + blocks * 16 * RT * 2);
   }
   {
     ProfScope prof_("attn_kvq", st);
-    const size_t lds = c.share ? (size_t)(WAVES * 16 * (D + PAD) + WAVES * 16 * 2) * sizeof(float) : 0;
-    attn_kvq_kernel<T, D, RT, PT><<<dim3((unsigned)(blocks * c.splits)), dim3(THREADS), lds, st>>>(p, a);
+    const size_t lds = c.share ? (size_t)(W * 16 * (D + PAD) + W * 16 * 2) * sizeof(float) : 0;
+    if (lds > 65536) {
+      static DeviceOnce once;
+      const hipError_t e = ensure_max_dynamic_lds(once, (const void*)attn_kvq_kernel<T, D, RT, PT, W>, (int)lds);
+      if (e != hipSuccess) return e;
+    }
+    attn_kvq_kernel<T, D, RT, PT, W><<<dim3((unsigned)blocks), dim3(64 * W), lds, st>>>(p, a);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || c.splits == 1) return e;
+    if (e != hipSuccess || !c.split) return e;
   }
   ProfScope prof_("kvq_combine", st);
-  kvq_combine_kernel<T, D><<<dim3((unsigned)(blocks * 16 * RT)), dim3(THREADS), 0, st>>>(p, a, 16 * RT);
+  kvq_combine_kernel<T, D><<<dim3((unsigned)(heads * c.row_blocks * 16 * RT)), dim3(COMBINE_THREADS), 0, st>>>(p, a, 16 * RT);
   return hipGetLastError();
+}
+template <typename T, int D, int RT, int PT> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
+  if constexpr (RT < 4) {
+    if (c.waves == 8) return run<T, D, RT, PT, 8>(p, c, ws, st);
+  }
+  return run<T, D, RT, PT, 4>(p, c, ws, st);
 }
 template <typename T, int D> hipError_t attn(const RowsParams& p, void* ws, hipStream_t st) {
   constexpr bool BF = sizeof(T) == 2;
@@ -519,13 +611,13 @@ template <typename T, int D> hipError_t attn(const RowsParams& p, void* ws, hipS
 
 size_t kvq_attn_workspace_bytes(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   const Plan c = plan_of(p, is_bf16, sel_stride);
-  if (c.splits == 1) return 0;
-  return (size_t)p.n_seqs * p.Hkv * c.row_blocks * c.splits * 16 * c.rt * (p.D + 2) * sizeof(float);
+  if (!c.split) return 0;
+  return (size_t)c.parts * c.row_blocks * 16 * c.rt * (p.D + 2) * sizeof(float) + (size_t)p.n_seqs * p.Hkv * sizeof(int2);
 }
 int64_t kvq_attn_blocks(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   const Plan c = plan_of(p, is_bf16, sel_stride);
-  const int64_t blocks = (int64_t)p.n_seqs * p.Hkv * c.row_blocks;
-  return blocks * (c.splits > 16 * c.rt ? c.splits : 16 * c.rt);
+  const int64_t combine = (int64_t)p.n_seqs * p.Hkv * c.row_blocks * 16 * c.rt;
+  return c.parts * c.row_blocks * 2 > combine ? c.parts * c.row_blocks * 2 : combine;   // (up to 512 threads)
 }
 
 hipError_t launch_attn_kvq(const RowsParams& p, bool is_bf16, void* ws, hipStream_t st) {
