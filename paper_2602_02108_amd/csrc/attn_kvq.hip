@@ -59,7 +59,6 @@ __device__ __forceinline__ void less(float& a, float& b, uint32_t w) {
 
 struct AttnArgs {
   int row_blocks;              // per (sequence, KV head)
-  int share;                   // the waves of a workgroup share a row block and split its tokens
   int split;                   // parts over workgroups (else one part per (sequence, KV head))
   int target, min_units;       // parts to aim at; units of a part at least
   int2* parts;                 // [sequence * Hkv + KV head]: first part, number of parts
@@ -75,23 +74,37 @@ template <int D> struct Raw {
   uint32_t vs[2];
 };
 
-template <int D> __device__ __forceinline__ void load_tile(const unsigned char* kt, const unsigned char* vt, int P, int off, int m, int kg, Raw<D>& r, int i) {
-  const int t = off + m;
-  const unsigned char* kc = kt + t * (D / 2) + kg * (D / 8);
+// Where a lane's share of a tile lies: offsets from the tile's codes (its row of the page) and from its scales.
+struct Lane { uint32_t k, ks, v, vs; };
+template <int D> __device__ __forceinline__ Lane lane_at(int P, int m, int kg) {
+  const int kb = D == 128 ? kg : kg >> 1, vb = D == 128 ? m >> 2 : m >> 3;
+  return {(uint32_t)(m * (D / 2) + kg * (D / 8)), (uint32_t)(kb * P + m), (uint32_t)(4 * kg * (D / 2) + m * (D / 32)), (uint32_t)(vb * P + 4 * kg)};
+}
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+// A page of one head: buffer loads take its base, a lane's offset and the tile's from three registers, so that addresses cost next to no
+// instruction; what lies past the page reads as zero.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t page_buffer(const unsigned char* base, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base), 0, bytes, 0x00027000);
+}
+// tile i of a unit: `codes` and `scales` are the offsets of the unit's first token in the page, `further` tokens lie before the tile
+template <int D, bool STREAM> __device__ __forceinline__ void load_tile(__amdgpu_buffer_rsrc_t kp, __amdgpu_buffer_rsrc_t vp, int codes, int scales, int further, const Lane& l, Raw<D>& r, int i) {
+  constexpr int AUX = STREAM ? 2 : 0;   // (non-temporal)
+  const int c = further * (D / 2);
   if constexpr (D == 128) {
-    const uint4 x = *reinterpret_cast<const uint4*>(kc);
+    const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(kp, l.k + c, codes, AUX);
     r.k[i][0] = x.x; r.k[i][1] = x.y; r.k[i][2] = x.z; r.k[i][3] = x.w;
   } else {
-    const uint2 x = *reinterpret_cast<const uint2*>(kc);
+    const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(kp, l.k + c, codes, AUX);
     r.k[i][0] = x.x; r.k[i][1] = x.y;
   }
-  const int kb = D == 128 ? kg : kg >> 1, vb = D == 128 ? m >> 2 : m >> 3;
-  r.ks[i] = kt[P * (D / 2) + kb * P + t];
-  const unsigned char* vc = vt + (off + 4 * kg) * (D / 2) + m * (D / 32);
+  r.ks[i] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(kp, l.ks + further, scales, 0);
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    r.v[i][j] = D == 128 ? *reinterpret_cast<const uint32_t*>(vc + j * (D / 2)) : *reinterpret_cast<const uint16_t*>(vc + j * (D / 2));
-  r.vs[i] = *reinterpret_cast<const uint32_t*>(vt + P * (D / 2) + vb * P + off + 4 * kg);
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (D == 128) r.v[i][j] = __builtin_amdgcn_raw_buffer_load_b32(vp, l.v + c + j * (D / 2), codes, AUX);
+    else r.v[i][j] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(vp, l.v + c + j * (D / 2), codes, AUX);
+  }
+  r.vs[i] = __builtin_amdgcn_raw_buffer_load_b32(vp, l.vs + further, scales, 0);
 }
 
 // This lane's D / 4 dims of a query row, as operands of the steps and terms.
@@ -115,6 +128,27 @@ template <typename T, int D, int QT> __device__ __forceinline__ void query_terms
         q[t][c] = make_uint4(w[0], w[1], w[2], w[3]);
       }
     }
+  }
+}
+
+// Queries that are needed in every step are waited for here, once.
+template <int RT, int QT, int NC> __device__ __forceinline__ void landed(uint4 (&q)[RT][QT][NC]) {
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(q[rt][t][c].x), "+v"(q[rt][t][c].y), "+v"(q[rt][t][c].z), "+v"(q[rt][t][c].w));
+}
+
+// Byte X of a tile's four tokens' codes converted: words of tokens (0, 1) and (2, 3) for its even and its odd dim.
+template <int X, int D> __device__ __forceinline__ void pairs(const Raw<D>& raw, int i, uint32_t* lo, uint32_t* hi) {
+#pragma unroll
+  for (int y = 0; y < 2; ++y) {   // (of a scale the conversion takes the exponent's bits alone)
+    const float sa = __uint_as_float(raw.vs[i] << (y ? 7 : 23)), sb = __uint_as_float(y ? raw.vs[i] >> 1 : raw.vs[i] << 15);
+    const uint32_t va = cvt2<X>(raw.v[i][2 * y], sa), vb = cvt2<X>(raw.v[i][2 * y + 1], sb);
+    lo[y] = low_halves(va, vb);
+    hi[y] = high_halves(va, vb);
   }
 }
 
@@ -163,8 +197,9 @@ __device__ __forceinline__ Part part_at(const RowsParams& p, const AttnArgs& a, 
   return {-1, 0, 0, 0};
 }
 
-template <typename T, int D, int RT, int PT, int W>
-__global__ __launch_bounds__(64 * W, RT == 4 ? 1 : 2) void attn_kvq_kernel(RowsParams p, AttnArgs a) {
+// WIDE: pages of 32 tokens and more, a unit lies in one.  STREAM: codes past the caches.
+template <typename T, int D, int RT, int PT, int W, bool WIDE, bool STREAM>
+__global__ __launch_bounds__(64 * W, RT == 1 && W == 4 && sizeof(T) == 2 ? 3 : 2) void attn_kvq_kernel(RowsParams p, AttnArgs a) {
   extern __shared__ __align__(16) float merge[];
   constexpr int QT = sizeof(T) == 2 ? 1 : 3, NC = D / 32, NJ = D / 16, ROWS = 16 * RT;
   const int lane = threadIdx.x & 63, m = lane & 15, kg = lane >> 4;
@@ -176,8 +211,8 @@ __global__ __launch_bounds__(64 * W, RT == 4 ? 1 : 2) void attn_kvq_kernel(RowsP
   const Seq s = seq_of(p, b);
   if (a.split && part.index == 0 && block == 0 && threadIdx.x == 0) a.parts[part.e] = make_int2(part.first, part.count);
   const int n_rows = s.n * p.G;
-  const int r0 = a.share ? block * ROWS : (block * W + wave) * ROWS;
-  if (r0 >= n_rows) return;      // (a workgroup that shares its rows leaves as a whole; the others have no barrier)
+  const int r0 = block * ROWS;
+  if (r0 >= n_rows) return;
   const int r_last = min(r0 + ROWS, n_rows) - 1;
   const int min_pos = s.pos + r0 / p.G, max_pos = s.pos + r_last / p.G;
 
@@ -215,7 +250,7 @@ __global__ __launch_bounds__(64 * W, RT == 4 ? 1 : 2) void attn_kvq_kernel(RowsP
     }
   }
   const int n_units = (n_tiles + 1) >> 1;
-  const int parts = a.share ? part.count * W : 1, mine = a.share ? part.index * W + wave : 0;
+  const int parts = part.count * W, mine = part.index * W + wave;
   int u = (int)((int64_t)n_units * mine / parts);
   const int u_end = (int)((int64_t)n_units * (mine + 1) / parts);
 
@@ -230,36 +265,62 @@ __global__ __launch_bounds__(64 * W, RT == 4 ? 1 : 2) void attn_kvq_kernel(RowsP
   }
   const float scale = p.sm_scale * LOG2E;
 
-  // pages of 64 consecutive entries, one per lane; tile -> (page pointers, position of its first token)
-  int win = -128, w_log = 0, w_phys = -1;
+  // pages of 64 consecutive entries, one per lane: logical page (-1: there is nothing) and where it lies in the pools
+  int win = 0, w_log = -1;
+  uint32_t w_lo = 0, w_hi = 0;
   auto window = [&](int e0) __attribute__((always_inline)) {
     win = e0;
     const int e = e0 + lane;
     w_log = e < n_entries ? (list ? list[e] : e) : -1;
-    w_phys = w_log >= 0 && w_log < n_pages ? page_of(p, b, w_log) : -1;
+    const int phys = w_log >= 0 && w_log < n_pages ? page_of(p, b, w_log) : -1;
+    if (phys < 0) w_log = -1;
+    const uint64_t at = (uint64_t)max(phys, 0) * (uint64_t)p.pool_page_stride;
+    w_lo = (uint32_t)at;
+    w_hi = (uint32_t)(at >> 32);
   };
   const unsigned char* kbase = (const unsigned char*)p.k_pool + (int64_t)g * p.pool_head_stride;
   const unsigned char* vbase = (const unsigned char*)p.v_pool + (int64_t)g * p.pool_head_stride;
-  struct Tile { const unsigned char *k, *v; int off, t0; };
-  auto tile_at = [&](int t) __attribute__((always_inline)) {
-    const int e = t >> log_tpp, off = (t & ((1 << log_tpp) - 1)) << 4;
-    if (t >= n_tiles) return Tile{kbase, vbase, 0, NO_TOKEN};
-    const int phys = __builtin_amdgcn_readlane(w_phys, e - win), page = __builtin_amdgcn_readlane(w_log, e - win);
-    if (phys < 0) return Tile{kbase, vbase, 0, NO_TOKEN};
-    return Tile{kbase + (int64_t)phys * p.pool_page_stride, vbase + (int64_t)phys * p.pool_page_stride, off, (page << p.log2_p) + off};
-  };
-  auto fetch = [&](int unit, Raw<D>& r, Tile (&tl)[2]) __attribute__((always_inline)) {
-    const int e0 = (2 * unit) >> log_tpp, e1 = (2 * unit + 1) >> log_tpp;
-    if (e1 - win >= 64 || win < 0) window(e0);
+  const Lane at_lane = lane_at<D>(p.P, m, kg);
+  const int tile_bytes = p.P * (D / 2 + D / 32), first_scale = p.P * (D / 2);
+  auto fetch = [&](int unit, Raw<D>& r, int (&t0)[2]) __attribute__((always_inline)) {   // t0: positions of the tiles' first tokens
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      tl[i] = tile_at(2 * unit + i);
-      load_tile<D>(tl[i].k, tl[i].v, p.P, tl[i].off, m, kg, r, i);
+    for (int i = 0; i < (WIDE ? 1 : 2); ++i) {
+      const int t = 2 * unit + i, e = t >> log_tpp, off = (t & ((1 << log_tpp) - 1)) << 4;
+      if (e - win >= 64) window(e);
+      const int at = e - win, page = __builtin_amdgcn_readlane(w_log, at);
+      const uint64_t where = (uint32_t)__builtin_amdgcn_readlane(w_lo, at) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(w_hi, at) << 32;
+      const __amdgpu_buffer_rsrc_t kp = page_buffer(kbase + where, tile_bytes), vp = page_buffer(vbase + where, tile_bytes);
+      const int codes = off * (D / 2), scales = first_scale + off;
+      t0[i] = page < 0 ? NO_TOKEN : (page << p.log2_p) + off;
+      load_tile<D, STREAM>(kp, vp, codes, scales, 0, at_lane, r, i);
+      if constexpr (WIDE) {
+        t0[1] = t0[0] + 16;
+        load_tile<D, STREAM>(kp, vp, codes, scales, 16, at_lane, r, 1);
+      }
     }
   };
 
-  auto unit = [&](Raw<D>& raw, const Tile (&tile)[2]) __attribute__((always_inline)) {
-    const bool masked = max(tile[0].t0, tile[1].t0) + 15 > min_pos;
+  auto unit = [&](int number, Raw<D>& raw, const int (&t0)[2]) __attribute__((always_inline)) {
+    const bool masked = (WIDE ? t0[1] : max(t0[0], t0[1])) + 15 > min_pos;
+    // Tokens that not every row sees.  Their V is zero where nothing of it is seen (it may be anything) and where it is NaN: a
+    // weight of zero does not stop a NaN, so the rows that do see it get theirs below.
+    bool nan_seen = false;
+    if (masked) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int t = t0[i] + 4 * kg + j;
+          const bool partly = t > min_pos, unseen = t > max_pos, bad = ((raw.vs[i] >> (8 * j)) & 255) == 255;
+          if (partly && (unseen || bad)) {
+            raw.v[i][j] = 0;
+            raw.vs[i] = (raw.vs[i] & ~(255u << (8 * j))) | (127u << (8 * j));
+          }
+          nan_seen |= partly && !unseen && bad;
+        }
+      }
+    }
+
     // S^T
     f32x4 st[RT][2];
 #pragma unroll
@@ -279,32 +340,13 @@ __global__ __launch_bounds__(64 * W, RT == 4 ? 1 : 2) void attn_kvq_kernel(RowsP
           for (int rt = 0; rt < RT; ++rt) st[rt][i] = mfma16(kf[c], q[rt][t][c], st[rt][i]);
     }
 
-    // Tokens that not every row sees.  Their V is zero where nothing of it is seen (it may be anything) and where it is NaN: a
-    // weight of zero does not stop a NaN, so the rows that do see it get theirs below.
-    bool nan_seen = false;
-    if (masked) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int t = tile[i].t0 + 4 * kg + j;
-          const bool partly = t > min_pos, unseen = t > max_pos, bad = ((raw.vs[i] >> (8 * j)) & 255) == 255;
-          if (partly && (unseen || bad)) {
-            raw.v[i][j] = 0;
-            raw.vs[i] = (raw.vs[i] & ~(255u << (8 * j))) | (127u << (8 * j));
-          }
-          nan_seen |= partly && !unseen && bad;
-        }
-      }
-    }
-
     float z[RT][8], all[RT];
     auto weights = [&](int rt) __attribute__((always_inline)) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) z[rt][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[rt][e >> 2][e & 3], scale, -ref[rt]));
       if (masked) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) z[rt][e] = tile[e >> 2].t0 + 4 * kg + (e & 3) <= pos[rt] ? z[rt][e] : 0.0f;
+        for (int e = 0; e < 8; ++e) z[rt][e] = t0[e >> 2] + 4 * kg + (e & 3) <= pos[rt] ? z[rt][e] : 0.0f;
       }
       all[rt] = ((z[rt][0] + z[rt][1]) + (z[rt][2] + z[rt][3])) + ((z[rt][4] + z[rt][5]) + (z[rt][6] + z[rt][7]));
     };
@@ -320,7 +362,7 @@ __global__ __launch_bounds__(64 * W, RT == 4 ? 1 : 2) void attn_kvq_kernel(RowsP
         float top = -INFINITY;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const bool seen = !masked || tile[e >> 2].t0 + 4 * kg + (e & 3) <= pos[rt];
+          const bool seen = !masked || t0[e >> 2] + 4 * kg + (e & 3) <= pos[rt];
           top = fmaxf(top, seen ? st[rt][e >> 2][e & 3] * scale : -INFINITY);
         }
         top = fmaxf(top, __shfl_xor(top, 16, 64));
@@ -351,30 +393,19 @@ __global__ __launch_bounds__(64 * W, RT == 4 ? 1 : 2) void attn_kvq_kernel(RowsP
     }
 
     // V: dims 2 x and 2 x + 1 of this lane's; tokens (i, 2 y), (i, 2 y + 1) make word 2 i + y of an operand
-    float vsf[2][4];
+    auto add = [&](int j, const uint4& va) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+      for (int t = PT - 1; t >= 0; --t)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) vsf[i][j] = kvq_scale((raw.vs[i] >> (8 * j)) & 255);
+        for (int rt = 0; rt < RT; ++rt) acc[rt][j] = mfma16(va, pf[rt][t], acc[rt][j]);
+    };
     auto dims = [&](auto sel) __attribute__((always_inline)) {
       constexpr int X = decltype(sel)::value;
       uint32_t lo[4], hi[4];
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const uint32_t va = cvt2<X>(raw.v[i][2 * y], vsf[i][2 * y]), vb = cvt2<X>(raw.v[i][2 * y + 1], vsf[i][2 * y + 1]);
-          lo[2 * i + y] = low_halves(va, vb);
-          hi[2 * i + y] = high_halves(va, vb);
-        }
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const uint4 va = k ? make_uint4(hi[0], hi[1], hi[2], hi[3]) : make_uint4(lo[0], lo[1], lo[2], lo[3]);
-#pragma unroll
-        for (int t = PT - 1; t >= 0; --t)
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt) acc[rt][2 * X + k] = mfma16(va, pf[rt][t], acc[rt][2 * X + k]);
-      }
+      for (int i = 0; i < 2; ++i) pairs<X>(raw, i, lo + 2 * i, hi + 2 * i);
+      add(2 * X, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+      add(2 * X + 1, make_uint4(hi[0], hi[1], hi[2], hi[3]));
     };
     dims(std::integral_constant<int, 0>{});
     dims(std::integral_constant<int, 1>{});
@@ -385,11 +416,13 @@ __global__ __launch_bounds__(64 * W, RT == 4 ? 1 : 2) void attn_kvq_kernel(RowsP
 
     if (__any(nan_seen)) {
       const int vb = D == 128 ? kg : kg >> 1;      // this lane's output dims are D/4 kg .. + D/4 - 1
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < 2; ++i) {
+        const int tile = 2 * number + i, e = tile >> log_tpp, off = (tile & ((1 << log_tpp) - 1)) << 4;
+        if (t0[i] >= NO_TOKEN) continue;
+        const unsigned char* vs = vbase + (int64_t)page_of(p, b, list ? list[e] : e) * p.pool_page_stride + p.P * (D / 2) + vb * p.P + off;
         for (int t = 0; t < 16; ++t) {
-          const int at = tile[i].t0 + t;
-          if (at <= min_pos || at > max_pos) continue;
-          if (tile[i].v[p.P * (D / 2) + vb * p.P + tile[i].off + t] != 255) continue;
+          const int at = t0[i] + t;
+          if (at <= min_pos || at > max_pos || vs[t] != 255) continue;
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt)
             if (at <= pos[rt]) {
@@ -397,19 +430,40 @@ __global__ __launch_bounds__(64 * W, RT == 4 ? 1 : 2) void attn_kvq_kernel(RowsP
               for (int j = 0; j < NJ; ++j) acc[rt][j] = f32x4{NAN, NAN, NAN, NAN};
             }
         }
+      }
     }
   };
 
-  Raw<D> raw[2];
-  Tile tile[2][2];
-  if (u < u_end) fetch(u, raw[0], tile[0]);
-  while (u < u_end) {
-    if (u + 1 < u_end) fetch(u + 1, raw[1], tile[1]);
-    unit(raw[0], tile[0]);
-    raw[0] = raw[1];
-    tile[0][0] = tile[1][0];
-    tile[0][1] = tile[1][1];
-    ++u;
+  // units in flight: a wave that waits for its next unit idles its share of the memory's latency (about a microsecond)
+  constexpr int AHEAD = 2;
+  Raw<D> raw[AHEAD];
+  int t0[AHEAD][2];
+  // The wait for a unit lets every later fetch fly on, if the compiler can count them: the steady loop fetches without a condition,
+  // and the queries have landed before it.
+  if (u < u_end) window((2 * u) >> log_tpp);
+  if (u + 2 * AHEAD <= u_end) {
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) fetch(u + k, raw[k], t0[k]);
+    landed(q);
+    for (; u + 2 * AHEAD <= u_end; u += AHEAD) {
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        unit(u + k, raw[k], t0[k]);
+        fetch(u + k + AHEAD, raw[k], t0[k]);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+      if (u + k < u_end) fetch(u + k, raw[k], t0[k]);
+  }
+  for (; u < u_end; u += AHEAD) {
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      if (u + k >= u_end) break;
+      unit(u + k, raw[k], t0[k]);
+      if (u + k + AHEAD < u_end) fetch(u + k + AHEAD, raw[k], t0[k]);
+    }
   }
 
   // lane (m, kg): query m, dims D/4 kg + D/16 i + j of acc[.][j][i]
@@ -434,19 +488,6 @@ __global__ __launch_bounds__(64 * W, RT == 4 ? 1 : 2) void attn_kvq_kernel(RowsP
     else *reinterpret_cast<float4*>(dst) = make_float4(y[0] * f, y[1] * f, y[2] * f, y[3] * f);
     if (first) p.lse[(int64_t)h * p.n_rows + s.row + i] = sum_r == 0.0f ? -INFINITY : (ref_r + __builtin_amdgcn_logf(sum_r)) * LN2;
   };
-
-  if (!a.share) {
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < NJ; j += 4) {
-          const float y[4] = {acc[rt][j][i], acc[rt][j + 1][i], acc[rt][j + 2][i], acc[rt][j + 3][i]};
-          put(16 * rt + m, (D / 4) * kg + NJ * i + j, y, ref[rt], sum[rt], i == 0 && j == 0 && kg == 0);
-        }
-    return;
-  }
 
   // the waves' sums, one row tile at a time: [wave][16][D + PAD] floats, [wave][16][2] references and sums
   float* ml = merge + W * 16 * (D + PAD);
@@ -537,36 +578,37 @@ __global__ __launch_bounds__(COMBINE_THREADS) void kvq_combine_kernel(RowsParams
 
 // How a call is cut.
 struct Plan {
-  int rt, waves, share, row_blocks, split, target, min_units;
+  int rt, waves, many, stream, row_blocks, split, target, min_units;
   int64_t parts;   // at most
 };
 Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   Plan c{};
   const int64_t rows = (int64_t)p.max_rows * p.G, heads = (int64_t)p.n_seqs * p.Hkv;
-  const int most = is_bf16 ? 4 : 2;
-  c.rt = rows <= 16 ? 1 : rows <= 32 || most == 2 ? 2 : 4;
-  c.waves = 4;
-  const int64_t own = (rows + 16 * c.rt * 4 - 1) / (16 * c.rt * 4);
-  c.share = own * heads < 256;
-  c.row_blocks = (int)(c.share ? (rows + 16 * c.rt - 1) / (16 * c.rt) : own);
-  c.min_units = 32;
-  c.target = 1;
-  c.parts = heads;
-  if (c.share) {
-    int64_t tokens = p.max_len;
-    if (sel_stride >= 0 && (int64_t)sel_stride * p.P < tokens) tokens = (int64_t)sel_stride * p.P;
-    const int64_t units = (tokens + 31) / 32, each = (units + c.min_units - 1) / c.min_units;
-    const int64_t target = WGS / c.row_blocks;
-    c.target = (int)(target < 1 ? 1 : target);
-    c.split = each > 1 && target > 1;
-    if (c.split) c.parts = heads * each < c.target + heads ? heads * each : c.target + heads;
-    else c.waves = c.rt < 4 ? 8 : 4;
-  }
+  c.rt = rows <= 16 || (!is_bf16 && p.D == 128) ? 1 : 2;   // (fp32 terms of two row tiles at head dim 128 do not fit the registers)
+  c.many = is_bf16 && rows > 64;
+  c.row_blocks = (int)((rows + 16 * c.rt - 1) / (16 * c.rt));
+  int64_t tokens = p.max_len;
+  if (sel_stride >= 0 && (int64_t)sel_stride * p.P < tokens) tokens = (int64_t)sel_stride * p.P;
+  const int64_t units = (tokens + 31) / 32;
+  // A part's sums are written and read again, which takes as long as a few units: eight of a row tile at head dim 128.
+  const int least = c.rt * p.D / 16 < 8 ? 8 : c.rt * p.D / 16;
+  c.min_units = least * (c.row_blocks < 4 ? c.row_blocks : 4);
+  const int64_t each = (units + c.min_units - 1) / c.min_units;
+  // Up to 40 units eight waves without a second launch are faster (1000 tokens: 9.4 us, 10.5 in parts; 2000: 13.4, 10.7).  A lone row block
+  // is cut in any case: the lengths of many sequences may differ (32 of 1 to 32K tokens: 25 us, 127 whole).  Several are cut
+  // where they leave workgroups idle (1024 rows x 7 over 8K tokens, 896 workgroups: 148 us, 170 in parts).
+  const int64_t target = c.row_blocks == 1 ? (WGS > 2 * heads ? WGS : 2 * heads) : WGS / c.row_blocks;
+  c.split = units > 40 && each > 1 && target >= 2 * heads;
+  c.target = (int)(target < 1 ? 1 : target);
+  c.parts = !c.split ? heads : heads * each < target + heads ? heads * each : target + heads;
+  c.waves = c.split || c.many ? 4 : 8;
+  // Codes past the caches once they would not stay in the last one (256 MiB) to the next call: 570 MB 117 -> 105 us, 62 MB 25.4 -> 26.2.
+  c.stream = heads * tokens * 2 * (p.D / 2 + p.D / 32) > (256ll << 20);
   return c;
 }
 
-template <typename T, int D, int RT, int PT, int W> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
-  AttnArgs a{c.row_blocks, c.share, c.split, c.target, c.min_units, nullptr, nullptr, nullptr};
+template <typename T, int D, int RT, int PT, int W, bool WIDE, bool STREAM> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
+  AttnArgs a{c.row_blocks, c.split, c.target, c.min_units, nullptr, nullptr, nullptr};
   const int64_t heads = (int64_t)p.n_seqs * p.Hkv, blocks = c.parts * c.row_blocks;
   if (c.split) {
     a.part = (float*)ws;
@@ -575,13 +617,14 @@ template <typename T, int D, int RT, int PT, int W> hipError_t run(const RowsPar
   }
   {
     ProfScope prof_("attn_kvq", st);
-    const size_t lds = c.share ? (size_t)(W * 16 * (D + PAD) + W * 16 * 2) * sizeof(float) : 0;
+    constexpr size_t lds = (size_t)(W * 16 * (D + PAD) + W * 16 * 2) * sizeof(float);
+    const auto kernel = attn_kvq_kernel<T, D, RT, PT, W, WIDE, STREAM>;
     if (lds > 65536) {
       static DeviceOnce once;
-      const hipError_t e = ensure_max_dynamic_lds(once, (const void*)attn_kvq_kernel<T, D, RT, PT, W>, (int)lds);
+      const hipError_t e = ensure_max_dynamic_lds(once, (const void*)kernel, (int)lds);
       if (e != hipSuccess) return e;
     }
-    attn_kvq_kernel<T, D, RT, PT, W><<<dim3((unsigned)blocks), dim3(64 * W), lds, st>>>(p, a);
+    kernel<<<dim3((unsigned)blocks), dim3(64 * W), lds, st>>>(p, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !c.split) return e;
   }
@@ -589,19 +632,23 @@ template <typename T, int D, int RT, int PT, int W> hipError_t run(const RowsPar
   kvq_combine_kernel<T, D><<<dim3((unsigned)(heads * c.row_blocks * 16 * RT)), dim3(COMBINE_THREADS), 0, st>>>(p, a, 16 * RT);
   return hipGetLastError();
 }
-template <typename T, int D, int RT, int PT> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
-  if constexpr (RT < 4) {
-    if (c.waves == 8) return run<T, D, RT, PT, 8>(p, c, ws, st);
+template <typename T, int D, int RT, int PT, int W> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
+  if (p.P < 32) return run<T, D, RT, PT, W, false, false>(p, c, ws, st);
+  if constexpr (RT == 1 && W == 4) {
+    if (c.stream) return run<T, D, RT, PT, W, true, true>(p, c, ws, st);
   }
-  return run<T, D, RT, PT, 4>(p, c, ws, st);
+  return run<T, D, RT, PT, W, true, false>(p, c, ws, st);
+}
+template <typename T, int D, int RT, int PT> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
+  return c.waves == 8 ? run<T, D, RT, PT, 8>(p, c, ws, st) : run<T, D, RT, PT, 4>(p, c, ws, st);
 }
 template <typename T, int D> hipError_t attn(const RowsParams& p, void* ws, hipStream_t st) {
-  constexpr bool BF = sizeof(T) == 2;
-  const Plan c = plan_of(p, BF, p.sel ? p.sel_stride : -1);
-  if constexpr (BF) {
-    if (c.rt == 1) return run<T, D, 1, 2>(p, c, ws, st);
-    if (c.rt == 2) return run<T, D, 2, 2>(p, c, ws, st);
-    return run<T, D, 4, 1>(p, c, ws, st);
+  const Plan c = plan_of(p, sizeof(T) == 2, p.sel ? p.sel_stride : -1);
+  if constexpr (sizeof(T) == 2) {
+    if (c.many) return run<T, D, 2, 1, 4>(p, c, ws, st);
+    return c.rt == 1 ? run<T, D, 1, 2>(p, c, ws, st) : run<T, D, 2, 2>(p, c, ws, st);
+  } else if constexpr (D == 128) {
+    return run<T, D, 1, 3>(p, c, ws, st);
   } else {
     return c.rt == 1 ? run<T, D, 1, 3>(p, c, ws, st) : run<T, D, 2, 3>(p, c, ws, st);
   }
