@@ -592,12 +592,14 @@ Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   const int64_t units = (tokens + 31) / 32;
   // A part's sums are written and read again, which takes as long as a few units: eight of a row tile at head dim 128.
   const int least = c.rt * p.D / 16 < 8 ? 8 : c.rt * p.D / 16;
-  c.min_units = least * (c.row_blocks < 4 ? c.row_blocks : 4);
+  c.min_units = least;
   const int64_t each = (units + c.min_units - 1) / c.min_units;
   // Up to 40 units eight waves without a second launch are faster (1000 tokens: 9.4 us, 10.5 in parts; 2000: 13.4, 10.7).  A lone row block
   // is cut in any case: the lengths of many sequences may differ (32 of 1 to 32K tokens: 25 us, 127 whole).  Several are cut
   // where they leave workgroups idle (1024 rows x 7 over 8K tokens, 896 workgroups: 148 us, 170 in parts).
-  const int64_t target = c.row_blocks == 1 ? (WGS > 2 * heads ? WGS : 2 * heads) : WGS / c.row_blocks;
+  // (the parts may be `heads` more than the target: kept within what the chip holds at once, as far as that leaves half of it)
+  const int64_t room = WGS / c.row_blocks, aim = room - heads > room / 2 ? room - heads : room / 2;
+  const int64_t target = c.row_blocks == 1 && aim < 2 * heads ? 2 * heads : aim;
   c.split = units > 40 && each > 1 && target >= 2 * heads;
   c.target = (int)(target < 1 ? 1 : target);
   c.parts = !c.split ? heads : heads * each < target + heads ? heads * each : target + heads;
