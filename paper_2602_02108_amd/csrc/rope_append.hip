@@ -140,22 +140,20 @@ __device__ __forceinline__ void turn_queries(const RowsParams& p, int x, int blo
   const T* src = (const T*)p.q.data + (int64_t)(s.row + i) * p.q.tok_stride;
   T* dst = (T*)p.q_out.data + (int64_t)(s.row + i) * p.q_out.tok_stride;
   const int h1 = min(h0 + heads, p.Hq);
-  for (int h = h0; h < h1; h += 4) {   // (four rows' loads in flight)
-    float v[4][16];
+  float v[4][16];   // (four rows' loads in flight)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const T* r = src + (int64_t)min(h + k, h1 - 1) * p.q.head_stride;
-      load8(r + a.lo, v[k]);
-      load8(r + a.hi, v[k] + 8);
-    }
+  for (int k = 0; k < 4; ++k) {
+    const T* r = src + (int64_t)min(h0 + k, h1 - 1) * p.q.head_stride;
+    load8(r + a.lo, v[k]);
+    load8(r + a.hi, v[k] + 8);
+  }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if (h + k >= h1) break;
-      if (a.turns) turn<BACK>(p, v[k], c, sn);
-      T* r = dst + (int64_t)(h + k) * p.q_out.head_stride;
-      store8(r + a.lo, v[k]);
-      store8(r + a.hi, v[k] + 8);
-    }
+  for (int k = 0; k < 4; ++k) {
+    if (h0 + k >= h1) break;
+    if (a.turns) turn<BACK>(p, v[k], c, sn);
+    T* r = dst + (int64_t)(h0 + k) * p.q_out.head_stride;
+    store8(r + a.lo, v[k]);
+    store8(r + a.hi, v[k] + 8);
   }
 }
 
@@ -169,9 +167,10 @@ __device__ __forceinline__ void append_page(const RowsParams& p, int x) {
   x /= SL;
   const bool keys = (x & 1) == 0;
   Span s;
-  if (!span_of(p, x >> 1, s) || s.phys < 0) return;
+  if (!span_of(p, x >> 1, s)) return;
   const oomb_rows& rows = keys ? p.k : p.v;
   const T* src = (const T*)rows.data + (int64_t)s.row * rows.tok_stride + (int64_t)s.g * rows.head_stride;
+  // (a page that is not there is found out at the first store: the rows' loads do not wait for its number)
   T* pool = (T*)(keys ? p.k_pool : p.v_pool) + (int64_t)s.phys * p.pool_page_stride + (int64_t)s.g * p.pool_head_stride;
   const int t0 = s.page << p.log2_p, tid = threadIdx.x;
   const int ul = tid & (U - 1);
@@ -194,6 +193,7 @@ __device__ __forceinline__ void append_page(const RowsParams& p, int x) {
       load8(r + a.hi, v[k] + 8);
       if (turns) load_angles(p, tk, a, c[k], sn[k]);
     }
+    if (s.phys < 0) return;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const int tk = t + k * (THREADS / U);
@@ -205,13 +205,17 @@ __device__ __forceinline__ void append_page(const RowsParams& p, int x) {
       if (sums) put(tk, v[k]);
     }
   }
-  if (!sums) return;
-  for (int t = t0 + (tid >> 2); t < s.first; t += THREADS / U) {
-    float v[16];
-    const T* r = pool + (int64_t)(t - t0) * p.pool_tok_stride;
-    load8(r + a.lo, v);
-    load8(r + a.hi, v + 8);
-    put(t, v);
+  if (!sums || s.phys < 0) return;
+  if (t0 + (tid >> 2) < s.first) {   // (a page has 128 tokens at most: two a thread)
+    float v[2][16];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const T* r = pool + (int64_t)(min(t0 + (tid >> 2) + k * (THREADS / U), s.first - 1) - t0) * p.pool_tok_stride;
+      load8(r + a.lo, v[k]);
+      load8(r + a.hi, v[k] + 8);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) put(min(t0 + (tid >> 2) + k * (THREADS / U), s.first - 1), v[k]);
   }
   __syncthreads();
   float* out = p.kbar + (((int64_t)s.b * p.table_stride + s.page) * p.Hkv + s.g) * D;
@@ -245,7 +249,7 @@ __device__ __forceinline__ void append_page_kvq(const RowsParams& p, int x) {
   constexpr int U = D / UNIT, NB = D / 32, TOK = THREADS / U;
   const bool keys = (x & 1) == 0;
   Span s;
-  if (!span_of(p, x >> 1, s) || s.phys < 0) return;
+  if (!span_of(p, x >> 1, s)) return;
   const oomb_rows& rows = keys ? p.k : p.v;
   const T* src = (const T*)rows.data + (int64_t)s.row * rows.tok_stride + (int64_t)s.g * rows.head_stride;
   unsigned char* tile = (unsigned char*)(keys ? p.k_pool : p.v_pool) + (int64_t)s.phys * p.pool_page_stride + (int64_t)s.g * p.pool_head_stride;
@@ -297,7 +301,7 @@ __device__ __forceinline__ void append_page_kvq(const RowsParams& p, int x) {
         if (a.hi / 32 == j) bhi = y;
         if (u == j) mine = y;
       }
-      if (tk >= s.last) continue;
+      if (tk >= s.last || s.phys < 0) continue;
       const uint32_t lo = blo == 255 ? 0 : codes8(v[k], kvq_scale(blo)), hi = bhi == 255 ? 0 : codes8(v[k] + 8, kvq_scale(bhi));
       unsigned char* r = tile + (tk - t0) * (D / 2);
       *reinterpret_cast<uint32_t*>(r + a.lo / 2) = lo;
@@ -306,11 +310,22 @@ __device__ __forceinline__ void append_page_kvq(const RowsParams& p, int x) {
       if (sums) put(tk, lo, hi, kvq_scale(blo), kvq_scale(bhi));
     }
   }
-  if (!sums) return;
-  for (int t = t0 + tid / U; t < s.first; t += TOK) {
-    const unsigned char* r = tile + (t - t0) * (D / 2);
-    put(t, *reinterpret_cast<const uint32_t*>(r + a.lo / 2), *reinterpret_cast<const uint32_t*>(r + a.hi / 2),
-        kvq_scale(scales[(a.lo / 32) * p.P + (t - t0)]), kvq_scale(scales[(a.hi / 32) * p.P + (t - t0)]));
+  if (!sums || s.phys < 0) return;
+  if (t0 + tid / U < s.first) {   // (a page has 128 tokens at most)
+    constexpr int K = 128 / TOK;
+    uint32_t lo[K], hi[K];
+    unsigned char slo[K], shi[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int at = min(t0 + tid / U + k * TOK, s.first - 1) - t0;
+      const unsigned char* r = tile + at * (D / 2);
+      lo[k] = *reinterpret_cast<const uint32_t*>(r + a.lo / 2);
+      hi[k] = *reinterpret_cast<const uint32_t*>(r + a.hi / 2);
+      slo[k] = scales[(a.lo / 32) * p.P + at];
+      shi[k] = scales[(a.hi / 32) * p.P + at];
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) put(min(t0 + tid / U + k * TOK, s.first - 1), lo[k], hi[k], kvq_scale(slo[k]), kvq_scale(shi[k]));
   }
   __syncthreads();
   float* out = p.kbar + (((int64_t)s.b * p.table_stride + s.page) * p.Hkv + s.g) * D;
@@ -372,14 +387,15 @@ __global__ __launch_bounds__(THREADS) void append_rope_bwd_kernel(RowsParams p, 
   else gather_page<T, GT, D>(p, x);
 }
 
-// ---- values of rows in a 4-bit cache: a thread per 32 dims of a row, key heads first -----------------------------------------
+// ---- values of rows in a 4-bit cache: a thread per 8 dims of a row (a word of codes, neighbouring lanes store neighbouring
+// words; 32 dims to a thread took 10.5 us for 8192 rows of 8 heads), key heads first -----------------------------------------
 template <typename T, int D>
 __global__ __launch_bounds__(THREADS) void kvq_read_kernel(RowsParams p, int blocks_per_seq) {
-  constexpr int NB = D / 32;
+  constexpr int NW = D / 8;
   const int b = blockIdx.x / blocks_per_seq;
   const int64_t at = (int64_t)(blockIdx.x - b * blocks_per_seq) * THREADS + threadIdx.x;
-  const int j = (int)(at % NB);
-  const int64_t y = at / NB;
+  const int j = (int)(at % NW);
+  const int64_t y = at / NW;
   const int i = (int)(y / (2 * p.Hkv)), w = (int)(y - (int64_t)i * 2 * p.Hkv), g = w >= p.Hkv ? w - p.Hkv : w;
   const Seq s = seq_of(p, b);
   const int pos = s.pos + i;
@@ -387,32 +403,28 @@ __global__ __launch_bounds__(THREADS) void kvq_read_kernel(RowsParams p, int blo
   const int32_t phys = page_of(p, b, pos >> p.log2_p);
   const int slot = pos & (p.P - 1);
   const oomb_rows& rows = w >= p.Hkv ? p.v : p.k;
-  T* dst = (T*)rows.data + (int64_t)(s.row + i) * rows.tok_stride + (int64_t)g * rows.head_stride + 32 * j;
-  uint4 codes = make_uint4(0, 0, 0, 0);
-  uint32_t byte = 127;
+  T* dst = (T*)rows.data + (int64_t)(s.row + i) * rows.tok_stride + (int64_t)g * rows.head_stride + 8 * j;
+  uint32_t codes = 0, byte = 127;
   if (phys >= 0) {
     const unsigned char* tile = (const unsigned char*)(w >= p.Hkv ? p.v_pool : p.k_pool) + (int64_t)phys * p.pool_page_stride + (int64_t)g * p.pool_head_stride;
-    codes = *reinterpret_cast<const uint4*>(tile + slot * (D / 2) + 16 * j);
-    byte = tile[p.P * (D / 2) + j * p.P + slot];
+    codes = *reinterpret_cast<const uint32_t*>(tile + slot * (D / 2) + 4 * j);
+    byte = tile[p.P * (D / 2) + (j / 4) * p.P + slot];
   }
-  const uint32_t word[4] = {codes.x, codes.y, codes.z, codes.w};
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const uint4 v = values8(word[k], kvq_scale(byte));
-    if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<uint4*>(dst + 8 * k) = v;
-    } else {
-      float f[8];
-      Vec16<bf16_t>::unpack(v, f);
-      store8(dst + 8 * k, f);
-    }
+  const uint4 v = values8(codes, kvq_scale(byte));
+  if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<uint4*>(dst) = v;
+  } else {
+    float f[8];
+    Vec16<bf16_t>::unpack(v, f);
+    store8(dst, f);
   }
 }
 
-// Heads per thread of the queries: as many as leave 128 Ki threads (half of what the chip holds at this kernel's registers), at most 8.
+// Heads per thread of the queries: up to the four whose loads are in flight together, as many as leave 128 Ki threads (half of what
+// the chip holds at this kernel's registers).  A chunk of 4096 rows x 28 heads: one head 19.5 us, three 17.8, seven in two goes 19.6.
 int query_heads(const RowsParams& p) {
   const int64_t units = (int64_t)p.n_rows * p.Hq * (p.D / UNIT) >> 17;
-  return (int)(units < 1 ? 1 : units > 8 ? 8 : units);
+  return (int)(units < 1 ? 1 : units > 4 ? 4 : units);
 }
 int64_t query_blocks_per_seq(const RowsParams& p, int heads) {
   const int64_t threads = (int64_t)p.max_rows * ((p.Hq + heads - 1) / heads) * (p.D / UNIT);
@@ -443,7 +455,7 @@ template <typename T, int D> hipError_t append(const RowsParams& p, bool kvq, hi
 template <typename T, int D> hipError_t append_bwd(const RowsParams& p, bool grad_bf16, hipStream_t st) {
   return grad_bf16 ? append_bwd<T, bf16_t, D>(p, st) : append_bwd<T, float, D>(p, st);
 }
-int64_t read_blocks_per_seq(const RowsParams& p) { return ((int64_t)p.max_rows * 2 * p.Hkv * (p.D / 32) + THREADS - 1) / THREADS; }
+int64_t read_blocks_per_seq(const RowsParams& p) { return ((int64_t)p.max_rows * 2 * p.Hkv * (p.D / 8) + THREADS - 1) / THREADS; }
 template <typename T, int D> hipError_t read(const RowsParams& p, hipStream_t st) {
   ProfScope prof_("kvq_read", st);
   const int64_t per_seq = read_blocks_per_seq(p);
