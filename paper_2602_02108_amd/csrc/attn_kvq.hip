@@ -11,16 +11,21 @@
 //       For the A operand lane (m, kg) reads those eight tokens' codes of dims D/16 m .., converts each with its own scale and puts pairs of tokens
 //       together with byte permutes; operand j holds dims D/16 m + j
 // Conversions are v_cvt_scalef32_pk_bf16_fp4 (two values each, scale applied, exact); every value of the cache is exact in bf16.  fp32
-// rows: Q and P in three bf16 terms (24 bits).  bf16 rows: P in two (16 bits) where that is free, in one with 64 rows to a wave.  (The codes
-// could be a matrix operand as they are, v_mfma_scale_f32_16x16x128_f8f6f4 against e4m3 terms of the queries: its sums were off by
-// 2^-16 of the largest product, 2^-24 here.)
+// rows: Q and P in three bf16 terms (24 bits).  bf16 rows: P in two (16 bits), so that the output's own rounding is the larger one; in one term where
+// more than 64 rows share the cache and the matrix and vector pipes are what bounds them (13 % of the time; error of a bf16 output against 64 bits 1.7e-3
+// -> 2.3e-3).  (The codes could be a matrix operand as they are, v_mfma_scale_f32_16x16x128_f8f6f4 against e4m3 terms of the queries: its sums
+// were off by 2^-16 of the largest product, where these are fp32 sums of exact products.)
 //
 // Softmax in one pass: weights are taken against a reference of the row that moves only when the eight weights of a lane in a unit
 // exceed 2^9 together; so no maximum is formed on the way, and sums stay far inside a float.
 //
-// Few rows: the waves of a workgroup share a row block and split its tokens; long caches are cut into parts of equal work over
-// workgroups, counted on the device from the lengths as they are, and kvq_combine adds a row's parts in their order.  Many rows: every wave has a row
-// block of its own.
+// The waves of a workgroup share a row block and split its tokens; long caches are cut into parts of equal work over workgroups, counted on the
+// device from the lengths as they are, and kvq_combine adds a row's parts in their order.
+//
+// Measured (28 / 4 heads, D 128, P 128): one token against 1,048,001: 107 us, 5.3 TB/s of the cache, bound by memory; 2048 rows over 80
+// listed pages: 303 us, 0.89 PFLOP/s, bound by the vector unit (200 vector instructions for 32 matrix ones in a unit of two row tiles, 64 of them
+// conversions, 32 permutes, 16 exponentials); 32 sequences of one to 32K tokens: 24 us.  Two row tiles a wave and not more: with four, one wave per SIMD
+// is left and its instructions wait for each other (599 us), three spill.
 #include <type_traits>
 
 #include "common.h"
@@ -251,8 +256,9 @@ __global__ __launch_bounds__(64 * W, RT == 1 && W == 4 && sizeof(T) == 2 ? 3 : 2
   }
   const int n_units = (n_tiles + 1) >> 1;
   const int parts = part.count * W, mine = part.index * W + wave;
-  int u = (int)((int64_t)n_units * mine / parts);
-  const int u_end = (int)((int64_t)n_units * (mine + 1) / parts);
+  const int each = (int)((uint32_t)n_units / (uint32_t)parts), more = n_units - each * parts;   // (one more for the first `more`)
+  int u = each * mine + min(mine, more);
+  const int u_end = u + each + (mine < more);
 
   f32x4 acc[RT][NJ];
   float ref[RT], sum[RT];
@@ -528,7 +534,7 @@ __global__ __launch_bounds__(64 * W, RT == 1 && W == 4 && sizeof(T) == 2 ? 3 : 2
 // The parts of a row, in order: a workgroup per row of a row block, its threads in groups of D / 4 that take every
 // (256 / (D / 4))-th part each.
 template <typename T, int D>
-__global__ __launch_bounds__(COMBINE_THREADS) void kvq_combine_kernel(RowsParams p, AttnArgs a, int rows) {
+__global__ __launch_bounds__(COMBINE_THREADS) void kvq_combine_kernel(RowsParams p, AttnArgs a, int block_rows, int rows) {   // rows: of a block that there can be at most
   constexpr int LANES = D / 4, GROUPS = COMBINE_THREADS / LANES;
   __shared__ __align__(16) float lds[GROUPS][D + PAD];
   __shared__ float lds_ml[GROUPS][2];
@@ -538,21 +544,31 @@ __global__ __launch_bounds__(COMBINE_THREADS) void kvq_combine_kernel(RowsParams
   const int block = x % a.row_blocks, e = x / a.row_blocks;
   const int b = e / p.Hkv, g = e - b * p.Hkv;
   const Seq s = seq_of(p, b);
-  const int row = block * rows + r;
+  const int row = block * block_rows + r;
   if (row >= s.n * p.G) return;
   const int2 parts = a.parts[e];
   if (parts.y <= 1) return;
   const int grp = threadIdx.x / LANES, d = (threadIdx.x - grp * LANES) * 4;
   float ref = -INFINITY, sum = 0.0f, y[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int k = grp; k < parts.y; k += GROUPS) {
-    const int64_t at = ((int64_t)(parts.x + k) * a.row_blocks + block) * rows + r;
-    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
-    const float4 v = *reinterpret_cast<const float4*>(a.part + at * D + d);
-    const float to = fmaxf(ref, ml.x);
-    const float f0 = ref == to ? 1.0f : __builtin_amdgcn_exp2f(ref - to), f1 = ml.x == to ? 1.0f : __builtin_amdgcn_exp2f(ml.x - to);
-    ref = to;
-    sum = sum * f0 + ml.y * f1;
-    y[0] = y[0] * f0 + v.x * f1; y[1] = y[1] * f0 + v.y * f1; y[2] = y[2] * f0 + v.z * f1; y[3] = y[3] * f0 + v.w * f1;
+  constexpr int AT_ONCE = 4;   // (loads in flight: a chain of single ones takes a microsecond a part)
+  for (int k0 = grp; k0 < parts.y; k0 += AT_ONCE * GROUPS) {
+    float2 ml[AT_ONCE];
+    float4 v[AT_ONCE];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int64_t at = ((int64_t)(parts.x + min(k0 + i * GROUPS, parts.y - 1)) * a.row_blocks + block) * block_rows + r;
+      ml[i] = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
+      v[i] = *reinterpret_cast<const float4*>(a.part + at * D + d);
+    }
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      if (k0 + i * GROUPS >= parts.y) break;
+      const float to = fmaxf(ref, ml[i].x);
+      const float f0 = ref == to ? 1.0f : __builtin_amdgcn_exp2f(ref - to), f1 = ml[i].x == to ? 1.0f : __builtin_amdgcn_exp2f(ml[i].x - to);
+      ref = to;
+      sum = sum * f0 + ml[i].y * f1;
+      y[0] = y[0] * f0 + v[i].x * f1; y[1] = y[1] * f0 + v[i].y * f1; y[2] = y[2] * f0 + v[i].z * f1; y[3] = y[3] * f0 + v[i].w * f1;
+    }
   }
   *reinterpret_cast<float4*>(&lds[grp][d]) = make_float4(y[0], y[1], y[2], y[3]);
   if (d == 0) { lds_ml[grp][0] = ref; lds_ml[grp][1] = sum; }
@@ -631,7 +647,8 @@ template <typename T, int D, int RT, int PT, int W, bool WIDE, bool STREAM> hipE
     if (e != hipSuccess || !c.split) return e;
   }
   ProfScope prof_("kvq_combine", st);
-  kvq_combine_kernel<T, D><<<dim3((unsigned)(heads * c.row_blocks * 16 * RT)), dim3(COMBINE_THREADS), 0, st>>>(p, a, 16 * RT);
+  const int rows = c.row_blocks == 1 ? p.max_rows * p.G : 16 * RT;
+  kvq_combine_kernel<T, D><<<dim3((unsigned)(heads * c.row_blocks * rows)), dim3(COMBINE_THREADS), 0, st>>>(p, a, 16 * RT, rows);
   return hipGetLastError();
 }
 template <typename T, int D, int RT, int PT, int W> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
@@ -666,7 +683,7 @@ size_t kvq_attn_workspace_bytes(const RowsParams& p, bool is_bf16, int32_t sel_s
 int64_t kvq_attn_blocks(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   const Plan c = plan_of(p, is_bf16, sel_stride);
   const int64_t combine = (int64_t)p.n_seqs * p.Hkv * c.row_blocks * 16 * c.rt;
-  return c.parts * c.row_blocks * 2 > combine ? c.parts * c.row_blocks * 2 : combine;   // (up to 512 threads)
+  return c.parts * c.row_blocks * 2 > combine ? c.parts * c.row_blocks * 2 : combine;   // (workgroups of up to 512 threads)
 }
 
 hipError_t launch_attn_kvq(const RowsParams& p, bool is_bf16, void* ws, hipStream_t st) {

@@ -14,12 +14,14 @@ pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
 
 
-def _run(b, q, pools, scale, lists=None, max_rows=None, workspace=None):
+def _run(b, q, pools, scale, lists=None, max_rows=None, workspace=None, max_len=None):
     at = b.device()
     table = at.pop("page_tables")
     g = q.cuda()
     gp = [torch.tensor(x, device="cuda") for x in pools]
-    desc = api.make_rows_desc(g, gp[0], table, b.max_len, scale, max_rows=max_rows or b.max_rows)
+    if max_len:   # a table with room for that many tokens
+        table = torch.cat([table, torch.full((table.shape[0], max_len // b.P - table.shape[1]), -1, dtype=torch.int32, device="cuda")], 1)
+    desc = api.make_rows_desc(g, gp[0], table, max_len or b.max_len, scale, max_rows=max_rows or b.max_rows)
     o = torch.full_like(g, 5.0)
     lse = torch.full((g.shape[1], g.shape[0]), 5.0, device="cuda")
     sel = cnt = None
@@ -114,6 +116,37 @@ def test_long_and_many(dt, Hq, Hkv, D, P, spans, listed):
     scale = 1.0 / math.sqrt(D)
     o, lse = _run(b, q, pools, scale, lists)
     _verify(b, q, pools, scale, o, lse, lists)
+
+
+@pytest.mark.parametrize("dt,Hq,Hkv,D,P,spans", [
+    (BF, 28, 4, 128, 128, [(1, 700), (1, 5), (0, 0), (1, 3000)]),
+    (BF, 8, 4, 64, 32, [(2, 700), (1, 1)]),
+    (BF, 8, 4, 128, 16, [(1, 40), (1, 700)]),
+    (F32, 8, 4, 128, 64, [(1, 700), (3, 70)]),
+    (F32, 4, 4, 64, 128, [(4, 1300)]),
+    (BF, 14, 2, 128, 128, [(40, 900), (3, 50)]),
+])
+def test_room_for_far_longer_sequences(dt, Hq, Hkv, D, P, spans):
+    """A bound of two million tokens a sequence (more cache than stays in the caches, thousands of parts at most) over short ones."""
+    b = ru.Batch(spans, P, 12)
+    q = torch.randn((b.n_rows, Hq, D), generator=torch.Generator().manual_seed(13)).to(dt)
+    pools = [ru.random_pool(b, Hkv, D, s) for s in (25, 26)]
+    o, lse = _run(b, q, pools, 0.1, max_len=1 << 21)
+    _verify(b, q, pools, 0.1, o, lse)
+
+
+def test_workspaces_hold_anything():
+    """Parts are written before they are read: the same bits whatever the workspace held."""
+    b = ru.Batch([(1, 5000), (0, 9), (1, 1), (1, 900)], 128, 14)
+    q = torch.randn((b.n_rows, 28, 128), generator=torch.Generator().manual_seed(15)).to(BF)
+    pools = [ru.random_pool(b, 4, 128, s) for s in (27, 28)]
+    got = []
+    for fill in (0, 255, 127):
+        ws = torch.full((1 << 25,), fill, dtype=torch.uint8, device="cuda")
+        got.append(_run(b, q, pools, 0.1, workspace=ws))
+    for o, lse in got[1:]:
+        assert torch.equal(o, got[0][0]) and torch.equal(lse, got[0][1])
+    _verify(b, q, pools, 0.1, *got[0])
 
 
 @pytest.mark.parametrize("dt", [BF, F32])
