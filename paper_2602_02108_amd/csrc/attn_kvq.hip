@@ -158,33 +158,43 @@ template <int X, int D> __device__ __forceinline__ void pairs(const Raw<D>& raw,
 }
 
 // ---- the parts of a call ------------------------------------------------------------------------------------------------
-// A bound of the units that the rows of (sequence, KV head) e see, -1 if it has no rows.
+// A bound of the units that the rows of (sequence, KV head) e see, -1 if it has no rows.  (No branch on a lane's values: a lane asks for several.)
 __device__ __forceinline__ int units_of(const RowsParams& p, int e) {
-  const int b = e / p.Hkv;
-  const Seq s = seq_of(p, b);
-  if (s.n == 0) return -1;
+  const Seq s = seq_of(p, e / p.Hkv);
   const int64_t tokens = p.sel ? (int64_t)min(max(p.sel_count[e], 0), p.sel_stride) * p.P : s.len;
-  return (int)((min(tokens, (int64_t)p.max_len) + 31) >> 5);
+  const int units = (int)((min(tokens, (int64_t)p.max_len) + 31) >> 5);
+  return s.n == 0 ? -1 : units;
 }
 struct Part { int e, first, index, count; };   // (sequence, KV head), its first part, this one of it, its number of parts
 // Part x of the call, by every lane of a wave; e < 0: there are fewer.
 __device__ __forceinline__ Part part_at(const RowsParams& p, const AttnArgs& a, int x, int lane) {
   const int n = p.n_seqs * p.Hkv;
   if (!a.split) return {x, x, 0, 1};
+  constexpr int HELD = 4;   // of a lane, loaded together (256 in all; more are asked for again)
+  int held[HELD];
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) held[i] = 64 * i < n ? units_of(p, min(64 * i + lane, n - 1)) : -1;
   float total = 0.0f;
-  int mine = -1;
-  for (int e = lane; e < n; e += 64) {
-    mine = units_of(p, e);
-    total += (float)max(mine, 0);
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    if (64 * i + lane >= n) held[i] = -1;
+    total += (float)max(held[i], 0);
   }
+  for (int e = 64 * HELD + lane; e < n; e += 64) total += (float)max(units_of(p, e), 0);
 #pragma unroll
   for (int w = 1; w < 64; w *= 2) total += __shfl_xor(total, w, 64);
-  const int per = max(a.min_units, (int)(total / (float)a.target) + 1);   // (the same sum in every wave of both kernels)
+  const int per = max(a.min_units, (int)(total / (float)a.target) + 1);   // (the same sum in every wave)
   int before = 0;
   for (int e0 = 0; e0 < n; e0 += 64) {
-    const int e = e0 + lane;
-    const int units = n <= 64 ? mine : e < n ? units_of(p, e) : -1;
-    const int parts = units < 0 ? 0 : max(1, (units + per - 1) / per);
+    int units = -1;
+    if (e0 >= 64 * HELD) {
+      units = e0 + lane < n ? units_of(p, e0 + lane) : -1;
+    } else {
+#pragma unroll
+      for (int i = 0; i < HELD; ++i)
+        if (e0 == 64 * i) units = held[i];
+    }
+    const int parts = units < 0 ? 0 : max(1, (int)((uint32_t)(units + per - 1) / (uint32_t)per));
     int upto = parts;
 #pragma unroll
     for (int w = 1; w < 64; w *= 2) {
@@ -531,14 +541,17 @@ __global__ __launch_bounds__(64 * W, RT == 1 && W == 4 && sizeof(T) == 2 ? 3 : 2
   }
 }
 
-// The parts of a row, in order: a workgroup per row of a row block, its threads in groups of D / 4 that take every
-// (256 / (D / 4))-th part each.
-template <typename T, int D>
+// The parts of a row, in order: a workgroup per row of a row block and slice of DW dims, its threads in groups of DW / 4 that take every
+// (256 / (DW / 4))-th part each.  A compute unit takes in about 10 B/ns of lines that others wrote, so a few rows of many parts go in slices of a
+// line (7 x 4 rows of 127 parts: 10.3 us whole).
+template <typename T, int D, int DW>
 __global__ __launch_bounds__(COMBINE_THREADS) void kvq_combine_kernel(RowsParams p, AttnArgs a, int block_rows, int rows) {   // rows: of a block that there can be at most
-  constexpr int LANES = D / 4, GROUPS = COMBINE_THREADS / LANES;
-  __shared__ __align__(16) float lds[GROUPS][D + PAD];
+  constexpr int LANES = DW / 4, GROUPS = COMBINE_THREADS / LANES;
+  __shared__ __align__(16) float lds[GROUPS][DW + PAD];
   __shared__ float lds_ml[GROUPS][2];
   int x = blockIdx.x;
+  const int slice = x % (D / DW);
+  x /= D / DW;
   const int r = x % rows;
   x /= rows;
   const int block = x % a.row_blocks, e = x / a.row_blocks;
@@ -558,7 +571,7 @@ __global__ __launch_bounds__(COMBINE_THREADS) void kvq_combine_kernel(RowsParams
     for (int i = 0; i < AT_ONCE; ++i) {
       const int64_t at = ((int64_t)(parts.x + min(k0 + i * GROUPS, parts.y - 1)) * a.row_blocks + block) * block_rows + r;
       ml[i] = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
-      v[i] = *reinterpret_cast<const float4*>(a.part + at * D + d);
+      v[i] = *reinterpret_cast<const float4*>(a.part + at * D + slice * DW + d);
     }
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i) {
@@ -586,10 +599,10 @@ __global__ __launch_bounds__(COMBINE_THREADS) void kvq_combine_kernel(RowsParams
   }
   const int i = row / p.G, h = g * p.G + (row - i * p.G);
   const float f = total == 0.0f ? 0.0f : 1.0f / total;
-  T* dst = (T*)p.q_out.data + (int64_t)(s.row + i) * p.q_out.tok_stride + (int64_t)h * p.q_out.head_stride + d;
+  T* dst = (T*)p.q_out.data + (int64_t)(s.row + i) * p.q_out.tok_stride + (int64_t)h * p.q_out.head_stride + slice * DW + d;
   if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(pack2_bf16(o[0] * f, o[1] * f), pack2_bf16(o[2] * f, o[3] * f));
   else *reinterpret_cast<float4*>(dst) = make_float4(o[0] * f, o[1] * f, o[2] * f, o[3] * f);
-  if (d == 0) p.lse[(int64_t)h * p.n_rows + s.row + i] = total == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * LN2;
+  if (d == 0 && slice == 0) p.lse[(int64_t)h * p.n_rows + s.row + i] = total == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * LN2;
 }
 
 // How a call is cut.
@@ -648,7 +661,9 @@ template <typename T, int D, int RT, int PT, int W, bool WIDE, bool STREAM> hipE
   }
   ProfScope prof_("kvq_combine", st);
   const int rows = c.row_blocks == 1 ? p.max_rows * p.G : 16 * RT;
-  kvq_combine_kernel<T, D><<<dim3((unsigned)(heads * c.row_blocks * rows)), dim3(COMBINE_THREADS), 0, st>>>(p, a, 16 * RT, rows);
+  const int64_t wgs = heads * c.row_blocks * rows;
+  if (wgs < 256 && c.parts > 32 * heads) kvq_combine_kernel<T, D, 32><<<dim3((unsigned)(wgs * (D / 32))), dim3(COMBINE_THREADS), 0, st>>>(p, a, 16 * RT, rows);
+  else kvq_combine_kernel<T, D, D><<<dim3((unsigned)wgs), dim3(COMBINE_THREADS), 0, st>>>(p, a, 16 * RT, rows);
   return hipGetLastError();
 }
 template <typename T, int D, int RT, int PT, int W> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
