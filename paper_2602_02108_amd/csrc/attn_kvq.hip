@@ -68,7 +68,7 @@ struct AttnArgs {
   int target, min_units;       // parts to aim at; units of a part at least
   int2* parts;                 // [sequence * Hkv + KV head]: first part, number of parts
   float* part;                 // [part][row block][row of the block][D] sums
-  float* part_ml;              // [part][row block][row][2]: reference, sum
+  float* part_ml;              // [part][row block][row][4]: reference, sum, sum of the rounded weights
 };
 
 // Codes and scales of a unit as a lane reads them.
@@ -271,11 +271,11 @@ __global__ __launch_bounds__(64 * W, RT == 1 && W == 4 && sizeof(T) == 2 ? 3 : 2
   const int u_end = u + each + (mine < more);
 
   f32x4 acc[RT][NJ];
-  float ref[RT], sum[RT];
+  float ref[RT], sum[RT], held[RT];   // held: the sum of the weights as the product takes them
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     ref[rt] = -INFINITY;
-    sum[rt] = 0.0f;
+    sum[rt] = held[rt] = 0.0f;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) acc[rt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -387,6 +387,7 @@ __global__ __launch_bounds__(64 * W, RT == 1 && W == 4 && sizeof(T) == 2 ? 3 : 2
         const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref[rt] - to);
         ref[rt] = to;
         sum[rt] *= f;
+        held[rt] *= f;
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[rt][j] *= f;
         weights(rt);
@@ -402,6 +403,7 @@ __global__ __launch_bounds__(64 * W, RT == 1 && W == 4 && sizeof(T) == 2 ? 3 : 2
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           w[e] = pack2_bf16(z[rt][2 * e], z[rt][2 * e + 1]);
+          if (PT == 1) held[rt] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[e]), __builtin_bit_cast(bf16x2, 0x3f803f80u), held[rt], false);
           if (t + 1 < PT) less(z[rt][2 * e], z[rt][2 * e + 1], w[e]);
         }
         pf[rt][t] = make_uint4(w[0], w[1], w[2], w[3]);
@@ -487,34 +489,40 @@ __global__ __launch_bounds__(64 * W, RT == 1 && W == 4 && sizeof(T) == 2 ? 3 : 2
   for (int rt = 0; rt < RT; ++rt) {
     sum[rt] += __shfl_xor(sum[rt], 16, 64);
     sum[rt] += __shfl_xor(sum[rt], 32, 64);
+    if (PT == 1) {
+      held[rt] += __shfl_xor(held[rt], 16, 64);
+      held[rt] += __shfl_xor(held[rt], 32, 64);
+    } else {
+      held[rt] = sum[rt];
+    }
   }
-  auto put = [&](int r, int d, const float* y, float ref_r, float sum_r, bool first) __attribute__((always_inline)) {   // four dims of row r of the block
+  auto put = [&](int r, int d, const float* y, float ref_r, float sum_r, float held_r, bool first) __attribute__((always_inline)) {   // four dims of row r of the block
     const int row = r0 + r;
     if (row >= n_rows) return;
     if (part.count > 1) {
       const int64_t at = (int64_t)blockIdx.x * ROWS + r;
       *reinterpret_cast<float4*>(a.part + at * D + d) = make_float4(y[0], y[1], y[2], y[3]);
-      if (first) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(ref_r, sum_r);
+      if (first) *reinterpret_cast<float4*>(a.part_ml + at * 4) = make_float4(ref_r, sum_r, held_r, 0.0f);
       return;
     }
     const int i = row / p.G, h = g * p.G + (row - i * p.G);
-    const float f = sum_r == 0.0f ? 0.0f : 1.0f / sum_r;
+    const float f = held_r == 0.0f ? 0.0f : 1.0f / held_r;
     T* dst = (T*)p.q_out.data + (int64_t)(s.row + i) * p.q_out.tok_stride + (int64_t)h * p.q_out.head_stride + d;
     if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(pack2_bf16(y[0] * f, y[1] * f), pack2_bf16(y[2] * f, y[3] * f));
     else *reinterpret_cast<float4*>(dst) = make_float4(y[0] * f, y[1] * f, y[2] * f, y[3] * f);
     if (first) p.lse[(int64_t)h * p.n_rows + s.row + i] = sum_r == 0.0f ? -INFINITY : (ref_r + __builtin_amdgcn_logf(sum_r)) * LN2;
   };
 
-  // the waves' sums, one row tile at a time: [wave][16][D + PAD] floats, [wave][16][2] references and sums
+  // the waves' sums, one row tile at a time: [wave][16][D + PAD] floats, [wave][16][4] references and sums of weights
   float* ml = merge + W * 16 * (D + PAD);
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     if (rt) __syncthreads();
-    if (kg == 0) *reinterpret_cast<float2*>(ml + (wave * 16 + m) * 2) = make_float2(ref[rt], sum[rt]);
+    if (kg == 0) *reinterpret_cast<float4*>(ml + (wave * 16 + m) * 4) = make_float4(ref[rt], sum[rt], held[rt], 0.0f);
     __syncthreads();
     float to = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < W; ++w) to = fmaxf(to, ml[(w * 16 + m) * 2]);
+    for (int w = 0; w < W; ++w) to = fmaxf(to, ml[(w * 16 + m) * 4]);
     const float f = ref[rt] == to ? 1.0f : __builtin_amdgcn_exp2f(ref[rt] - to);
     float* mine = merge + (wave * 16 + m) * (D + PAD) + (D / 4) * kg;
 #pragma unroll
@@ -526,17 +534,19 @@ __global__ __launch_bounds__(64 * W, RT == 1 && W == 4 && sizeof(T) == 2 ? 3 : 2
     for (int e = threadIdx.x; e < 16 * (D / 4); e += 64 * W) {
       const int r = e / (D / 4), d = (e - r * (D / 4)) * 4;
       if (r0 + 16 * rt + r >= n_rows) break;
-      float y[4] = {0.f, 0.f, 0.f, 0.f}, ref_r = -INFINITY, sum_r = 0.0f;
+      float y[4] = {0.f, 0.f, 0.f, 0.f}, ref_r = -INFINITY, sum_r = 0.0f, held_r = 0.0f;
 #pragma unroll
-      for (int w = 0; w < W; ++w) ref_r = fmaxf(ref_r, ml[(w * 16 + r) * 2]);
+      for (int w = 0; w < W; ++w) ref_r = fmaxf(ref_r, ml[(w * 16 + r) * 4]);
 #pragma unroll
       for (int w = 0; w < W; ++w) {
         const float4 v = *reinterpret_cast<const float4*>(merge + (w * 16 + r) * (D + PAD) + d);
-        const float rw = ml[(w * 16 + r) * 2], sw = ml[(w * 16 + r) * 2 + 1];
-        sum_r += sw * (rw == ref_r ? 1.0f : __builtin_amdgcn_exp2f(rw - ref_r));
+        const float4 mw = *reinterpret_cast<const float4*>(ml + (w * 16 + r) * 4);
+        const float fw = mw.x == ref_r ? 1.0f : __builtin_amdgcn_exp2f(mw.x - ref_r);
+        sum_r += mw.y * fw;
+        held_r += mw.z * fw;
         y[0] += v.x; y[1] += v.y; y[2] += v.z; y[3] += v.w;
       }
-      put(16 * rt + r, d, y, ref_r, sum_r, d == 0);
+      put(16 * rt + r, d, y, ref_r, sum_r, held_r, d == 0);
     }
   }
 }
@@ -548,7 +558,7 @@ template <typename T, int D, int DW>
 __global__ __launch_bounds__(COMBINE_THREADS) void kvq_combine_kernel(RowsParams p, AttnArgs a, int block_rows, int rows) {   // rows: of a block that there can be at most
   constexpr int LANES = DW / 4, GROUPS = COMBINE_THREADS / LANES;
   __shared__ __align__(16) float lds[GROUPS][DW + PAD];
-  __shared__ float lds_ml[GROUPS][2];
+  __shared__ float lds_ml[GROUPS][3];
   int x = blockIdx.x;
   const int slice = x % (D / DW);
   x /= D / DW;
@@ -562,15 +572,15 @@ __global__ __launch_bounds__(COMBINE_THREADS) void kvq_combine_kernel(RowsParams
   const int2 parts = a.parts[e];
   if (parts.y <= 1) return;
   const int grp = threadIdx.x / LANES, d = (threadIdx.x - grp * LANES) * 4;
-  float ref = -INFINITY, sum = 0.0f, y[4] = {0.f, 0.f, 0.f, 0.f};
+  float ref = -INFINITY, sum = 0.0f, held = 0.0f, y[4] = {0.f, 0.f, 0.f, 0.f};
   constexpr int AT_ONCE = 4;   // (loads in flight: a chain of single ones takes a microsecond a part)
   for (int k0 = grp; k0 < parts.y; k0 += AT_ONCE * GROUPS) {
-    float2 ml[AT_ONCE];
+    float4 ml[AT_ONCE];
     float4 v[AT_ONCE];
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i) {
       const int64_t at = ((int64_t)(parts.x + min(k0 + i * GROUPS, parts.y - 1)) * a.row_blocks + block) * block_rows + r;
-      ml[i] = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
+      ml[i] = *reinterpret_cast<const float4*>(a.part_ml + at * 4);
       v[i] = *reinterpret_cast<const float4*>(a.part + at * D + slice * DW + d);
     }
 #pragma unroll
@@ -580,14 +590,15 @@ __global__ __launch_bounds__(COMBINE_THREADS) void kvq_combine_kernel(RowsParams
       const float f0 = ref == to ? 1.0f : __builtin_amdgcn_exp2f(ref - to), f1 = ml[i].x == to ? 1.0f : __builtin_amdgcn_exp2f(ml[i].x - to);
       ref = to;
       sum = sum * f0 + ml[i].y * f1;
+      held = held * f0 + ml[i].z * f1;
       y[0] = y[0] * f0 + v[i].x * f1; y[1] = y[1] * f0 + v[i].y * f1; y[2] = y[2] * f0 + v[i].z * f1; y[3] = y[3] * f0 + v[i].w * f1;
     }
   }
   *reinterpret_cast<float4*>(&lds[grp][d]) = make_float4(y[0], y[1], y[2], y[3]);
-  if (d == 0) { lds_ml[grp][0] = ref; lds_ml[grp][1] = sum; }
+  if (d == 0) { lds_ml[grp][0] = ref; lds_ml[grp][1] = sum; lds_ml[grp][2] = held; }
   __syncthreads();
   if (grp) return;
-  float top = -INFINITY, total = 0.0f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  float top = -INFINITY, total = 0.0f, total_held = 0.0f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int k = 0; k < GROUPS; ++k) top = fmaxf(top, lds_ml[k][0]);
 #pragma unroll
@@ -595,10 +606,11 @@ __global__ __launch_bounds__(COMBINE_THREADS) void kvq_combine_kernel(RowsParams
     const float f = lds_ml[k][0] == top ? 1.0f : __builtin_amdgcn_exp2f(lds_ml[k][0] - top);
     const float4 v = *reinterpret_cast<const float4*>(&lds[k][d]);
     total += lds_ml[k][1] * f;
+    total_held += lds_ml[k][2] * f;
     o[0] += v.x * f; o[1] += v.y * f; o[2] += v.z * f; o[3] += v.w * f;
   }
   const int i = row / p.G, h = g * p.G + (row - i * p.G);
-  const float f = total == 0.0f ? 0.0f : 1.0f / total;
+  const float f = total_held == 0.0f ? 0.0f : 1.0f / total_held;
   T* dst = (T*)p.q_out.data + (int64_t)(s.row + i) * p.q_out.tok_stride + (int64_t)h * p.q_out.head_stride + slice * DW + d;
   if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(pack2_bf16(o[0] * f, o[1] * f), pack2_bf16(o[2] * f, o[3] * f));
   else *reinterpret_cast<float4*>(dst) = make_float4(o[0] * f, o[1] * f, o[2] * f, o[3] * f);
@@ -644,11 +656,11 @@ template <typename T, int D, int RT, int PT, int W, bool WIDE, bool STREAM> hipE
   if (c.split) {
     a.part = (float*)ws;
     a.part_ml = a.part + blocks * 16 * RT * D;
-    a.parts = (int2*)(a.part_ml + blocks * 16 * RT * 2);
+    a.parts = (int2*)(a.part_ml + blocks * 16 * RT * 4);
   }
   {
     ProfScope prof_("attn_kvq", st);
-    constexpr size_t lds = (size_t)(W * 16 * (D + PAD) + W * 16 * 2) * sizeof(float);
+    constexpr size_t lds = (size_t)(W * 16 * (D + PAD) + W * 16 * 4) * sizeof(float);
     const auto kernel = attn_kvq_kernel<T, D, RT, PT, W, WIDE, STREAM>;
     if (lds > 65536) {
       static DeviceOnce once;
@@ -693,7 +705,7 @@ template <typename T, int D> hipError_t attn(const RowsParams& p, void* ws, hipS
 size_t kvq_attn_workspace_bytes(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   const Plan c = plan_of(p, is_bf16, sel_stride);
   if (!c.split) return 0;
-  return (size_t)c.parts * c.row_blocks * 16 * c.rt * (p.D + 2) * sizeof(float) + (size_t)p.n_seqs * p.Hkv * sizeof(int2);
+  return (size_t)c.parts * c.row_blocks * 16 * c.rt * (p.D + 4) * sizeof(float) + (size_t)p.n_seqs * p.Hkv * sizeof(int2);
 }
 int64_t kvq_attn_blocks(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   const Plan c = plan_of(p, is_bf16, sel_stride);

@@ -135,6 +135,30 @@ def test_room_for_far_longer_sequences(dt, Hq, Hkv, D, P, spans):
     _verify(b, q, pools, 0.1, o, lse)
 
 
+@pytest.mark.parametrize("dt,Hq,Hkv,D,P,spans", [
+    (BF, 14, 2, 128, 128, [(40, 900), (1, 300)]), (BF, 4, 2, 64, 16, [(40, 500), (3, 30)]), (BF, 4, 2, 128, 64, [(2, 9000)]),
+    (BF, 7, 1, 128, 128, [(64, 20000)]), (F32, 4, 2, 64, 32, [(20, 300)]),
+])
+def test_constant_values_come_out_as_they_are(dt, Hq, Hkv, D, P, spans):
+    """V is 1.5 throughout: O is 1.5 whatever the weights are rounded to (they are divided by the sum of what the product took), in
+    every route; keys give the first tokens larger logits, so that the others' weights are alike and no powers of two."""
+    b = ru.Batch(spans, P, 18)
+    q = torch.ones((b.n_rows, Hq, D), dtype=dt)
+    pools = [ru.random_pool(b, Hkv, D, s) for s in (29, 30)]
+    for s, (_, t) in enumerate(b.spans):
+        for l in range(-(-t // P)):
+            pos = l * P + np.arange(P)
+            k = np.where(pos < 5, 0.5, 0.0)[None, :, None] * np.ones((Hkv, 1, D))
+            for pool, x in ((pools[0], k), (pools[1], np.full((Hkv, P, D), 1.5))):
+                code, byte = ru.quantise(x)
+                byte[:, min(P, t - l * P):] = 255
+                pool[b.tables[s, l]] = ru.pack(code, byte)
+    o, lse = _run(b, q, pools, 0.37 / D)
+    # one rounding of the output, of a value that is off by the sums' 2^-20 at most
+    assert (o[:b.rows].double() - 1.5).abs().max() <= 1.5 * (2.0 ** -19 if dt == F32 else 0.0)
+    _verify(b, q, pools, 0.37 / D, o, lse)
+
+
 def test_workspaces_hold_anything():
     """Parts are written before they are read: the same bits whatever the workspace held."""
     b = ru.Batch([(1, 5000), (0, 9), (1, 1), (1, 900)], 128, 14)
