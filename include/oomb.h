@@ -459,7 +459,8 @@ oomb_status oomb_kv_append_rope_bwd(const oomb_rows_desc* desc, const oomb_seqs*
 /*
  * A cache held in 4 bits ("kvq").  A pool is bytes [n_phys][Hkv][tile], tile = P * (D / 2 + D / 32): the codes [P][D / 2] of
  * a page's tokens (dim 2 i in the low half of byte i), then the scales [D / 32][P], one byte per block of 32 dims and token.  A code
- * is a sign bit over {0, 0.5, 1, 1.5, 2, 3, 4, 6} (e2m1), a scale byte s stands for 2^(s - 127), and 255 for NaN.
+ * is a sign bit over {0, 0.5, 1, 1.5, 2, 3, 4, 6} (e2m1), a scale byte s stands for 2^(s - 127), and 255 for NaN (the append writes 2 .. 252
+ * and 255, and a cache that is filled by other means keeps to these).
  * What a token takes is 68 bytes per head at D = 128, against 256 in bf16.
  *
  * oomb_kvq_append_rope: oomb_kv_append_rope into such pools.  A block's scale is the smallest power of two, 2^-125 .. 2^125, of

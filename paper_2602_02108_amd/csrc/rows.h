@@ -1,4 +1,4 @@
-// Packed rows of several sequences: what the kernels of rope_append.hip and attn_kvq.hip share (layouts: include/oomb.h).
+// Packed rows of several sequences: what the kernels of rope_append.hip and attn_kvq.h share (layouts: include/oomb.h).
 #pragma once
 #include "common.h"
 
@@ -70,6 +70,10 @@ hipError_t launch_append_rope_bwd(const RowsParams& p, bool is_bf16, bool grad_b
 hipError_t launch_kvq_read(const RowsParams& p, bool is_bf16, hipStream_t st);
 size_t kvq_attn_workspace_bytes(const RowsParams& p, bool is_bf16, int32_t sel_stride);
 hipError_t launch_attn_kvq(const RowsParams& p, bool is_bf16, void* ws, hipStream_t st);
+hipError_t launch_attn_kvq_bf16_128(const RowsParams& p, void* ws, hipStream_t st);
+hipError_t launch_attn_kvq_bf16_64(const RowsParams& p, void* ws, hipStream_t st);
+hipError_t launch_attn_kvq_f32_128(const RowsParams& p, void* ws, hipStream_t st);
+hipError_t launch_attn_kvq_f32_64(const RowsParams& p, void* ws, hipStream_t st);
 // workgroups that a launch would take (the grid may hold 2^24 - 1 of 256 threads)
 int64_t append_rope_blocks(const RowsParams& p, bool kvq);
 int64_t kvq_read_blocks(const RowsParams& p);
