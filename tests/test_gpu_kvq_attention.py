@@ -364,6 +364,59 @@ def test_captured_generation_replays_like_eager_steps():
             assert torch.equal(a, c), f"replay {i}"
 
 
+def test_two_captured_graphs_share_a_workspace():
+    """Nothing stays in a workspace from call to call: graphs of other shapes replayed in turn over one give the eager results."""
+    ws = torch.empty(1 << 25, dtype=torch.uint8, device="cuda")
+    calls = []
+    for seed, (spans, Hq, Hkv, D, P) in enumerate([([(1, 6000), (1, 40)], 28, 4, 128, 128), ([(5, 3000), (2, 900), (5, 5)], 14, 2, 64, 16)]):
+        b = ru.Batch(spans, P, seed)
+        q = torch.randn((b.n_rows, Hq, D), generator=torch.Generator().manual_seed(seed)).to(BF).cuda()
+        gp = [torch.tensor(ru.random_pool(b, Hkv, D, 31 + 2 * seed + i), device="cuda") for i in range(2)]
+        at = b.device()
+        table = at.pop("page_tables")
+        desc = api.make_rows_desc(q, gp[0], table, b.max_len, 0.1, max_rows=b.max_rows)
+        assert 0 < api.kvq_workspace_bytes(desc) <= ws.numel()
+        o, lse = torch.zeros_like(q), torch.zeros((Hq, b.n_rows), device="cuda")
+
+        def call(desc=desc, q=q, gp=gp, table=table, at=at, o=o, lse=lse):
+            api.paged_attn_fwd_kvq(desc, q, *gp, table, o=o, lse=lse, workspace=ws, **at)
+
+        call()
+        torch.cuda.synchronize()
+        want = o.clone(), lse.clone()
+        graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graph, stream=side):
+            call()
+        calls.append((graph, o, lse, want, call))   # (the call holds what its graph reads)
+    for _ in range(3):
+        for graph, o, lse, want, _call in calls:
+            o.fill_(7.0)
+            lse.fill_(7.0)
+            o[-2:], lse[:, -2:] = 0.0, 0.0   # (rows of no sequence)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+
+
+def test_rows_in_front_of_the_first_sequence_are_left_alone():
+    b = ru.Batch([(3, 50), (2, 7)], 16, 3, behind=4)
+    q = torch.randn((b.n_rows, 4, 64), generator=torch.Generator().manual_seed(3)).cuda()
+    gp = [torch.tensor(ru.random_pool(b, 2, 64, s), device="cuda") for s in (35, 36)]
+    at = b.device()
+    table = at.pop("page_tables")
+    desc = api.make_rows_desc(q, gp[0], table, b.max_len, 0.1, max_rows=3)
+    o, lse = api.paged_attn_fwd_kvq(desc, q, *gp, table, **at)
+    moved = torch.cat([q[-2:], q[:-2]])
+    at["row_starts"] += 2
+    o2, lse2 = torch.full_like(o, 9.0), torch.full_like(lse, 9.0)
+    api.paged_attn_fwd_kvq(desc, moved, *gp, table, o=o2, lse=lse2, **at)
+    torch.cuda.synchronize()
+    assert torch.equal(o2[2:7], o[:5]) and torch.equal(lse2[:, 2:7], lse[:, :5])
+    assert (o2[:2] == 9.0).all() and (o2[7:] == 9.0).all() and (lse2[:, :2] == 9.0).all() and (lse2[:, 7:] == 9.0).all()
+
+
 def test_prompt_in_chunks_then_generation():
     """A prompt goes through in chunks -- append with rotation and means, pages picked from the means, attention over the picked pages --
     and tokens are generated over all of the cache; every output against 64 bits over what the cache holds."""
