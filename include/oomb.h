@@ -477,7 +477,8 @@ oomb_status oomb_kv_append_rope_bwd(const oomb_rows_desc* desc, const oomb_seqs*
  *   q, o [n_rows][Hq][D] (o must not overlap q);  lse [Hq][n_rows] float
  *   sel_pages [n_seqs][Hkv][sel_stride] int32 logical pages, ascending, distinct, and sel_count [n_seqs][Hkv]; NULL: every page
  * A row that sees no token gets O = 0 and LSE = -infinity.  A value that is not finite reaches the rows that see its token, and no
- * other.  fp32 rows: products in three bf16 terms per value (the cache's values are exact in one), sums in fp32.
+ * other.  bf16 rows: weights in two bf16 terms (2^-16 of a weight), whatever
+ * else is in the call; fp32 rows: products in three bf16 terms per value (the cache's values are exact in one).  Sums in fp32.
  * Results do not depend on scheduling.  Workspace: oomb_kvq_workspace_bytes(desc, sel_stride), sel_stride < 0 for every page (with
  * less than that, OOMB_ERR_WORKSPACE; it may be 0); calls that overlap in time need workspaces of their own.
  */

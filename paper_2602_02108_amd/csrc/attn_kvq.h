@@ -11,9 +11,8 @@
 //       For the A operand lane (m, kg) reads those eight tokens' codes of dims D/16 m .., converts each with its own scale and puts pairs of tokens
 //       together with byte permutes; operand j holds dims D/16 m + j
 // Conversions are v_cvt_scalef32_pk_bf16_fp4 (two values each, scale applied, exact); every value of the cache is exact in bf16.  fp32
-// rows: Q and P in three bf16 terms (24 bits).  bf16 rows: P in two (16 bits), so that the output's own rounding is the larger one; in one term where
-// more than 64 rows share the cache and the matrix and vector pipes are what bounds them (13 % of the time; error of a bf16 output against 64 bits 1.7e-3
-// -> 2.3e-3); the output is divided by the sum of the weights as rounded, the log-sum-exp is that of the exact ones.  (The codes could be a matrix operand as they are, v_mfma_scale_f32_16x16x128_f8f6f4 against e4m3 terms of the queries: its sums
+// rows: Q and P in three bf16 terms (24 bits).  bf16 rows: P in two (16 bits), so that the output's own rounding is the larger one, whatever else is in the
+// call (in one term a bf16 output is 2.3e-3 from 64 bits instead of 1.7e-3, which is its own rounding).  (The codes could be a matrix operand as they are, v_mfma_scale_f32_16x16x128_f8f6f4 against e4m3 terms of the queries: its sums
 // were off by 2^-16 of the largest product, where these are fp32 sums of exact products.)
 //
 // Softmax in one pass: weights are taken against a reference of the row that moves only when the eight weights of a lane in a unit
@@ -23,8 +22,8 @@
 // device from the lengths as they are, and kvq_combine adds a row's parts in their order.
 //
 // Measured (28 / 4 heads, D 128, P 128): one token against 1,048,001: 104 us, 5.5 TB/s of the cache, bound by memory; 2048 rows over 80
-// listed pages: 306 us, 0.88 PFLOP/s, bound by the vector unit (200 vector instructions for 32 matrix ones in a unit of two row tiles, 64 of them
-// conversions, 32 permutes, 16 exponentials); 32 sequences of one to 32K tokens: 24 us.  Two row tiles a wave and not more: with four, one wave per SIMD
+// listed pages: 381 us, 0.71 PFLOP/s, bound by the vector unit (240 vector instructions for 48 matrix ones in a unit of two row tiles, 64 of them
+// conversions, 32 permutes, 16 exponentials, 40 for the second terms of the weights); 32 sequences of one to 32K tokens: 24 us.  Two row tiles a wave and not more: with four, one wave per SIMD
 // is left and its instructions wait for each other (599 us), three spill.
 #pragma once
 #include <type_traits>
@@ -69,7 +68,7 @@ struct AttnArgs {
   int target, min_units;       // parts to aim at; units of a part at least
   int2* parts;                 // [sequence * Hkv + KV head]: first part, number of parts
   float* part;                 // [part][row block][row of the block][D] sums
-  float* part_ml;              // [part][row block][row][4]: reference, sum, sum of the rounded weights
+  float* part_ml;              // [part][row block][row][2]: reference, sum
 };
 
 // Codes and scales of a unit as a lane reads them.
@@ -214,10 +213,10 @@ __device__ __forceinline__ Part part_at(const RowsParams& p, const AttnArgs& a, 
 }
 
 // WIDE: pages of 32 tokens and more, a unit lies in one.  STREAM: codes past the caches.
-template <typename T, int D, int RT, int PT, int W, bool WIDE, bool STREAM>
+template <typename T, int D, int RT, int W, bool WIDE, bool STREAM>
 __global__ __launch_bounds__(64 * W, RT == 1 && W == 4 && sizeof(T) == 2 ? 3 : 2) void attn_kvq_kernel(RowsParams p, AttnArgs a) {
   extern __shared__ __align__(16) float merge[];
-  constexpr int QT = sizeof(T) == 2 ? 1 : 3, NC = D / 32, NJ = D / 16, ROWS = 16 * RT;
+  constexpr int QT = sizeof(T) == 2 ? 1 : 3, PT = sizeof(T) == 2 ? 2 : 3, NC = D / 32, NJ = D / 16, ROWS = 16 * RT;
   const int lane = threadIdx.x & 63, m = lane & 15, kg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int px = blockIdx.x / a.row_blocks, block = blockIdx.x - px * a.row_blocks;
@@ -272,11 +271,11 @@ __global__ __launch_bounds__(64 * W, RT == 1 && W == 4 && sizeof(T) == 2 ? 3 : 2
   const int u_end = u + each + (mine < more);
 
   f32x4 acc[RT][NJ];
-  float ref[RT], sum[RT], held[RT];   // held: the sum of the weights as the product takes them
+  float ref[RT], sum[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     ref[rt] = -INFINITY;
-    sum[rt] = held[rt] = 0.0f;
+    sum[rt] = 0.0f;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) acc[rt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -388,7 +387,6 @@ __global__ __launch_bounds__(64 * W, RT == 1 && W == 4 && sizeof(T) == 2 ? 3 : 2
         const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref[rt] - to);
         ref[rt] = to;
         sum[rt] *= f;
-        held[rt] *= f;
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[rt][j] *= f;
         weights(rt);
@@ -404,7 +402,6 @@ __global__ __launch_bounds__(64 * W, RT == 1 && W == 4 && sizeof(T) == 2 ? 3 : 2
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           w[e] = pack2_bf16(z[rt][2 * e], z[rt][2 * e + 1]);
-          if (PT == 1) held[rt] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[e]), __builtin_bit_cast(bf16x2, 0x3f803f80u), held[rt], false);
           if (t + 1 < PT) less(z[rt][2 * e], z[rt][2 * e + 1], w[e]);
         }
         pf[rt][t] = make_uint4(w[0], w[1], w[2], w[3]);
@@ -490,40 +487,34 @@ __global__ __launch_bounds__(64 * W, RT == 1 && W == 4 && sizeof(T) == 2 ? 3 : 2
   for (int rt = 0; rt < RT; ++rt) {
     sum[rt] += __shfl_xor(sum[rt], 16, 64);
     sum[rt] += __shfl_xor(sum[rt], 32, 64);
-    if (PT == 1) {
-      held[rt] += __shfl_xor(held[rt], 16, 64);
-      held[rt] += __shfl_xor(held[rt], 32, 64);
-    } else {
-      held[rt] = sum[rt];
-    }
   }
-  auto put = [&](int r, int d, const float* y, float ref_r, float sum_r, float held_r, bool first) __attribute__((always_inline)) {   // four dims of row r of the block
+  auto put = [&](int r, int d, const float* y, float ref_r, float sum_r, bool first) __attribute__((always_inline)) {   // four dims of row r of the block
     const int row = r0 + r;
     if (row >= n_rows) return;
     if (part.count > 1) {
       const int64_t at = (int64_t)blockIdx.x * ROWS + r;
       *reinterpret_cast<float4*>(a.part + at * D + d) = make_float4(y[0], y[1], y[2], y[3]);
-      if (first) *reinterpret_cast<float4*>(a.part_ml + at * 4) = make_float4(ref_r, sum_r, held_r, 0.0f);
+      if (first) *reinterpret_cast<float2*>(a.part_ml + at * 2) = make_float2(ref_r, sum_r);
       return;
     }
     const int i = row / p.G, h = g * p.G + (row - i * p.G);
-    const float f = held_r == 0.0f ? 0.0f : 1.0f / held_r;
+    const float f = sum_r == 0.0f ? 0.0f : 1.0f / sum_r;
     T* dst = (T*)p.q_out.data + (int64_t)(s.row + i) * p.q_out.tok_stride + (int64_t)h * p.q_out.head_stride + d;
     if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(pack2_bf16(y[0] * f, y[1] * f), pack2_bf16(y[2] * f, y[3] * f));
     else *reinterpret_cast<float4*>(dst) = make_float4(y[0] * f, y[1] * f, y[2] * f, y[3] * f);
     if (first) p.lse[(int64_t)h * p.n_rows + s.row + i] = sum_r == 0.0f ? -INFINITY : (ref_r + __builtin_amdgcn_logf(sum_r)) * LN2;
   };
 
-  // the waves' sums, one row tile at a time: [wave][16][D + PAD] floats, [wave][16][4] references and sums of weights
+  // the waves' sums, one row tile at a time: [wave][16][D + PAD] floats, [wave][16][2] references and sums of weights
   float* ml = merge + W * 16 * (D + PAD);
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     if (rt) __syncthreads();
-    if (kg == 0) *reinterpret_cast<float4*>(ml + (wave * 16 + m) * 4) = make_float4(ref[rt], sum[rt], held[rt], 0.0f);
+    if (kg == 0) *reinterpret_cast<float2*>(ml + (wave * 16 + m) * 2) = make_float2(ref[rt], sum[rt]);
     __syncthreads();
     float to = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < W; ++w) to = fmaxf(to, ml[(w * 16 + m) * 4]);
+    for (int w = 0; w < W; ++w) to = fmaxf(to, ml[(w * 16 + m) * 2]);
     const float f = ref[rt] == to ? 1.0f : __builtin_amdgcn_exp2f(ref[rt] - to);
     float* mine = merge + (wave * 16 + m) * (D + PAD) + (D / 4) * kg;
 #pragma unroll
@@ -535,19 +526,18 @@ __global__ __launch_bounds__(64 * W, RT == 1 && W == 4 && sizeof(T) == 2 ? 3 : 2
     for (int e = threadIdx.x; e < 16 * (D / 4); e += 64 * W) {
       const int r = e / (D / 4), d = (e - r * (D / 4)) * 4;
       if (r0 + 16 * rt + r >= n_rows) break;
-      float y[4] = {0.f, 0.f, 0.f, 0.f}, ref_r = -INFINITY, sum_r = 0.0f, held_r = 0.0f;
+      float y[4] = {0.f, 0.f, 0.f, 0.f}, ref_r = -INFINITY, sum_r = 0.0f;
 #pragma unroll
-      for (int w = 0; w < W; ++w) ref_r = fmaxf(ref_r, ml[(w * 16 + r) * 4]);
+      for (int w = 0; w < W; ++w) ref_r = fmaxf(ref_r, ml[(w * 16 + r) * 2]);
 #pragma unroll
       for (int w = 0; w < W; ++w) {
         const float4 v = *reinterpret_cast<const float4*>(merge + (w * 16 + r) * (D + PAD) + d);
-        const float4 mw = *reinterpret_cast<const float4*>(ml + (w * 16 + r) * 4);
+        const float2 mw = *reinterpret_cast<const float2*>(ml + (w * 16 + r) * 2);
         const float fw = mw.x == ref_r ? 1.0f : __builtin_amdgcn_exp2f(mw.x - ref_r);
         sum_r += mw.y * fw;
-        held_r += mw.z * fw;
         y[0] += v.x; y[1] += v.y; y[2] += v.z; y[3] += v.w;
       }
-      put(16 * rt + r, d, y, ref_r, sum_r, held_r, d == 0);
+      put(16 * rt + r, d, y, ref_r, sum_r, d == 0);
     }
   }
 }
@@ -559,7 +549,7 @@ template <typename T, int D, int DW>
 __global__ __launch_bounds__(COMBINE_THREADS) void kvq_combine_kernel(RowsParams p, AttnArgs a, int block_rows, int rows) {   // rows: of a block that there can be at most
   constexpr int LANES = DW / 4, GROUPS = COMBINE_THREADS / LANES;
   __shared__ __align__(16) float lds[GROUPS][DW + PAD];
-  __shared__ float lds_ml[GROUPS][3];
+  __shared__ float lds_ml[GROUPS][2];
   int x = blockIdx.x;
   const int slice = x % (D / DW);
   x /= D / DW;
@@ -573,15 +563,15 @@ __global__ __launch_bounds__(COMBINE_THREADS) void kvq_combine_kernel(RowsParams
   const int2 parts = a.parts[e];
   if (parts.y <= 1) return;
   const int grp = threadIdx.x / LANES, d = (threadIdx.x - grp * LANES) * 4;
-  float ref = -INFINITY, sum = 0.0f, held = 0.0f, y[4] = {0.f, 0.f, 0.f, 0.f};
+  float ref = -INFINITY, sum = 0.0f, y[4] = {0.f, 0.f, 0.f, 0.f};
   constexpr int AT_ONCE = 4;   // (loads in flight: a chain of single ones takes a microsecond a part)
   for (int k0 = grp; k0 < parts.y; k0 += AT_ONCE * GROUPS) {
-    float4 ml[AT_ONCE];
+    float2 ml[AT_ONCE];
     float4 v[AT_ONCE];
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i) {
       const int64_t at = ((int64_t)(parts.x + min(k0 + i * GROUPS, parts.y - 1)) * a.row_blocks + block) * block_rows + r;
-      ml[i] = *reinterpret_cast<const float4*>(a.part_ml + at * 4);
+      ml[i] = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
       v[i] = *reinterpret_cast<const float4*>(a.part + at * D + slice * DW + d);
     }
 #pragma unroll
@@ -591,15 +581,14 @@ __global__ __launch_bounds__(COMBINE_THREADS) void kvq_combine_kernel(RowsParams
       const float f0 = ref == to ? 1.0f : __builtin_amdgcn_exp2f(ref - to), f1 = ml[i].x == to ? 1.0f : __builtin_amdgcn_exp2f(ml[i].x - to);
       ref = to;
       sum = sum * f0 + ml[i].y * f1;
-      held = held * f0 + ml[i].z * f1;
       y[0] = y[0] * f0 + v[i].x * f1; y[1] = y[1] * f0 + v[i].y * f1; y[2] = y[2] * f0 + v[i].z * f1; y[3] = y[3] * f0 + v[i].w * f1;
     }
   }
   *reinterpret_cast<float4*>(&lds[grp][d]) = make_float4(y[0], y[1], y[2], y[3]);
-  if (d == 0) { lds_ml[grp][0] = ref; lds_ml[grp][1] = sum; lds_ml[grp][2] = held; }
+  if (d == 0) { lds_ml[grp][0] = ref; lds_ml[grp][1] = sum; }
   __syncthreads();
   if (grp) return;
-  float top = -INFINITY, total = 0.0f, total_held = 0.0f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  float top = -INFINITY, total = 0.0f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int k = 0; k < GROUPS; ++k) top = fmaxf(top, lds_ml[k][0]);
 #pragma unroll
@@ -607,11 +596,10 @@ __global__ __launch_bounds__(COMBINE_THREADS) void kvq_combine_kernel(RowsParams
     const float f = lds_ml[k][0] == top ? 1.0f : __builtin_amdgcn_exp2f(lds_ml[k][0] - top);
     const float4 v = *reinterpret_cast<const float4*>(&lds[k][d]);
     total += lds_ml[k][1] * f;
-    total_held += lds_ml[k][2] * f;
     o[0] += v.x * f; o[1] += v.y * f; o[2] += v.z * f; o[3] += v.w * f;
   }
   const int i = row / p.G, h = g * p.G + (row - i * p.G);
-  const float f = total_held == 0.0f ? 0.0f : 1.0f / total_held;
+  const float f = total == 0.0f ? 0.0f : 1.0f / total;
   T* dst = (T*)p.q_out.data + (int64_t)(s.row + i) * p.q_out.tok_stride + (int64_t)h * p.q_out.head_stride + slice * DW + d;
   if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(pack2_bf16(o[0] * f, o[1] * f), pack2_bf16(o[2] * f, o[3] * f));
   else *reinterpret_cast<float4*>(dst) = make_float4(o[0] * f, o[1] * f, o[2] * f, o[3] * f);
@@ -620,14 +608,13 @@ __global__ __launch_bounds__(COMBINE_THREADS) void kvq_combine_kernel(RowsParams
 
 // How a call is cut.
 struct Plan {
-  int rt, waves, many, stream, row_blocks, split, target, min_units;
+  int rt, waves, stream, row_blocks, split, target, min_units;
   int64_t parts;   // at most
 };
 Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   Plan c{};
   const int64_t rows = (int64_t)p.max_rows * p.G, heads = (int64_t)p.n_seqs * p.Hkv;
   c.rt = rows <= 16 || (!is_bf16 && p.D == 128) ? 1 : 2;   // (fp32 terms of two row tiles at head dim 128 do not fit the registers)
-  c.many = is_bf16 && rows > 64;
   c.row_blocks = (int)((rows + 16 * c.rt - 1) / (16 * c.rt));
   int64_t tokens = p.max_len;
   if (sel_stride >= 0 && (int64_t)sel_stride * p.P < tokens) tokens = (int64_t)sel_stride * p.P;
@@ -645,25 +632,25 @@ Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   c.split = units > 40 && each > 1 && target >= 2 * heads;
   c.target = (int)(target < 1 ? 1 : target);
   c.parts = !c.split ? heads : heads * each < target + heads ? heads * each : target + heads;
-  c.waves = c.split || c.many ? 4 : 8;
+  c.waves = c.split || (is_bf16 && rows > 64) ? 4 : 8;   // (2048 rows over 80 pages: eight waves 404 us, four 346, both in one term)
   // Codes past the caches once they would not stay in the last one (256 MiB) to the next call: 570 MB 117 -> 105 us, 62 MB 25.4 -> 26.2
   // (bf16 rows of head dim 128, where both were timed; the other forms are without it).
   c.stream = heads * tokens * 2 * (p.D / 2 + p.D / 32) > (256ll << 20);
   return c;
 }
 
-template <typename T, int D, int RT, int PT, int W, bool WIDE, bool STREAM> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
+template <typename T, int D, int RT, int W, bool WIDE, bool STREAM> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
   AttnArgs a{c.row_blocks, c.split, c.target, c.min_units, nullptr, nullptr, nullptr};
   const int64_t heads = (int64_t)p.n_seqs * p.Hkv, blocks = c.parts * c.row_blocks;
   if (c.split) {
     a.part = (float*)ws;
     a.part_ml = a.part + blocks * 16 * RT * D;
-    a.parts = (int2*)(a.part_ml + blocks * 16 * RT * 4);
+    a.parts = (int2*)(a.part_ml + blocks * 16 * RT * 2);
   }
   {
     ProfScope prof_("attn_kvq", st);
-    constexpr size_t lds = (size_t)(W * 16 * (D + PAD) + W * 16 * 4) * sizeof(float);
-    const auto kernel = attn_kvq_kernel<T, D, RT, PT, W, WIDE, STREAM>;
+    constexpr size_t lds = (size_t)(W * 16 * (D + PAD) + W * 16 * 2) * sizeof(float);
+    const auto kernel = attn_kvq_kernel<T, D, RT, W, WIDE, STREAM>;
     if (lds > 65536) {
       static DeviceOnce once;
       const hipError_t e = ensure_max_dynamic_lds(once, (const void*)kernel, (int)lds);
@@ -680,27 +667,23 @@ template <typename T, int D, int RT, int PT, int W, bool WIDE, bool STREAM> hipE
   else kvq_combine_kernel<T, D, D><<<dim3((unsigned)wgs), dim3(COMBINE_THREADS), 0, st>>>(p, a, 16 * RT, rows);
   return hipGetLastError();
 }
-template <typename T, int D, int RT, int PT, int W> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
-  if (p.P < 32) return run<T, D, RT, PT, W, false, false>(p, c, ws, st);
+template <typename T, int D, int RT, int W> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
+  if (p.P < 32) return run<T, D, RT, W, false, false>(p, c, ws, st);
   if constexpr (RT == 1 && W == 4 && D == 128 && sizeof(T) == 2) {
-    if (c.stream) return run<T, D, RT, PT, W, true, true>(p, c, ws, st);
+    if (c.stream) return run<T, D, RT, W, true, true>(p, c, ws, st);
   }
-  return run<T, D, RT, PT, W, true, false>(p, c, ws, st);
+  return run<T, D, RT, W, true, false>(p, c, ws, st);
 }
-template <typename T, int D, int RT, int PT> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
-  return c.waves == 8 ? run<T, D, RT, PT, 8>(p, c, ws, st) : run<T, D, RT, PT, 4>(p, c, ws, st);
+template <typename T, int D, int RT> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
+  return c.waves == 8 ? run<T, D, RT, 8>(p, c, ws, st) : run<T, D, RT, 4>(p, c, ws, st);
 }
 // (instantiated for one type and head dim per source file, which are compiled side by side)
 template <typename T, int D> hipError_t attn(const RowsParams& p, void* ws, hipStream_t st) {
   const Plan c = plan_of(p, sizeof(T) == 2, p.sel ? p.sel_stride : -1);
-  if constexpr (sizeof(T) == 2) {
-    if (c.many) return run<T, D, 2, 1, 4>(p, c, ws, st);
-    return c.rt == 1 ? run<T, D, 1, 2>(p, c, ws, st) : run<T, D, 2, 2>(p, c, ws, st);
-  } else if constexpr (D == 128) {
-    return run<T, D, 1, 3>(p, c, ws, st);
-  } else {
-    return c.rt == 1 ? run<T, D, 1, 3>(p, c, ws, st) : run<T, D, 2, 3>(p, c, ws, st);
+  if constexpr (sizeof(T) == 2 || D == 64) {
+    if (c.rt == 2) return run<T, D, 2>(p, c, ws, st);
   }
+  return run<T, D, 1>(p, c, ws, st);
 }
 
 }  // namespace

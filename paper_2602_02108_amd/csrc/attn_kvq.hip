@@ -6,7 +6,7 @@ namespace oomb {
 size_t kvq_attn_workspace_bytes(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   const Plan c = plan_of(p, is_bf16, sel_stride);
   if (!c.split) return 0;
-  return (size_t)c.parts * c.row_blocks * 16 * c.rt * (p.D + 4) * sizeof(float) + (size_t)p.n_seqs * p.Hkv * sizeof(int2);
+  return (size_t)c.parts * c.row_blocks * 16 * c.rt * (p.D + 2) * sizeof(float) + (size_t)p.n_seqs * p.Hkv * sizeof(int2);
 }
 int64_t kvq_attn_blocks(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   const Plan c = plan_of(p, is_bf16, sel_stride);

@@ -1,0 +1,46 @@
+"""GPU tests of the calls over packed rows at the edges of what the header allows."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2602_02108_amd import api
+
+import rows_util as ru
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def _batch(spans, P, Hq, Hkv, D, dt, seed, **kw):
+    """(batch, queries on the CPU and the GPU, pools as numpy and on the GPU, page tables, the other device arrays)"""
+    b = ru.Batch(spans, P, seed, **kw)
+    q = torch.randn((b.n_rows, Hq, D), generator=torch.Generator().manual_seed(seed)).to(dt)
+    pools = [ru.random_pool(b, Hkv, D, 100 * seed + i) for i in (1, 2)]
+    at = b.device()
+    return b, q, q.cuda(), pools, [torch.tensor(x, device="cuda") for x in pools], at.pop("page_tables"), at
+
+
+def _check(b, q, pools, scale, o, lse, terms, lists=None):
+    wo, wl, to, tl = ru.attend(b, q, *pools, scale, lists, terms)
+    live = slice(0, b.rows)
+    ru.check("LSE", lse.cpu().double().numpy()[:, live], wl[:, live], tl[:, live])
+    ru.check("O", o.cpu().double().numpy()[live], wo[live], to[live])
+
+
+# (spans, (Hq, Hkv), D, P): rows that share a cache below, at and past 64, alone and beside others, over few tokens, so that sums of
+# weights of either sign come out small and a weight's rounding shows beside the output's own
+@pytest.mark.parametrize("spans,heads,D,P", [
+    ([(16, 90)], (4, 1), 128, 128), ([(64, 130)], (1, 1), 128, 32), ([(65, 130)], (1, 1), 128, 32), ([(64, 100)], (2, 2), 64, 16),
+    ([(65, 100)], (2, 2), 64, 16), ([(9, 60), (1, 50)], (14, 2), 64, 16), ([(1, 100), (40, 170), (2, 64)], (14, 2), 128, 128),
+    ([(200, 260), (1, 33)], (28, 4), 128, 128),
+])
+def test_weights_of_bf16_rows_hold_sixteen_bits_in_every_call(spans, heads, D, P):
+    """Two bf16 terms of a weight: 2^-8 of it is left by the first rounding, 2^-8 of that by the second."""
+    b, q, gq, pools, gp, table, at = _batch(spans, P, *heads, D, BF, 41)
+    scale = 1.0 / math.sqrt(D)
+    desc = api.make_rows_desc(gq, gp[0], table, b.max_len, scale, max_rows=b.max_rows)
+    o, lse = api.paged_attn_fwd_kvq(desc, gq, *gp, table, **at)
+    _check(b, q, pools, scale, o, lse, 2.0 ** -16)
