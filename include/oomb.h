@@ -475,7 +475,8 @@ oomb_status oomb_kv_append_rope_bwd(const oomb_rows_desc* desc, const oomb_seqs*
  * t <= p of its sequence whose page is listed for KV head g = h / G:
  *   O[r,h,:] = sum_t exp(s_t - LSE) V[t],  LSE[h][r] = log sum_t exp(s_t),  s_t = sm_scale <Q[r,h], K[t]>
  *   q, o [n_rows][Hq][D] (o must not overlap q);  lse [Hq][n_rows] float
- *   sel_pages [n_seqs][Hkv][sel_stride] int32 logical pages, ascending, distinct, and sel_count [n_seqs][Hkv]; NULL: every page
+ *   sel_pages [n_seqs][Hkv][sel_stride] int32 logical pages, ascending, distinct, and sel_count [n_seqs][Hkv]; NULL: every page.
+ *            A count is cut to 0 .. sel_stride; sel_stride 0 lists nothing
  * A row that sees no token gets O = 0 and LSE = -infinity.  A value that is not finite reaches the rows that see its token, and no
  * other.  bf16 rows: weights in two bf16 terms (2^-16 of a weight), whatever
  * else is in the call; fp32 rows: products in three bf16 terms per value (the cache's values are exact in one).  Sums in fp32.

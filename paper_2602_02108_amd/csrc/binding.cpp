@@ -338,7 +338,9 @@ PyObject* attn_fwd_kvq(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     stride = (int32_t)sel->size(-1);
   }
   if (!place({q, kp, vp, pt, lens, starts, sel, sel ? cnt : nullptr, o, lse, ws}, &st, &guard)) return status(-1);
-  OOMB_CALL(oomb_paged_attn_fwd_kvq(&d, &seqs, &rq, ptr(kp), ptr(vp), (const int32_t*)ptr(sel), (const int32_t*)ptr(cnt), stride, &ro, (float*)ptr(lse), ptr(ws), bytes(ws), st));
+  // (lists without room are lists all the same: a tensor without elements has no address, so they go by that of the counts, which is not read through)
+  const int32_t* lists_at = (const int32_t*)ptr(sel && stride == 0 ? cnt : sel);
+  OOMB_CALL(oomb_paged_attn_fwd_kvq(&d, &seqs, &rq, ptr(kp), ptr(vp), lists_at, (const int32_t*)ptr(cnt), stride, &ro, (float*)ptr(lse), ptr(ws), bytes(ws), st));
 }
 
 #define OOMB_METHOD(name, fn) {name, (PyCFunction)(void (*)(void))(guarded<fn>), METH_FASTCALL, nullptr}

@@ -44,3 +44,17 @@ def test_weights_of_bf16_rows_hold_sixteen_bits_in_every_call(spans, heads, D, P
     desc = api.make_rows_desc(gq, gp[0], table, b.max_len, scale, max_rows=b.max_rows)
     o, lse = api.paged_attn_fwd_kvq(desc, gq, *gp, table, **at)
     _check(b, q, pools, scale, o, lse, 2.0 ** -16)
+
+
+@pytest.mark.parametrize("dt,spans,P", [(BF, [(1, 200), (3, 40)], 128), (F32, [(5, 77)], 16), (BF, [(1, 6000), (2, 50)], 128), (BF, [(80, 300)], 32)])
+def test_lists_without_room_list_nothing(dt, spans, P):
+    """sel_pages [n_seqs][Hkv][0]: no row sees a token, in a cache that is walked whole and in one that is split."""
+    b, q, gq, pools, gp, table, at = _batch(spans, P, 4, 2, 128, dt, 42)
+    desc = api.make_rows_desc(gq, gp[0], table, b.max_len, 0.1, max_rows=b.max_rows)
+    sel = torch.empty((len(spans), 2, 0), dtype=torch.int32, device="cuda")
+    for fill in (0, 3):   # (a count is cut to the row's room)
+        cnt = torch.full((len(spans), 2), fill, dtype=torch.int32, device="cuda")
+        o, lse = torch.full_like(gq, 5.0), torch.full((4, b.n_rows), 5.0, device="cuda")
+        api.paged_attn_fwd_kvq(desc, gq, *gp, table, sel, cnt, o, lse, **at)
+        assert (o[:b.rows] == 0).all() and (lse[:, :b.rows] == -math.inf).all()
+        assert (o[b.rows:] == 5.0).all() and (lse[:, b.rows:] == 5.0).all()
