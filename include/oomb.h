@@ -388,7 +388,11 @@ oomb_status oomb_check_inputs(const oomb_attn_desc* desc, const int32_t* page_ta
  * writes them.  Sequence b's logical page l is physical page page_tables[b][l]; pages may be shared by sequences as long as no
  * row is appended to them.
  * All of these arrays are read on the device (a captured graph follows them from replay to replay); what the host gives are bounds: no sequence has more than
- * max_rows rows or max_len tokens.  Rows beyond max_rows are left out, and lengths are cut to max_len.  A row of a
+ * max_rows rows or max_len tokens.  A launch holds fewer than 2^24 workgroups of 256 threads, and what a call launches goes by the bounds, n_seqs times what
+ * max_rows rows take (attention: max_rows * Hq / 32 of bf16, up to / 8 of few or of fp32 rows; read: max_rows * Hkv * D / 1024; appends and their
+ * backward: up to max_rows * Hq * D / 4096, and 2 Hkv D / 64 for each of the pages that max_rows rows touch): more is OOMB_ERR_UNSUPPORTED, and a
+ * closer bound helps.
+ * Rows beyond max_rows are left out, and lengths are cut to max_len.  A row of a
  * sequence shorter than its rows (a position below 0) does not exist: the appends and their backward leave it alone, for attention it sees nothing.  A physical page outside [0, num_phys_pages)
  * holds nothing: rows are not written there (their gradients and read values are 0) and attention does not see it.
  */

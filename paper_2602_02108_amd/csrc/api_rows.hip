@@ -161,17 +161,17 @@ oomb_status oomb_paged_attn_fwd_kvq(const oomb_rows_desc* desc, const oomb_seqs*
   OOMB_CHECK(check_rows(desc, KVQ, &p));
   if (!(desc->sm_scale > 0.f) || !std::isfinite(desc->sm_scale)) return OOMB_ERR_INVALID_ARG;
   OOMB_CHECK(check_seqs(seqs, &p));
+  if (sel_pages && (!sel_count || sel_stride < 0)) return OOMB_ERR_INVALID_ARG;
+  const bool bf = desc->dtype == OOMB_BF16;
+  const int32_t width = sel_pages ? sel_stride : -1;
+  if (!grid_fits(kvq_attn_blocks(p, bf, width))) return OOMB_ERR_UNSUPPORTED;
   const size_t es = elem_size(desc->dtype);
   OOMB_CHECK(check_tensor(q, p, p.Hq, es, &p.q));
   OOMB_CHECK(check_tensor(o, p, p.Hq, es, &p.q_out));
   if (!k_pool || !v_pool || !lse || !aligned16(k_pool) || !aligned16(v_pool)) return OOMB_ERR_INVALID_ARG;
-  if (sel_pages && (!sel_count || sel_stride < 0)) return OOMB_ERR_INVALID_ARG;
   p.k_pool = const_cast<void*>(k_pool); p.v_pool = const_cast<void*>(v_pool);
   p.sel = sel_pages; p.sel_count = sel_count; p.sel_stride = sel_stride;
   p.lse = lse;
-  const bool bf = desc->dtype == OOMB_BF16;
-  const int32_t width = sel_pages ? sel_stride : -1;
-  if (!grid_fits(kvq_attn_blocks(p, bf, width))) return OOMB_ERR_UNSUPPORTED;
   const size_t need = kvq_attn_workspace_bytes(p, bf, width);
   if (need && (!workspace || workspace_bytes < need || !aligned16(workspace))) return OOMB_ERR_WORKSPACE;
   return launched(launch_attn_kvq(p, bf, workspace, (hipStream_t)hip_stream));

@@ -638,6 +638,9 @@ Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   c.stream = heads * tokens * 2 * (p.D / 2 + p.D / 32) > (256ll << 20);
   return c;
 }
+// Rows that the combine has a workgroup for, and its workgroups (before slices, which only a few rows have); it runs where c.split.
+int combine_rows(const RowsParams& p, const Plan& c) { return c.row_blocks == 1 ? p.max_rows * p.G : 16 * c.rt; }
+int64_t combine_blocks(const RowsParams& p, const Plan& c) { return (int64_t)p.n_seqs * p.Hkv * c.row_blocks * combine_rows(p, c); }
 
 template <typename T, int D, int RT, int W, bool WIDE, bool STREAM> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
   AttnArgs a{c.row_blocks, c.split, c.target, c.min_units, nullptr, nullptr, nullptr};
@@ -661,8 +664,8 @@ template <typename T, int D, int RT, int W, bool WIDE, bool STREAM> hipError_t r
     if (e != hipSuccess || !c.split) return e;
   }
   ProfScope prof_("kvq_combine", st);
-  const int rows = c.row_blocks == 1 ? p.max_rows * p.G : 16 * RT;
-  const int64_t wgs = heads * c.row_blocks * rows;
+  const int rows = combine_rows(p, c);
+  const int64_t wgs = combine_blocks(p, c);
   if (wgs < 256 && c.parts > 32 * heads) kvq_combine_kernel<T, D, 32><<<dim3((unsigned)(wgs * (D / 32))), dim3(COMBINE_THREADS), 0, st>>>(p, a, 16 * RT, rows);
   else kvq_combine_kernel<T, D, D><<<dim3((unsigned)wgs), dim3(COMBINE_THREADS), 0, st>>>(p, a, 16 * RT, rows);
   return hipGetLastError();

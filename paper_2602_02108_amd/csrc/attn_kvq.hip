@@ -10,8 +10,8 @@ size_t kvq_attn_workspace_bytes(const RowsParams& p, bool is_bf16, int32_t sel_s
 }
 int64_t kvq_attn_blocks(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   const Plan c = plan_of(p, is_bf16, sel_stride);
-  const int64_t combine = (int64_t)p.n_seqs * p.Hkv * c.row_blocks * 16 * c.rt;
-  return c.parts * c.row_blocks * 2 > combine ? c.parts * c.row_blocks * 2 : combine;   // (workgroups of up to 512 threads)
+  const int64_t attn = c.parts * c.row_blocks * (c.waves / 4), combine = c.split ? combine_blocks(p, c) : 0;   // (in workgroups of 256 threads)
+  return attn > combine ? attn : combine;
 }
 
 hipError_t launch_attn_kvq(const RowsParams& p, bool is_bf16, void* ws, hipStream_t st) {

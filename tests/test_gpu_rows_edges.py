@@ -58,3 +58,23 @@ def test_lists_without_room_list_nothing(dt, spans, P):
         api.paged_attn_fwd_kvq(desc, gq, *gp, table, sel, cnt, o, lse, **at)
         assert (o[:b.rows] == 0).all() and (lse[:, :b.rows] == -math.inf).all()
         assert (o[b.rows:] == 5.0).all() and (lse[:, b.rows:] == 5.0).all()
+
+
+@pytest.mark.parametrize("dt,Hq,Hkv,D,P", [(BF, 8, 2, 64, 16), (F32, 8, 4, 128, 32)])
+def test_many_short_sequences_under_a_loose_bound(dt, Hq, Hkv, D, P):
+    """A thousand sequences of a few rows each, max_rows the rows of all."""
+    rng = np.random.default_rng(5)
+    spans = [(int(n), int(n + rng.integers(0, 40))) for n in rng.integers(0, 7, 1000)]
+    b, q, gq, pools, gp, table, at = _batch(spans, P, Hq, Hkv, D, dt, 43)
+    desc = api.make_rows_desc(gq, gp[0], table, b.max_len, 0.1)
+    assert desc.max_rows == b.n_rows and len(spans) * Hq * b.n_rows > 1 << 24
+    o, lse = api.paged_attn_fwd_kvq(desc, gq, *gp, table, **at)
+    _check(b, q, pools, 0.1, o, lse, 2.0 ** -22 if dt == F32 else 2.0 ** -16)
+    close = api.make_rows_desc(gq, gp[0], table, b.max_len, 0.1, max_rows=b.max_rows)
+    k, v = gq[:, :Hkv], gq[:, Hkv:2 * Hkv]
+    got = []
+    for d in (desc, close):
+        x = [t.clone() for t in gp]
+        y = api.kvq_append_rope(d, k, v, table, *x, q=gq, **at)
+        got.append([y, *x, *api.kvq_read(d, *x, table, **at)])
+    assert all(torch.equal(a, c) for a, c in zip(*got)) and not torch.equal(got[0][1], gp[0])
