@@ -23,7 +23,7 @@
 //
 // Measured (28 / 4 heads, D 128, P 128): one token against 1,048,001: 104 us, 5.5 TB/s of the cache, bound by memory; 2048 rows over 80
 // listed pages: 381 us, 0.71 PFLOP/s, bound by the vector unit (240 vector instructions for 48 matrix ones in a unit of two row tiles, 64 of them
-// conversions, 32 permutes, 16 exponentials, 40 for the second terms of the weights); 32 sequences of one to 32K tokens: 24 us.  Two row tiles a wave and not more: with four, one wave per SIMD
+// conversions, 32 permutes, 16 exponentials, 40 for the second terms of the weights); 32 sequences of one to 32K tokens: 22 us.  Two row tiles a wave and not more: with four, one wave per SIMD
 // is left and its instructions wait for each other (599 us), three spill.
 #pragma once
 #include <type_traits>
@@ -633,9 +633,12 @@ Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   c.target = (int)(target < 1 ? 1 : target);
   c.parts = !c.split ? heads : heads * each < target + heads ? heads * each : target + heads;
   c.waves = c.split || (is_bf16 && rows > 64) ? 4 : 8;   // (2048 rows over 80 pages: eight waves 404 us, four 346, both in one term)
-  // Codes past the caches once they would not stay in the last one (256 MiB) to the next call: 570 MB 117 -> 105 us, 62 MB 25.4 -> 26.2
-  // (bf16 rows of head dim 128, where both were timed; the other forms are without it).
-  c.stream = heads * tokens * 2 * (p.D / 2 + p.D / 32) > (256ll << 20);
+  // Codes past the caches once they would not stay in the last one (256 MiB) to the next call: 570 MB 117 -> 105 us, 62 MB 22.0 -> 23.6
+  // (bf16 rows of head dim 128, where both were timed; the other forms are without it).  What is read is bounded by the lengths' bound and by the
+  // pools: a batch whose bound alone is large (32 sequences of up to 32K tokens, 570 MB, that hold 62) goes by its pools, and one of short sequences
+  // in large pools under a large bound loses the 7 %.
+  const int64_t reach = heads * tokens, held = p.num_phys * p.Hkv * p.P;
+  c.stream = (reach < held ? reach : held) * 2 * (p.D / 2 + p.D / 32) > (256ll << 20);
   return c;
 }
 // Rows that the combine has a workgroup for, and its workgroups (before slices, which only a few rows have); it runs where c.split.

@@ -78,3 +78,20 @@ def test_many_short_sequences_under_a_loose_bound(dt, Hq, Hkv, D, P):
         y = api.kvq_append_rope(d, k, v, table, *x, q=gq, **at)
         got.append([y, *x, *api.kvq_read(d, *x, table, **at)])
     assert all(torch.equal(a, c) for a, c in zip(*got)) and not torch.equal(got[0][1], gp[0])
+
+
+def test_codes_past_the_caches_give_the_same_bits():
+    """A pool past the last cache's size under a bound to match is read past it: the same rows over a small pool, and over the large one."""
+    b, q, gq, pools, gp, table, at = _batch([(1, 900), (2, 5000), (0, 3), (1, 1)], 128, 8, 4, 128, BF, 44)
+    n_phys = 4000   # of 2 x 34 KiB
+    large = [torch.full((n_phys, *x.shape[1:]), 255, dtype=torch.uint8, device="cuda") for x in gp]
+    for x, y in zip(large, gp):
+        x[:b.n_phys] = y
+    assert 2 * large[0].numel() > 256 << 20
+    room = torch.cat([table, torch.full((4, 8192 - table.shape[1]), -1, dtype=torch.int32, device="cuda")], 1)
+    got = []
+    for x in (gp, large):
+        desc = api.make_rows_desc(gq, x[0], room, 1 << 20, 0.1, max_rows=2)
+        got.append(api.paged_attn_fwd_kvq(desc, gq, *x, room, **at))
+    assert all(torch.equal(a, c) for a, c in zip(*got))
+    _check(b, q, pools, 0.1, *got[0], 2.0 ** -16)
