@@ -706,10 +706,15 @@ def _rows_refused(where: str, desc: RowsDesc, rows, pools, page_tables, seq_lens
     return _refused(where)
 
 
-def _rows_like(q, heads, row_starts):
-    """A new row tensor; rows that belong to no sequence are written by no call and start at zero."""
-    make = torch.empty if row_starts is None else torch.zeros
-    return make((q.shape[0], heads, q.shape[2]), dtype=q.dtype, device=q.device)
+def _new_rows(desc, heads, device, every_row: bool):
+    """A new row tensor for a call that writes every row, or leaves some alone: those start at zero."""
+    make = torch.empty if every_row else torch.zeros
+    return make((desc.n_rows, heads, desc.head_dim), dtype=torch.bfloat16 if desc.dtype == BF16 else torch.float32, device=device)
+
+
+def _all_exist(desc, seq_lens, row_starts) -> bool:
+    """Whether every row is sure to be a token of a sequence.  With lengths on the device, a sequence may be shorter than its rows."""
+    return row_starts is None and seq_lens is None and desc.n_rows <= desc.n_seqs * desc.max_len
 
 
 def _rope(rope):
@@ -718,7 +723,7 @@ def _rope(rope):
 
 def _append_rope(where, native, pool_dtype, desc, k, v, page_tables, k_pool, v_pool, q, q_out, rope, kbar_cache, seq_lens, row_starts):
     if q is not None and q_out is None:
-        q_out = _rows_like(q, desc.n_q_heads, row_starts)
+        q_out = _new_rows(desc, desc.n_q_heads, q.device, _all_exist(desc, seq_lens, row_starts))
     st = native(desc, *_rope(rope), q, q_out, k, v, page_tables, seq_lens, row_starts, k_pool, v_pool, kbar_cache)
     if st < 0:
         rows = [("k", k, desc.n_kv_heads), ("v", v, desc.n_kv_heads)]
@@ -734,7 +739,7 @@ def _append_rope(where, native, pool_dtype, desc, k, v, page_tables, k_pool, v_p
 def kv_append_rope(desc: RowsDesc, k, v, page_tables, k_pool, v_pool, q=None, q_out=None, rope: Optional[Rope] = None, kbar_cache=None, seq_lens=None,
                    row_starts=None):
     """oomb_kv_append_rope: the rows' keys, rotated, and values into their pages (+ the means of the pages they fill into kbar_cache).
-    Returns q rotated (q_out, a new tensor unless given; None without q)."""
+    Returns q rotated (q_out, a new tensor unless given, zero where rows do not exist; None without q)."""
     return _append_rope("oomb_kv_append_rope", (_nb or _native()).kv_append_rope, torch.bfloat16 if desc.dtype == BF16 else torch.float32, desc, k, v,
                         page_tables, k_pool, v_pool, q, q_out, rope, kbar_cache, seq_lens, row_starts)
 
@@ -750,10 +755,8 @@ def kv_append_rope_bwd(desc: RowsDesc, dk_pool, dv_pool, page_tables, d_q=None, 
                        seq_lens=None, row_starts=None):
     """oomb_kv_append_rope_bwd: the gradients with respect to the rows that kv_append_rope took, from d_q (of its q_out) and the gradient pools
     (float32 or bfloat16; desc made with one of them as the pool).  Returns (d_q_out, d_k, d_v), d_q_out None without d_q."""
-    dt = torch.bfloat16 if desc.dtype == BF16 else torch.float32
-    make = torch.empty if row_starts is None else torch.zeros
     def new(heads):
-        return make((desc.n_rows, heads, desc.head_dim), dtype=dt, device=dk_pool.device)
+        return _new_rows(desc, heads, dk_pool.device, _all_exist(desc, seq_lens, row_starts))
     if d_q is not None and d_q_out is None:
         d_q_out = new(desc.n_q_heads)
     if d_k is None:
@@ -774,9 +777,7 @@ def kv_append_rope_bwd(desc: RowsDesc, dk_pool, dv_pool, page_tables, d_q=None, 
 
 def kvq_read(desc: RowsDesc, k_pool, v_pool, page_tables, k_out=None, v_out=None, seq_lens=None, row_starts=None):
     """oomb_kvq_read: the rows' values as a cache of 4-bit codes holds them.  Returns (k [n_rows][Hkv][D], v)."""
-    dt = torch.bfloat16 if desc.dtype == BF16 else torch.float32
-    make = torch.empty if row_starts is None else torch.zeros
-    k_out, v_out = (make((desc.n_rows, desc.n_kv_heads, desc.head_dim), dtype=dt, device=k_pool.device) if t is None else t for t in (k_out, v_out))
+    k_out, v_out = (_new_rows(desc, desc.n_kv_heads, k_pool.device, _all_exist(desc, seq_lens, row_starts)) if t is None else t for t in (k_out, v_out))
     st = (_nb or _native()).kvq_read(desc, page_tables, seq_lens, row_starts, k_pool, v_pool, k_out, v_out)
     if st < 0:
         raise _rows_refused("oomb_kvq_read", desc, [("k_out", k_out, desc.n_kv_heads), ("v_out", v_out, desc.n_kv_heads)],
@@ -796,7 +797,7 @@ def paged_attn_fwd_kvq(desc: RowsDesc, q, k_pool, v_pool, page_tables, sel_pages
     """oomb_paged_attn_fwd_kvq: attention of the rows over a cache of 4-bit codes, every page or lists [n_seqs][Hkv][stride] ([Hkv][stride] for
     one sequence).  Returns (O [n_rows][Hq][D], LSE [Hq][n_rows] float32)."""
     if o is None:
-        o = _rows_like(q, desc.n_q_heads, row_starts)
+        o = _new_rows(desc, desc.n_q_heads, q.device, row_starts is None)   # (a row that does not exist gets zeros from the call)
     if lse is None:
         lse = (torch.empty if row_starts is None else torch.zeros)((desc.n_q_heads, desc.n_rows), dtype=torch.float32, device=q.device)
     if workspace is None:

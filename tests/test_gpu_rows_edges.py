@@ -80,6 +80,42 @@ def test_many_short_sequences_under_a_loose_bound(dt, Hq, Hkv, D, P):
     assert all(torch.equal(a, c) for a, c in zip(*got)) and not torch.equal(got[0][1], gp[0])
 
 
+def _garbage(*tensors):
+    """The memory that the allocator gives next to tensors of these shapes holds NaN."""
+    held = [torch.full_like(t, math.nan) for t in tensors for _ in range(3)]
+    torch.cuda.synchronize()
+    del held
+
+
+@pytest.mark.parametrize("lens", [True, False], ids=["lengths", "bound-alone"])
+def test_new_tensors_hold_zeros_where_rows_do_not_exist(lens):
+    """Equal rows, some sequences shorter than theirs: the surplus in front is written by no call, and is zero in a new tensor."""
+    P, D, Hq, Hkv, n = 16, 64, 4, 2, 6
+    b = ru.Batch([(n, 4), (n, 4), (n, 4)] if not lens else [(n, 20), (n, 4), (n, 0)], P, 3, behind=0)
+    gen = torch.Generator().manual_seed(1)
+    q, k, v = (torch.randn((3 * n, h, D), generator=gen).cuda() for h in (Hq, Hkv, Hkv))
+    at = b.device()
+    table, seq_lens = at["page_tables"], at["seq_lens"] if lens else None
+    live = torch.zeros(3 * n, dtype=torch.bool)
+    live[[r for r, _, _ in b.each_row()]] = True
+    plain = [torch.randn((b.n_phys, Hkv, P, D), generator=gen).cuda() for _ in range(2)]
+    codes = [api.kvq_pool(b.n_phys, Hkv, P, D) for _ in range(2)]
+    desc = api.make_rows_desc(q, plain[0], table, b.max_len, max_rows=n)
+    kvq = api.make_rows_desc(q, codes[0], table, b.max_len, max_rows=n)
+    calls = [lambda: [api.kv_append_rope(desc, k, v, table, *plain, q=q, seq_lens=seq_lens)],
+             lambda: [api.kvq_append_rope(kvq, k, v, table, *codes, q=q, seq_lens=seq_lens)],
+             lambda: api.kv_append_rope_bwd(desc, *plain, table, d_q=q, seq_lens=seq_lens),
+             lambda: api.kvq_read(kvq, *codes, table, seq_lens=seq_lens)]
+    for call in calls:
+        _garbage(q, k)
+        for t in call():
+            t = t.cpu()
+            assert (t[~live] == 0).all() and (t[live] != 0).any(-1).all()
+    _garbage(q, torch.empty(Hq, 3 * n, device="cuda"))
+    o, lse = api.paged_attn_fwd_kvq(kvq, q, *codes, table, seq_lens=seq_lens)
+    assert (o.cpu()[~live] == 0).all() and (lse.cpu()[:, ~live] == -math.inf).all() and lse.cpu()[:, live].isfinite().all()
+
+
 def test_codes_past_the_caches_give_the_same_bits():
     """A pool past the last cache's size under a bound to match is read past it: the same rows over a small pool, and over the large one."""
     b, q, gq, pools, gp, table, at = _batch([(1, 900), (2, 5000), (0, 3), (1, 1)], 128, 8, 4, 128, BF, 44)
