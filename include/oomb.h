@@ -483,7 +483,8 @@ oomb_status oomb_kv_append_rope_bwd(const oomb_rows_desc* desc, const oomb_seqs*
  *            A count is cut to 0 .. sel_stride; sel_stride 0 lists nothing
  * A row that sees no token gets O = 0 and LSE = -infinity.  A value that is not finite reaches the rows that see its token, and no
  * other.  bf16 rows: weights in two bf16 terms (2^-16 of a weight), whatever
- * else is in the call; fp32 rows: products in three bf16 terms per value (the cache's values are exact in one).  Sums in fp32.
+ * else is in the call; fp32 rows: products in three bf16 terms per value (the cache's values are exact in one).  Sums in fp32:
+ * a logit below a float's range has no weight, one above it makes its row NaN, and an output may overflow where values of V pass 2^128 / (64 T), T the tokens seen.
  * Results do not depend on scheduling.  Workspace: oomb_kvq_workspace_bytes(desc, sel_stride), sel_stride < 0 for every page (with
  * less than that, OOMB_ERR_WORKSPACE; it may be 0); calls that overlap in time need workspaces of their own.
  */

@@ -357,22 +357,22 @@ __global__ __launch_bounds__(64 * W, RT == 1 && W == 4 && sizeof(T) == 2 ? 3 : 2
     }
 
     float z[RT][8], all[RT];
-    auto weights = [&](int rt) __attribute__((always_inline)) {
+    auto weights = [&](int rt, float from) __attribute__((always_inline)) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) z[rt][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[rt][e >> 2][e & 3], scale, -ref[rt]));
+      for (int e = 0; e < 8; ++e) z[rt][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[rt][e >> 2][e & 3], scale, -from));
       if (masked) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) z[rt][e] = t0[e >> 2] + 4 * kg + (e & 3) <= pos[rt] ? z[rt][e] : 0.0f;
       }
       all[rt] = ((z[rt][0] + z[rt][1]) + (z[rt][2] + z[rt][3])) + ((z[rt][4] + z[rt][5]) + (z[rt][6] + z[rt][7]));
     };
-    float most = 0.0f;
+    bool up = false;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      weights(rt);
-      most = fmaxf(most, all[rt]);
+      weights(rt, ref[rt]);
+      up |= !(all[rt] <= MOST);
     }
-    if (__any(most > MOST)) {   // (the first unit of a row: its reference is -infinity)
+    if (__any(up)) {   // (the first unit of a row: its reference is -infinity, so weights are infinite, or NaN where the logit is -infinity too)
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         float top = -INFINITY;
@@ -389,7 +389,7 @@ __global__ __launch_bounds__(64 * W, RT == 1 && W == 4 && sizeof(T) == 2 ? 3 : 2
         sum[rt] *= f;
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[rt][j] *= f;
-        weights(rt);
+        weights(rt, to == -INFINITY ? 0.0f : to);   // (all that was seen may be -infinity: no weight)
       }
     }
     uint4 pf[RT][PT];

@@ -116,6 +116,42 @@ def test_new_tensors_hold_zeros_where_rows_do_not_exist(lens):
     assert (o.cpu()[~live] == 0).all() and (lse.cpu()[:, ~live] == -math.inf).all() and lse.cpu()[:, live].isfinite().all()
 
 
+@pytest.mark.parametrize("dt,n,t,Hq,Hkv,D,P", [(BF, 1, 60, 2, 2, 64, 16), (F32, 3, 60, 2, 1, 128, 16), (BF, 40, 90, 4, 2, 128, 32), (F32, 1, 3000, 1, 1, 64, 128)])
+def test_logits_below_a_floats_range_have_no_weight(dt, n, t, Hq, Hkv, D, P):
+    """Every second token's logits are about -2^140, minus infinity in fp32: their weight is zero as it is in 64 bits."""
+    b = ru.Batch([(n, t)], P, 6, behind=0)
+    q = torch.randn((b.n_rows, Hq, D), generator=torch.Generator().manual_seed(2)).to(dt)
+    q[..., 0] = 2.0 ** 60
+    pools = [ru.random_pool(b, Hkv, D, s) for s in (51, 52)]
+    for l in range(b.cols):
+        page = b.tables[0, l]
+        x = ru.values(*ru.unpack(pools[0][page], P, D))
+        low = (l * P + np.arange(P)) % 2 == 0
+        x[:, low, 0], x[:, ~low, :32] = -2.0 ** 80, 0.0
+        code, byte = ru.quantise(np.nan_to_num(x))
+        pools[0][page] = ru.pack(code, byte)
+    at = b.device()
+    table, gp, gq = at.pop("page_tables"), [torch.tensor(x, device="cuda") for x in pools], q.cuda()
+    desc = api.make_rows_desc(gq, gp[0], table, t, 0.125)
+    o, lse = api.paged_attn_fwd_kvq(desc, gq, *gp, table, **at)
+    # the seen logits as the definition has them: those of the other tokens, whose first block is zero
+    keep = q.clone()
+    keep[..., :32] = 0.0
+    x, seen = keep.double().numpy(), np.arange(t) % 2 == 1
+    for h in range(Hq):
+        g = h // (Hq // Hkv)
+        k, v = ru.sequence_values(b, pools[0], 0, g, D), ru.sequence_values(b, pools[1], 0, g, D)
+        s = 0.125 * (x[:, h] @ k.T)
+        s = np.where(seen & (np.arange(t) <= (t - n + np.arange(n))[:, None]), s, -np.inf)
+        want = np.log(np.exp(s).sum(-1))
+        p = np.exp(s - want[:, None])
+        got, glse = o[:, h].cpu().double().numpy(), lse[h].cpu().double().numpy()
+        # logits: D exact products summed in fp32 and three roundings; twice that and two terms of the weights; half a step of the output
+        off = (D + 3) * 2.0 ** -24 * 0.125 * (np.abs(x[:, h]) @ np.abs(k).T)[:, seen].max() + t * 2.0 ** -24
+        tol = (p @ np.abs(v)) * (2.0 ** -16 + 2 * off) + ru.HALF[dt] * np.abs(p @ v)
+        assert (np.abs(got - p @ v) <= tol).all() and (np.abs(glse - want) <= off + 2.0 ** -20).all()
+
+
 def test_codes_past_the_caches_give_the_same_bits():
     """A pool past the last cache's size under a bound to match is read past it: the same rows over a small pool, and over the large one."""
     b, q, gq, pools, gp, table, at = _batch([(1, 900), (2, 5000), (0, 3), (1, 1)], 128, 8, 4, 128, BF, 44)
