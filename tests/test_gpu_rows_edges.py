@@ -152,6 +152,68 @@ def test_logits_below_a_floats_range_have_no_weight(dt, n, t, Hq, Hkv, D, P):
         assert (np.abs(got - p @ v) <= tol).all() and (np.abs(glse - want) <= off + 2.0 ** -20).all()
 
 
+def _written(b, P, D, last=None, most=None):
+    """Which bytes of a [n_phys][...][tile] pool the rows of a batch take: codes and scales of their tokens."""
+    mask = np.zeros((b.n_phys, P * (D // 2 + D // 32)), bool)
+    for r, s, pos in b.each_row():
+        if pos >= (last or 1 << 40) or r - b.starts[s] >= (most or 1 << 40) or not 0 <= b.tables[s, pos // P] < b.n_phys:
+            continue
+        at = pos % P
+        mask[b.tables[s, pos // P], at * (D // 2):(at + 1) * (D // 2)] = True
+        mask[b.tables[s, pos // P], P * (D // 2) + at::P] = True
+    return mask
+
+
+@pytest.mark.parametrize("dt,Hq,Hkv,D,P,spans", [
+    (BF, 28, 4, 128, 128, [(1, 1), (1, 128), (1, 129), (1, 300), (0, 77), (0, 0)]), (BF, 4, 2, 128, 32, [(64, 64), (95, 700)]),
+    (F32, 2, 1, 64, 16, [(40, 43), (16, 32), (0, 5), (7, 7)]), (BF, 14, 2, 64, 16, [(33, 100), (1, 16), (17, 17), (5, 37)]),
+    (F32, 2, 2, 128, 64, [(10, 6), (3, 65)]),
+])
+@pytest.mark.parametrize("means", [False, True])
+def test_a_quantised_append_leaves_every_other_byte(dt, Hq, Hkv, D, P, spans, means):
+    b = ru.Batch(spans, P, 8)
+    rng = np.random.default_rng(9)
+    before = [rng.integers(0, 256, (b.n_phys, Hkv, P * (D // 2 + D // 32)), dtype=np.uint8) for _ in range(2)]
+    pools = [torch.tensor(x, device="cuda") for x in before]
+    k, v = (torch.randn((b.n_rows, Hkv, D), generator=torch.Generator().manual_seed(s)).to(dt) for s in (1, 2))
+    at = b.device()
+    table = at.pop("page_tables")
+    desc = api.make_rows_desc(k.cuda(), pools[0], table, b.max_len, max_rows=b.max_rows)
+    kbar = torch.zeros((len(spans), b.cols, Hkv, D), device="cuda") if means else None
+    api.kvq_append_rope(desc, k.cuda(), v.cuda(), table, *pools, kbar_cache=kbar, **at)
+    mask = _written(b, P, D)[:, None]
+    want = [x.copy() for x in before]
+    for r, s, pos in b.each_row():
+        for w, x in zip(want, (k, v)):
+            codes, scales = ru.unpack(w[b.tables[s, pos // P]], P, D)
+            codes[:, pos % P], scales[:, pos % P] = ru.quantise(x[r].double().numpy())
+            w[b.tables[s, pos // P]] = ru.pack(codes, scales)
+    for name, got, w, old in zip("KV", pools, want, before):
+        got = got.cpu().numpy()
+        assert np.array_equal(np.where(mask, 0, got), np.where(mask, 0, old)), f"{name}: bytes of no row were written"
+        # (N(0, 1) values, none of them zero or infinite: the codes that a search finds, to the sign)
+        assert np.array_equal(got, w), f"{name}: {int((got != w).sum())} bytes differ"
+
+
+def test_bytes_of_rows_that_do_not_exist_stay():
+    """Rows in front of the first token, past max_rows, past max_len and of pages that the pool does not have."""
+    P, D = 16, 64
+    b = ru.Batch([(10, 6), (20, 40), (4, 300)], P, 2)
+    b.tables[1, 2] = b.n_phys
+    at = b.device()
+    table = at.pop("page_tables")
+    k, v = (torch.randn((b.n_rows, 1, D), generator=torch.Generator().manual_seed(s)).cuda() for s in (1, 2))
+    before = torch.randint(0, 256, (b.n_phys, 1, api.kvq_tile_bytes(P, D)), generator=torch.Generator().manual_seed(3), dtype=torch.uint8)
+    pools = [before.cuda() for _ in range(2)]
+    desc = api.make_rows_desc(k, pools[0], table, 48, max_rows=18)
+    api.kvq_append_rope(desc, k, v, table, *pools, **at)
+    b.spans = [(n, min(t, 48)) for n, t in b.spans]
+    mask = _written(b, P, D, 48, 18)[:, None]
+    assert mask.any()
+    for got in pools:
+        assert np.array_equal(np.where(mask, 0, got.cpu().numpy()), np.where(mask, 0, before.numpy()))
+
+
 def test_codes_past_the_caches_give_the_same_bits():
     """A pool past the last cache's size under a bound to match is read past it: the same rows over a small pool, and over the large one."""
     b, q, gq, pools, gp, table, at = _batch([(1, 900), (2, 5000), (0, 3), (1, 1)], 128, 8, 4, 128, BF, 44)
