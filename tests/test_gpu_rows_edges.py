@@ -229,3 +229,23 @@ def test_codes_past_the_caches_give_the_same_bits():
         got.append(api.paged_attn_fwd_kvq(desc, gq, *x, room, **at))
     assert all(torch.equal(a, c) for a, c in zip(*got))
     _check(b, q, pools, 0.1, *got[0], 2.0 ** -16)
+
+
+@pytest.mark.parametrize("dt,Hq,Hkv,D,P,spans", [
+    (BF, 14, 2, 128, 128, [(1, 9000), (300, 1000), (4, 5000), (0, 70), (1, 1)]), (F32, 4, 2, 64, 16, [(200, 200), (1, 7000), (1, 3)]),
+    (BF, 4, 1, 64, 32, [(17, 20000), (130, 131)]),
+])
+def test_prompts_beside_long_single_tokens(dt, Hq, Hkv, D, P, spans):
+    """One call with a prompt, drafted and single tokens over long caches: each as the definition has it, and the single ones as alone."""
+    b, q, gq, pools, gp, table, at = _batch(spans, P, Hq, Hkv, D, dt, 45)
+    desc = api.make_rows_desc(gq, gp[0], table, b.max_len, 0.1, max_rows=b.max_rows)
+    o, lse = api.paged_attn_fwd_kvq(desc, gq, *gp, table, **at)
+    terms = 2.0 ** -22 if dt == F32 else 2.0 ** -16
+    _check(b, q, pools, 0.1, o, lse, terms)
+    for s, (n, t) in enumerate(spans):
+        if 0 < n < 20:
+            r = slice(b.starts[s], b.starts[s] + n)
+            one = api.make_rows_desc(gq[r], gp[0], table[s], t, 0.1)
+            o1, l1 = o.clone(), lse.clone()
+            o1[r], l1[:, r] = api.paged_attn_fwd_kvq(one, gq[r], *gp, table[s])
+            _check(b, q, pools, 0.1, o1, l1, terms)
