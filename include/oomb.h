@@ -395,6 +395,8 @@ oomb_status oomb_check_inputs(const oomb_attn_desc* desc, const int32_t* page_ta
  * Rows beyond max_rows are left out, and lengths are cut to max_len.  A row of a
  * sequence shorter than its rows (a position below 0) does not exist: the appends and their backward leave it alone, for attention it sees nothing.  A physical page outside [0, num_phys_pages)
  * holds nothing: rows are not written there (their gradients and read values are 0) and attention does not see it.
+ * Pools of bf16 / fp32 are read by oomb_paged_attn_fwd and its backward, whole pages of one sequence at a time; 4-bit pools by
+ * oomb_paged_attn_fwd_kvq, any rows at any length.
  */
 typedef struct {
   int32_t n_q_heads, n_kv_heads; /* Hq, Hkv; Hkv divides Hq */

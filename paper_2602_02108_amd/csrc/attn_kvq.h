@@ -21,7 +21,7 @@
 // The waves of a workgroup share a row block and split its tokens; long caches are cut into parts of equal work over workgroups, counted on the
 // device from the lengths as they are, and kvq_combine adds a row's parts in their order.
 //
-// Measured (28 / 4 heads, D 128, P 128): one token against 1,048,001: 104 us, 5.5 TB/s of the cache, bound by memory; 2048 rows over 80
+// Measured (28 / 4 heads, D 128, P 128): one token against 1,048,001: 103 us, 5.5 TB/s of the cache, bound by memory; 2048 rows over 80
 // listed pages: 381 us, 0.71 PFLOP/s, bound by the vector unit (240 vector instructions for 48 matrix ones in a unit of two row tiles, 64 of them
 // conversions, 32 permutes, 16 exponentials, 40 for the second terms of the weights); 32 sequences of one to 32K tokens: 22 us.  Two row tiles a wave and not more: with four, one wave per SIMD
 // is left and its instructions wait for each other (599 us), three spill.
@@ -632,7 +632,7 @@ Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   c.split = units > 40 && each > 1 && target >= 2 * heads;
   c.target = (int)(target < 1 ? 1 : target);
   c.parts = !c.split ? heads : heads * each < target + heads ? heads * each : target + heads;
-  c.waves = c.split || (is_bf16 && rows > 64) ? 4 : 8;   // (2048 rows over 80 pages: eight waves 404 us, four 346, both in one term)
+  c.waves = c.split || (is_bf16 && rows > 64) ? 4 : 8;   // (4096 rows over 16K tokens: eight waves 1270 us, four 1176; 64 rows of 7 heads: 39.8, 41.0)
   // Codes past the caches once they would not stay in the last one (256 MiB) to the next call: 570 MB 117 -> 105 us, 62 MB 22.0 -> 23.6
   // (bf16 rows of head dim 128, where both were timed; the other forms are without it).  What is read is bounded by the lengths' bound and by the
   // pools: a batch whose bound alone is large (32 sequences of up to 32K tokens, 570 MB, that hold 62) goes by its pools, and one of short sequences
