@@ -610,6 +610,7 @@ def local_page_list(desc: AttnDesc, window_pages: int, device, sel_pages=None, s
 
 
 # ---- packed rows of any number of sequences: rotation and append, their backward, a cache held in 4 bits (include/oomb.h) ----
+# (row tensors that a call makes itself are zero where it writes nothing: rows of no sequence, or in front of its first token)
 
 class Rope:
     """Tables of a position rotation: cos, sin [positions][rot_dim / 2] float32; pairs in halves, or neighbours."""
@@ -718,7 +719,7 @@ def _all_exist(desc, seq_lens, row_starts) -> bool:
 
 
 def _rope(rope):
-    return (None, None, False) if rope is None else (rope.cos, rope.sin, rope.interleaved)
+    return (None, None, False) if rope is None else (rope.cos, rope.sin, bool(rope.interleaved))
 
 
 def _append_rope(where, native, pool_dtype, desc, k, v, page_tables, k_pool, v_pool, q, q_out, rope, kbar_cache, seq_lens, row_starts):

@@ -249,3 +249,20 @@ def test_prompts_beside_long_single_tokens(dt, Hq, Hkv, D, P, spans):
             o1, l1 = o.clone(), lse.clone()
             o1[r], l1[:, r] = api.paged_attn_fwd_kvq(one, gq[r], *gp, table[s])
             _check(b, q, pools, 0.1, o1, l1, terms)
+
+
+@pytest.mark.parametrize("flag", [1, np.bool_(True)])
+def test_pairs_of_a_rope_are_neighbours_by_any_truth_value(flag):
+    b = ru.Batch([(5, 9)], 16, 1, behind=0)
+    x = torch.randn((5, 2, 64), generator=torch.Generator().manual_seed(1)).cuda()
+    cos, sin = (t.cuda() for t in ru.tables(9, 64))
+    pools = [torch.zeros((b.n_phys, 2, 16, 64), device="cuda") for _ in range(2)]
+    at = b.device()
+    table = at.pop("page_tables")
+    desc = api.make_rows_desc(x, pools[0], table, 9)
+    rope = api.Rope(cos, sin)
+    halves = api.kv_append_rope(desc, x, x, table, *pools, q=x, rope=rope, **at)
+    rope.interleaved = flag
+    got = api.kv_append_rope(desc, x, x, table, *pools, q=x, rope=rope, **at)
+    want = api.kv_append_rope(desc, x, x, table, *pools, q=x, rope=api.Rope(cos, sin, True), **at)
+    assert torch.equal(got, want) and not torch.equal(got, halves)
