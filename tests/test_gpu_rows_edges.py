@@ -266,3 +266,19 @@ def test_pairs_of_a_rope_are_neighbours_by_any_truth_value(flag):
     got = api.kv_append_rope(desc, x, x, table, *pools, q=x, rope=rope, **at)
     want = api.kv_append_rope(desc, x, x, table, *pools, q=x, rope=api.Rope(cos, sin, True), **at)
     assert torch.equal(got, want) and not torch.equal(got, halves)
+
+
+@pytest.mark.parametrize("dt,spans,Hq,Hkv,D,P", [(BF, [(6, 40), (1, 20)], 4, 2, 128, 16), (BF, [(30, 40), (9, 200)], 14, 2, 64, 32), (BF, [(70, 150)], 3, 3, 128, 64),
+                                                 (F32, [(20, 90), (2, 300)], 4, 1, 128, 16)])
+def test_nan_blocks_leave_the_other_rows_their_bits(dt, spans, Hq, Hkv, D, P):
+    """NaN blocks of K and V near the end of each sequence: the rows that see them are NaN where they should be, the others as exact as ever."""
+    b, q, gq, pools, gp, table, at = _batch(spans, P, Hq, Hkv, D, dt, 46)
+    for s, (n, t) in enumerate(spans):
+        for pool, back, g, block in ((pools[1], n // 2 + 1, 0, D // 32 - 1), (pools[1], 1, Hkv - 1, 0), (pools[0], 2, Hkv - 1, 1)):
+            pos = max(t - back, 0)
+            pool[b.tables[s, pos // P], g, P * D // 2 + block * P + pos % P] = 255
+            gp[0 if pool is pools[0] else 1].copy_(torch.tensor(pool))
+    desc = api.make_rows_desc(gq, gp[0], table, b.max_len, 0.1, max_rows=b.max_rows)
+    o, lse = api.paged_attn_fwd_kvq(desc, gq, *gp, table, **at)
+    _check(b, q, pools, 0.1, o, lse, 2.0 ** -22 if dt == F32 else 2.0 ** -16)
+    assert o[:b.rows].isnan().any() and o[:b.rows].isfinite().any()
