@@ -395,8 +395,8 @@ oomb_status oomb_check_inputs(const oomb_attn_desc* desc, const int32_t* page_ta
  * Rows beyond max_rows are left out, and lengths are cut to max_len.  A row of a
  * sequence shorter than its rows (a position below 0) does not exist: the appends and their backward leave it alone, for attention it sees nothing.  A physical page outside [0, num_phys_pages)
  * holds nothing: rows are not written there (their gradients and read values are 0) and attention does not see it.
- * Pools of bf16 / fp32 are read by oomb_paged_attn_fwd and its backward, whole pages of one sequence at a time; 4-bit pools by
- * oomb_paged_attn_fwd_kvq, any rows at any length.
+ * Pools of bf16 / fp32 are read by oomb_paged_attn_fwd_rows, any rows at any length, and by oomb_paged_attn_fwd and its backward, whole pages of one
+ * sequence at a time; 4-bit pools by oomb_paged_attn_fwd_kvq, any rows at any length.
  */
 typedef struct {
   int32_t n_q_heads, n_kv_heads; /* Hq, Hkv; Hkv divides Hq */
@@ -499,6 +499,18 @@ size_t oomb_kvq_workspace_bytes(const oomb_rows_desc* desc, int32_t sel_stride);
 oomb_status oomb_paged_attn_fwd_kvq(const oomb_rows_desc* desc, const oomb_seqs* seqs, const oomb_rows* q, const void* k_pool,
                                     const void* v_pool, const int32_t* sel_pages, const int32_t* sel_count, int32_t sel_stride,
                                     const oomb_rows* o, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * oomb_paged_attn_fwd_rows: attention of the rows over pools [n_phys][Hkv][P][D] of their type (the pools that oomb_kv_append_rope
+ * fills), as oomb_paged_attn_fwd_kvq over its own: the same rows, lists, outputs and empty rows.  A page of one KV head spans less than 2 GiB.  bf16 rows:
+ * weights in two bf16 terms (2^-16 of a weight); fp32 rows: products in fp32.  Sums in fp32.  What is not seen may hold anything.  Of what is seen, a NaN in K makes
+ * its rows NaN; an infinity or a NaN in V makes that dim of its rows infinite or NaN, and of no other.
+ * Results do not depend on scheduling.  Workspace: oomb_rows_workspace_bytes(desc, sel_stride), as above.
+ */
+size_t oomb_rows_workspace_bytes(const oomb_rows_desc* desc, int32_t sel_stride);
+oomb_status oomb_paged_attn_fwd_rows(const oomb_rows_desc* desc, const oomb_seqs* seqs, const oomb_rows* q, const void* k_pool,
+                                     const void* v_pool, const int32_t* sel_pages, const int32_t* sel_count, int32_t sel_stride,
+                                     const oomb_rows* o, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 const char* oomb_status_string(int32_t status);
 

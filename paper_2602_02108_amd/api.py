@@ -30,7 +30,8 @@ EXPORTS = ["oomb_workspace_bytes", "oomb_page_score_topk", "oomb_paged_attn_fwd"
            "oomb_paged_attn_fwd_qp", "oomb_paged_attn_bwd_qp", "oomb_page_vote_topk",
            "oomb_offload_plan", "oomb_offload_fetch", "oomb_offload_writeback", "oomb_check_inputs",
            "oomb_page_score_topk_noalloc", "oomb_kv_append_rope", "oomb_kv_append_rope_bwd",
-           "oomb_kvq_append_rope", "oomb_kvq_read", "oomb_kvq_workspace_bytes", "oomb_paged_attn_fwd_kvq"]
+           "oomb_kvq_append_rope", "oomb_kvq_read", "oomb_kvq_workspace_bytes", "oomb_paged_attn_fwd_kvq",
+           "oomb_rows_workspace_bytes", "oomb_paged_attn_fwd_rows"]
 
 
 class AttnDesc(ctypes.Structure):
@@ -150,6 +151,10 @@ def lib():
         l.oomb_kvq_workspace_bytes.argtypes = [rd, i32]
         l.oomb_paged_attn_fwd_kvq.restype = i32
         l.oomb_paged_attn_fwd_kvq.argtypes = [rd, sq, rw, vp, vp, vp, vp, i32, rw, vp, vp, u64, vp]
+        l.oomb_rows_workspace_bytes.restype = u64
+        l.oomb_rows_workspace_bytes.argtypes = [rd, i32]
+        l.oomb_paged_attn_fwd_rows.restype = i32
+        l.oomb_paged_attn_fwd_rows.argtypes = l.oomb_paged_attn_fwd_kvq.argtypes
         _lib = l
     return _lib
 
@@ -793,20 +798,22 @@ def kvq_workspace_bytes(desc: RowsDesc, sel_stride: int = -1) -> int:
     return int(lib().oomb_kvq_workspace_bytes(ctypes.byref(desc), int(sel_stride)))
 
 
-def paged_attn_fwd_kvq(desc: RowsDesc, q, k_pool, v_pool, page_tables, sel_pages=None, sel_count=None, o=None, lse=None, workspace=None, seq_lens=None,
-                       row_starts=None):
-    """oomb_paged_attn_fwd_kvq: attention of the rows over a cache of 4-bit codes, every page or lists [n_seqs][Hkv][stride] ([Hkv][stride] for
-    one sequence).  Returns (O [n_rows][Hq][D], LSE [Hq][n_rows] float32)."""
+def rows_workspace_bytes(desc: RowsDesc, sel_stride: int = -1) -> int:
+    """oomb_rows_workspace_bytes: what paged_attn_fwd_rows needs with lists of this row stride (-1: every page); may be 0."""
+    return int(lib().oomb_rows_workspace_bytes(ctypes.byref(desc), int(sel_stride)))
+
+
+def _attn_fwd_packed(where, native, workspace_bytes, pool_dtype, desc, q, k_pool, v_pool, page_tables, sel_pages, sel_count, o, lse, workspace, seq_lens,
+                     row_starts):
     if o is None:
         o = _new_rows(desc, desc.n_q_heads, q.device, row_starts is None)   # (a row that does not exist gets zeros from the call)
     if lse is None:
         lse = (torch.empty if row_starts is None else torch.zeros)((desc.n_q_heads, desc.n_rows), dtype=torch.float32, device=q.device)
     if workspace is None:
-        need = kvq_workspace_bytes(desc, -1 if sel_pages is None else int(sel_pages.shape[-1]))
+        need = workspace_bytes(desc, -1 if sel_pages is None else int(sel_pages.shape[-1]))
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    st = (_nb or _native()).attn_fwd_kvq(desc, q, k_pool, v_pool, page_tables, seq_lens, row_starts, sel_pages, sel_count, o, lse, workspace)
+    st = native(desc, q, k_pool, v_pool, page_tables, seq_lens, row_starts, sel_pages, sel_count, o, lse, workspace)
     if st < 0:
-        where = "oomb_paged_attn_fwd_kvq"
         lists = desc.n_seqs * desc.n_kv_heads
         if lse.dtype != torch.float32 or tuple(lse.shape) != (desc.n_q_heads, desc.n_rows) or not lse.is_contiguous():
             raise OombError(ERR_INVALID_ARG, f"{where}: lse must be contiguous float32 [{desc.n_q_heads}][{desc.n_rows}]")
@@ -815,8 +822,24 @@ def paged_attn_fwd_kvq(desc: RowsDesc, q, k_pool, v_pool, page_tables, sel_pages
                                       sel_pages.numel() != lists * sel_pages.shape[-1]):
             raise OombError(ERR_INVALID_ARG, f"{where}: sel_pages must be contiguous int32 [n_seqs][Hkv][stride], sel_count [n_seqs][Hkv]")
         raise _rows_refused(where, desc, [("q", q, desc.n_q_heads), ("o", o, desc.n_q_heads)],
-                            [("k_pool", k_pool, torch.uint8), ("v_pool", v_pool, torch.uint8)], page_tables, seq_lens, row_starts,
+                            [("k_pool", k_pool, pool_dtype), ("v_pool", v_pool, pool_dtype)], page_tables, seq_lens, row_starts,
                             others=[("sel_pages", sel_pages), ("sel_count", sel_count), ("lse", lse), ("workspace", workspace)])
     if st != OK:
-        raise OombError(st, "oomb_paged_attn_fwd_kvq")
+        raise OombError(st, where)
     return o, lse
+
+
+def paged_attn_fwd_kvq(desc: RowsDesc, q, k_pool, v_pool, page_tables, sel_pages=None, sel_count=None, o=None, lse=None, workspace=None, seq_lens=None,
+                       row_starts=None):
+    """oomb_paged_attn_fwd_kvq: attention of the rows over a cache of 4-bit codes, every page or lists [n_seqs][Hkv][stride] ([Hkv][stride] for
+    one sequence).  Returns (O [n_rows][Hq][D], LSE [Hq][n_rows] float32)."""
+    return _attn_fwd_packed("oomb_paged_attn_fwd_kvq", (_nb or _native()).attn_fwd_kvq, kvq_workspace_bytes, torch.uint8, desc, q, k_pool, v_pool, page_tables,
+                            sel_pages, sel_count, o, lse, workspace, seq_lens, row_starts)
+
+
+def paged_attn_fwd_rows(desc: RowsDesc, q, k_pool, v_pool, page_tables, sel_pages=None, sel_count=None, o=None, lse=None, workspace=None, seq_lens=None,
+                        row_starts=None):
+    """oomb_paged_attn_fwd_rows: paged_attn_fwd_kvq over pools [n_phys][Hkv][P][D] of the rows' type."""
+    return _attn_fwd_packed("oomb_paged_attn_fwd_rows", (_nb or _native()).attn_fwd_rows, rows_workspace_bytes,
+                            torch.bfloat16 if desc.dtype == BF16 else torch.float32, desc, q, k_pool, v_pool, page_tables, sel_pages, sel_count, o, lse,
+                            workspace, seq_lens, row_starts)

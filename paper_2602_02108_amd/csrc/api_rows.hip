@@ -96,6 +96,31 @@ oomb_status append_rope(const oomb_rows_desc* desc, const oomb_seqs* seqs, const
   return launched(launch_append_rope(p, desc->dtype == OOMB_BF16, kvq, (hipStream_t)hip_stream));
 }
 
+template <bool KVQ_POOLS>
+oomb_status attn_fwd(const oomb_rows_desc* desc, const oomb_seqs* seqs, const oomb_rows* q, const void* k_pool, const void* v_pool,
+                     const int32_t* sel_pages, const int32_t* sel_count, int32_t sel_stride, const oomb_rows* o, float* lse, void* workspace,
+                     size_t workspace_bytes, void* hip_stream) {
+  RowsParams p{};
+  OOMB_CHECK(check_rows(desc, KVQ_POOLS ? KVQ : SAME, &p));
+  if (!(desc->sm_scale > 0.f) || !std::isfinite(desc->sm_scale)) return OOMB_ERR_INVALID_ARG;
+  OOMB_CHECK(check_seqs(seqs, &p));
+  if (sel_pages && (!sel_count || sel_stride < 0)) return OOMB_ERR_INVALID_ARG;
+  const bool bf = desc->dtype == OOMB_BF16;
+  const int32_t width = sel_pages ? sel_stride : -1;
+  const size_t es = elem_size(desc->dtype);
+  if (!KVQ_POOLS && (p.P - 1) * (p.pool_tok_stride / 16) + p.D / 16 > (INT32_MAX / 16) / (int64_t)es) return OOMB_ERR_UNSUPPORTED;   // (a page of one head: 32-bit offsets)
+  if (!grid_fits((KVQ_POOLS ? kvq_attn_blocks : rows_attn_blocks)(p, bf, width))) return OOMB_ERR_UNSUPPORTED;
+  OOMB_CHECK(check_tensor(q, p, p.Hq, es, &p.q));
+  OOMB_CHECK(check_tensor(o, p, p.Hq, es, &p.q_out));
+  if (!k_pool || !v_pool || !lse || !aligned16(k_pool) || !aligned16(v_pool)) return OOMB_ERR_INVALID_ARG;
+  p.k_pool = const_cast<void*>(k_pool); p.v_pool = const_cast<void*>(v_pool);
+  p.sel = sel_pages; p.sel_count = sel_count; p.sel_stride = sel_stride;
+  p.lse = lse;
+  const size_t need = (KVQ_POOLS ? kvq_attn_workspace_bytes : rows_attn_workspace_bytes)(p, bf, width);
+  if (need && (!workspace || workspace_bytes < need || !aligned16(workspace))) return OOMB_ERR_WORKSPACE;
+  return launched((KVQ_POOLS ? launch_attn_kvq : launch_attn_rows)(p, bf, workspace, (hipStream_t)hip_stream));
+}
+
 }  // namespace
 
 extern "C" {
@@ -154,27 +179,22 @@ size_t oomb_kvq_workspace_bytes(const oomb_rows_desc* desc, int32_t sel_stride) 
   return kvq_attn_workspace_bytes(p, desc->dtype == OOMB_BF16, sel_stride);
 }
 
+size_t oomb_rows_workspace_bytes(const oomb_rows_desc* desc, int32_t sel_stride) {
+  RowsParams p{};
+  if (check_rows(desc, SAME, &p) != OOMB_OK) return 0;
+  return rows_attn_workspace_bytes(p, desc->dtype == OOMB_BF16, sel_stride);
+}
+
 oomb_status oomb_paged_attn_fwd_kvq(const oomb_rows_desc* desc, const oomb_seqs* seqs, const oomb_rows* q, const void* k_pool,
                                     const void* v_pool, const int32_t* sel_pages, const int32_t* sel_count, int32_t sel_stride,
                                     const oomb_rows* o, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
-  RowsParams p{};
-  OOMB_CHECK(check_rows(desc, KVQ, &p));
-  if (!(desc->sm_scale > 0.f) || !std::isfinite(desc->sm_scale)) return OOMB_ERR_INVALID_ARG;
-  OOMB_CHECK(check_seqs(seqs, &p));
-  if (sel_pages && (!sel_count || sel_stride < 0)) return OOMB_ERR_INVALID_ARG;
-  const bool bf = desc->dtype == OOMB_BF16;
-  const int32_t width = sel_pages ? sel_stride : -1;
-  if (!grid_fits(kvq_attn_blocks(p, bf, width))) return OOMB_ERR_UNSUPPORTED;
-  const size_t es = elem_size(desc->dtype);
-  OOMB_CHECK(check_tensor(q, p, p.Hq, es, &p.q));
-  OOMB_CHECK(check_tensor(o, p, p.Hq, es, &p.q_out));
-  if (!k_pool || !v_pool || !lse || !aligned16(k_pool) || !aligned16(v_pool)) return OOMB_ERR_INVALID_ARG;
-  p.k_pool = const_cast<void*>(k_pool); p.v_pool = const_cast<void*>(v_pool);
-  p.sel = sel_pages; p.sel_count = sel_count; p.sel_stride = sel_stride;
-  p.lse = lse;
-  const size_t need = kvq_attn_workspace_bytes(p, bf, width);
-  if (need && (!workspace || workspace_bytes < need || !aligned16(workspace))) return OOMB_ERR_WORKSPACE;
-  return launched(launch_attn_kvq(p, bf, workspace, (hipStream_t)hip_stream));
+  return attn_fwd<true>(desc, seqs, q, k_pool, v_pool, sel_pages, sel_count, sel_stride, o, lse, workspace, workspace_bytes, hip_stream);
+}
+
+oomb_status oomb_paged_attn_fwd_rows(const oomb_rows_desc* desc, const oomb_seqs* seqs, const oomb_rows* q, const void* k_pool,
+                                     const void* v_pool, const int32_t* sel_pages, const int32_t* sel_count, int32_t sel_stride,
+                                     const oomb_rows* o, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return attn_fwd<false>(desc, seqs, q, k_pool, v_pool, sel_pages, sel_count, sel_stride, o, lse, workspace, workspace_bytes, hip_stream);
 }
 
 }  // extern "C"

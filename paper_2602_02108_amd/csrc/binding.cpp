@@ -319,13 +319,14 @@ PyObject* kvq_read(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   OOMB_CALL(oomb_kvq_read(&d, &seqs, ptr(kp), ptr(vp), &rk, &rv, st));
 }
 
-// attn_fwd_kvq(desc, q, k_pool, v_pool, page_tables, seq_lens, row_starts, sel_pages, sel_count, o, lse, workspace)
-PyObject* attn_fwd_kvq(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+// attn_fwd_kvq / attn_fwd_rows(desc, q, k_pool, v_pool, page_tables, seq_lens, row_starts, sel_pages, sel_count, o, lse, workspace)
+template <bool KVQ> PyObject* attn_fwd_packed(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   OOMB_ROWS_ARGS(12);
   const at::Tensor *q = tensor(a[1], bad), *kp = tensor(a[2], bad), *vp = tensor(a[3], bad), *pt = tensor(a[4], bad), *lens = tensor(a[5], bad), *starts = tensor(a[6], bad),
                    *sel = tensor(a[7], bad), *cnt = tensor(a[8], bad), *o = tensor(a[9], bad), *lse = tensor(a[10], bad), *ws = tensor(a[11], bad);
   oomb_seqs seqs; oomb_rows rq, ro;
-  if (bad || !row_tensor(d, q, d.n_q_heads, &rq) || !row_tensor(d, o, d.n_q_heads, &ro) || !pool(d, kp, at::kByte, true) || !pool(d, vp, at::kByte, true) ||
+  const at::ScalarType pt_ = KVQ ? at::kByte : type_of(d.dtype);
+  if (bad || !row_tensor(d, q, d.n_q_heads, &rq) || !row_tensor(d, o, d.n_q_heads, &ro) || !pool(d, kp, pt_, KVQ) || !pool(d, vp, pt_, KVQ) ||
       !seqs_of(d, pt, lens, starts, &seqs) || !lse || lse->scalar_type() != at::kFloat || lse->dim() != 2 || lse->size(0) != d.n_q_heads || lse->size(1) != d.n_rows ||
       !lse->is_contiguous() || (ws && !ws->is_contiguous()))
     return status(-1);
@@ -340,7 +341,8 @@ PyObject* attn_fwd_kvq(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
   if (!place({q, kp, vp, pt, lens, starts, sel, sel ? cnt : nullptr, o, lse, ws}, &st, &guard)) return status(-1);
   // (lists without room are lists all the same: a tensor without elements has no address, so they go by that of the counts, which is not read through)
   const int32_t* lists_at = (const int32_t*)ptr(sel && stride == 0 ? cnt : sel);
-  OOMB_CALL(oomb_paged_attn_fwd_kvq(&d, &seqs, &rq, ptr(kp), ptr(vp), lists_at, (const int32_t*)ptr(cnt), stride, &ro, (float*)ptr(lse), ptr(ws), bytes(ws), st));
+  OOMB_CALL((KVQ ? oomb_paged_attn_fwd_kvq : oomb_paged_attn_fwd_rows)(&d, &seqs, &rq, ptr(kp), ptr(vp), lists_at, (const int32_t*)ptr(cnt), stride, &ro,
+                                                                       (float*)ptr(lse), ptr(ws), bytes(ws), st));
 }
 
 #define OOMB_METHOD(name, fn) {name, (PyCFunction)(void (*)(void))(guarded<fn>), METH_FASTCALL, nullptr}
@@ -360,7 +362,8 @@ PyMethodDef methods[] = {
     OOMB_METHOD("kvq_append_rope", append_rope<true>),
     OOMB_METHOD("kv_append_rope_bwd", append_rope_bwd),
     OOMB_METHOD("kvq_read", kvq_read),
-    OOMB_METHOD("attn_fwd_kvq", attn_fwd_kvq),
+    OOMB_METHOD("attn_fwd_kvq", attn_fwd_packed<true>),
+    OOMB_METHOD("attn_fwd_rows", attn_fwd_packed<false>),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,4 +1,4 @@
-// Packed rows of several sequences: what the kernels of rope_append.hip and attn_kvq.h share (layouts: include/oomb.h).
+// Packed rows of several sequences: what the kernels of rope_append.hip, attn_kvq.h and attn_rows.h share (layouts: include/oomb.h).
 #pragma once
 #include "common.h"
 
@@ -74,9 +74,16 @@ hipError_t launch_attn_kvq_bf16_128(const RowsParams& p, void* ws, hipStream_t s
 hipError_t launch_attn_kvq_bf16_64(const RowsParams& p, void* ws, hipStream_t st);
 hipError_t launch_attn_kvq_f32_128(const RowsParams& p, void* ws, hipStream_t st);
 hipError_t launch_attn_kvq_f32_64(const RowsParams& p, void* ws, hipStream_t st);
+size_t rows_attn_workspace_bytes(const RowsParams& p, bool is_bf16, int32_t sel_stride);
+hipError_t launch_attn_rows(const RowsParams& p, bool is_bf16, void* ws, hipStream_t st);
+hipError_t launch_attn_rows_bf16_128(const RowsParams& p, void* ws, hipStream_t st);
+hipError_t launch_attn_rows_bf16_64(const RowsParams& p, void* ws, hipStream_t st);
+hipError_t launch_attn_rows_f32_128(const RowsParams& p, void* ws, hipStream_t st);
+hipError_t launch_attn_rows_f32_64(const RowsParams& p, void* ws, hipStream_t st);
 // workgroups that a launch would take (the grid may hold 2^24 - 1 of 256 threads)
 int64_t append_rope_blocks(const RowsParams& p, bool kvq);
 int64_t kvq_read_blocks(const RowsParams& p);
 int64_t kvq_attn_blocks(const RowsParams& p, bool is_bf16, int32_t sel_stride);
+int64_t rows_attn_blocks(const RowsParams& p, bool is_bf16, int32_t sel_stride);
 
 }  // namespace oomb
