@@ -512,6 +512,82 @@ oomb_status oomb_paged_attn_fwd_rows(const oomb_rows_desc* desc, const oomb_seqs
                                      const void* v_pool, const int32_t* sel_pages, const int32_t* sel_count, int32_t sel_stride,
                                      const oomb_rows* o, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/*
+ * Generation with several hypotheses a text: the steps between two passes of attention.  One step selects (oomb_beam_topk), forks the sequences
+ * (oomb_page_fork: tables, lengths and reference counts; oomb_page_copy: the pages that it lists, in any number of pools), appends and attends.  All arrays
+ * are device memory, read when the kernels run, so that a captured step follows them; the lists of pools' addresses and the descriptors are host memory.
+ *
+ * State of a cache: page_tables [n_seqs][table_cols] (rows table_stride apart), seq_lens [n_seqs], and refs [num_phys_pages]: how often the tables' entries of
+ * all sequences (those of pages that hold tokens, ceil(len / P) a sequence) name the page, and 0 for a free page.  A caller that holds a page besides adds one of its
+ * own.  Free pages are taken lowest number first.  Lengths are cut to what a row holds, entries outside [0, num_phys_pages) hold nothing.
+ *
+ * oomb_page_fork: the n_out sequences of the next step.  Child b
+ *   parents[b] in [0, n_seqs)  continues that sequence: it shares its full pages.  A partly filled last page stays the first child's if refs names nobody
+ *                              else; every other child gets a free page, and copies[b] = {that page, the new one, tokens to copy}
+ *   OOMB_FORK_BEGINS           begins a new one
+ *   anything else              holds nothing (length 0, whatever grow[b] says)
+ * and gets room for grow[b] more tokens (NULL or below 0: none), in free pages: lens_out[b] = len + grow[b], cut to what a row of tables_out holds.  Sequences
+ * without a child end, and a page that nobody names any more is free in refs_out (a page freed in this step is not handed out in it).
+ *   tables_out [n_out][out_cols] (rows out_stride apart; not in the memory of page_tables)  entries past a sequence's pages are -1
+ *   lens_out [n_out] (may be seq_lens), refs_out [num_phys_pages] (may be refs)
+ *   copies [n_out][3]  {source, destination, tokens}, or {-1, -1, 0} where nothing is to be copied
+ *   status [2]         pages taken, and pages that were missing: their entries are -1 (what is appended there is dropped and not attended)
+ * n_seqs and n_out up to 4096, page_size a power of two.
+ *
+ * oomb_page_compact: the n used pages (refs > 0) move to the places 0 .. n - 1: the i-th used page from n on goes to the i-th free page below n.
+ *   tables_out (may be page_tables), refs_out (may be refs); n_out and out_cols as n_seqs and table_cols
+ *   moves [max_moves >= num_phys_pages / 2][3]  {source, destination, page_size}; entries past status[1] are left as they were
+ *   page_map [num_phys_pages]  the new number of every page, -1 for free ones (for tables that are not in this call)
+ *   status [2]                 n, number of moves
+ *
+ * oomb_page_copy: pool[dst][every head][first tokens rows] = pool[src][...] in n_pools pools of one layout (strides in bytes, 16-byte aligned; tok_stride 0: a
+ * page of a head is one piece of row_bytes bytes, copied whole, as in a pool of 4-bit codes).  max_copies entries, or count[0] (device) of them if that is not NULL
+ * and smaller.  Entries outside the pools copy nothing; no destination may be another entry's source or destination.  A launch takes 64 pools.
+ */
+#define OOMB_FORK_NONE (-1)
+#define OOMB_FORK_BEGINS (-2)
+typedef struct {
+  int32_t n_seqs, n_out, page_size, reserved;
+  int64_t table_cols, table_stride, out_cols, out_stride; /* entries */
+  int64_t num_phys_pages;
+} oomb_pages_desc;
+typedef struct {
+  int32_t n_pools, n_heads, page_size, row_bytes;
+  int64_t num_phys_pages, page_stride, head_stride, tok_stride; /* bytes */
+  int64_t max_copies;
+} oomb_copy_desc;
+size_t oomb_page_fork_workspace_bytes(int32_t n_seqs, int32_t n_out, int64_t num_phys_pages);
+oomb_status oomb_page_fork(const oomb_pages_desc* desc, const int32_t* page_tables, const int32_t* seq_lens, const int32_t* parents,
+                           const int32_t* grow, const int32_t* refs, int32_t* tables_out, int32_t* lens_out, int32_t* refs_out,
+                           int32_t* copies, int32_t* status, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t oomb_page_compact_workspace_bytes(int64_t num_phys_pages);
+oomb_status oomb_page_compact(const oomb_pages_desc* desc, const int32_t* page_tables, const int32_t* seq_lens, const int32_t* refs,
+                              int32_t* tables_out, int32_t* refs_out, int32_t* moves, int64_t max_moves, int32_t* page_map, int32_t* status,
+                              void* workspace, size_t workspace_bytes, void* hip_stream);
+oomb_status oomb_page_copy(const oomb_copy_desc* desc, void* const* pools, const int32_t* copies, const int32_t* count, void* hip_stream);
+
+/*
+ * oomb_beam_topk: of every group's beams and tokens the n_out best
+ *   c(w, v) = scores[w] + x[w][v] - log sum_u exp(x[w][u])
+ * descending, ties to the lowest w * vocab + v.
+ *   logits [n_groups * n_beams][vocab] of dtype, rows row_stride elements apart, aligned to their elements
+ *   scores [n_groups][n_beams] float;  done [n_groups][n_beams] int32 or NULL: a beam that has ended offers one candidate, pad_token at its score, and its
+ *          logits are not read
+ *   parents, tokens [n_groups][n_out] int32, scores_out [n_groups][n_out] float (not in the memory of scores): parents are rows of all groups,
+ *          group * n_beams + w, as oomb_page_fork takes them
+ * A logit of -infinity is never taken.  A beam whose score, or whose log-sum (a logit of +infinity or NaN, nothing but -infinity), is not finite offers nothing;
+ * where candidates run out: -1, -1, -infinity.  Exponentials in fp32, their sums across threads and the candidates in 64 bits: two candidates of different beams
+ * that lie within about 2^-22 of each other may change places.  n_out and n_beams up to 64.
+ */
+typedef struct {
+  int32_t n_groups, n_beams, vocab, n_out;
+  int32_t dtype, pad_token;
+  int64_t row_stride;
+} oomb_beam_desc;
+size_t oomb_beam_workspace_bytes(const oomb_beam_desc* desc);
+oomb_status oomb_beam_topk(const oomb_beam_desc* desc, const void* logits, const float* scores, const int32_t* done, int32_t* parents,
+                           int32_t* tokens, float* scores_out, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 const char* oomb_status_string(int32_t status);
 
 /* major * 10000 + minor * 100 + patch */

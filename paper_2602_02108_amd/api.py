@@ -31,7 +31,8 @@ EXPORTS = ["oomb_workspace_bytes", "oomb_page_score_topk", "oomb_paged_attn_fwd"
            "oomb_offload_plan", "oomb_offload_fetch", "oomb_offload_writeback", "oomb_check_inputs",
            "oomb_page_score_topk_noalloc", "oomb_kv_append_rope", "oomb_kv_append_rope_bwd",
            "oomb_kvq_append_rope", "oomb_kvq_read", "oomb_kvq_workspace_bytes", "oomb_paged_attn_fwd_kvq",
-           "oomb_rows_workspace_bytes", "oomb_paged_attn_fwd_rows"]
+           "oomb_rows_workspace_bytes", "oomb_paged_attn_fwd_rows", "oomb_page_fork_workspace_bytes", "oomb_page_fork",
+           "oomb_page_compact_workspace_bytes", "oomb_page_compact", "oomb_page_copy", "oomb_beam_workspace_bytes", "oomb_beam_topk"]
 
 
 class AttnDesc(ctypes.Structure):
@@ -67,6 +68,23 @@ class Seqs(ctypes.Structure):
 class RopeDesc(ctypes.Structure):
     _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("n_pos", ctypes.c_int64),
                 ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
+class PagesDesc(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_out", ctypes.c_int32), ("page_size", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("table_cols", ctypes.c_int64), ("table_stride", ctypes.c_int64), ("out_cols", ctypes.c_int64), ("out_stride", ctypes.c_int64),
+                ("num_phys_pages", ctypes.c_int64)]
+
+
+class CopyDesc(ctypes.Structure):
+    _fields_ = [("n_pools", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("page_size", ctypes.c_int32), ("row_bytes", ctypes.c_int32),
+                ("num_phys_pages", ctypes.c_int64), ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("tok_stride", ctypes.c_int64),
+                ("max_copies", ctypes.c_int64)]
+
+
+class BeamDesc(ctypes.Structure):
+    _fields_ = [("n_groups", ctypes.c_int32), ("n_beams", ctypes.c_int32), ("vocab", ctypes.c_int32), ("n_out", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("pad_token", ctypes.c_int32), ("row_stride", ctypes.c_int64)]
 
 
 class OombError(RuntimeError):
@@ -155,6 +173,21 @@ def lib():
         l.oomb_rows_workspace_bytes.argtypes = [rd, i32]
         l.oomb_paged_attn_fwd_rows.restype = i32
         l.oomb_paged_attn_fwd_rows.argtypes = l.oomb_paged_attn_fwd_kvq.argtypes
+        pd, cd, bd = (ctypes.POINTER(t) for t in (PagesDesc, CopyDesc, BeamDesc))
+        l.oomb_page_fork_workspace_bytes.restype = u64
+        l.oomb_page_fork_workspace_bytes.argtypes = [i32, i32, i64]
+        l.oomb_page_fork.restype = i32
+        l.oomb_page_fork.argtypes = [pd] + [vp] * 11 + [u64, vp]
+        l.oomb_page_compact_workspace_bytes.restype = u64
+        l.oomb_page_compact_workspace_bytes.argtypes = [i64]
+        l.oomb_page_compact.restype = i32
+        l.oomb_page_compact.argtypes = [pd] + [vp] * 6 + [i64, vp, vp, vp, u64, vp]
+        l.oomb_page_copy.restype = i32
+        l.oomb_page_copy.argtypes = [cd, vp, vp, vp, vp]
+        l.oomb_beam_workspace_bytes.restype = u64
+        l.oomb_beam_workspace_bytes.argtypes = [bd]
+        l.oomb_beam_topk.restype = i32
+        l.oomb_beam_topk.argtypes = [bd] + [vp] * 7 + [u64, vp]
         _lib = l
     return _lib
 
@@ -843,3 +876,182 @@ def paged_attn_fwd_rows(desc: RowsDesc, q, k_pool, v_pool, page_tables, sel_page
     return _attn_fwd_packed("oomb_paged_attn_fwd_rows", (_nb or _native()).attn_fwd_rows, rows_workspace_bytes,
                             torch.bfloat16 if desc.dtype == BF16 else torch.float32, desc, q, k_pool, v_pool, page_tables, sel_pages, sel_count, o, lse,
                             workspace, seq_lens, row_starts)
+
+
+# ---- generation with several hypotheses a text: the steps between two passes of attention (include/oomb.h) ----
+
+FORK_NONE, FORK_BEGINS = -1, -2   # parents of a sequence that holds nothing, and of one that begins
+
+
+class PageFork:
+    """What page_fork leaves: tables [n_out][cols], lens [n_out], refs [n_phys], copies [n_out][3] (for page_copy), status [2] (pages taken, pages missing)."""
+    __slots__ = ("tables", "lens", "refs", "copies", "status")
+
+    def __init__(self, tables, lens, refs, copies, status):
+        self.tables, self.lens, self.refs, self.copies, self.status = tables, lens, refs, copies, status
+
+
+class PageCompact:
+    """What page_compact leaves: tables, refs, moves [n_phys / 2][3] (for page_copy, status[1:] of them), page_map [n_phys], status [2] (used pages, moves)."""
+    __slots__ = ("tables", "refs", "moves", "page_map", "status")
+
+    def __init__(self, tables, refs, moves, page_map, status):
+        self.tables, self.refs, self.moves, self.page_map, self.status = tables, refs, moves, page_map, status
+
+
+def _gen_refused(where: str, ints=(), floats=(), others=()):
+    """The error of a call whose tensors the native module did not take.  ints, floats: (name, tensor, shape; None in it: any size)."""
+    tensors = list(others)
+    for dt, group in ((torch.int32, ints), (torch.float32, floats)):
+        for name, t, shape in group:
+            if t is None:
+                continue
+            if not isinstance(t, torch.Tensor) or t.dtype != dt or t.dim() != len(shape) or any(n is not None and t.shape[i] != n for i, n in enumerate(shape)) or \
+                    (t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1):
+                return OombError(ERR_INVALID_ARG, f"{where}: {name} must be {dt} {['any' if n is None else n for n in shape]}, its last dim contiguous")
+            tensors.append((name, t))
+    devices = {t.device for _, t in tensors if isinstance(t, torch.Tensor)}
+    if len(devices) > 1 or any(x.type != "cuda" for x in devices):
+        return OombError(ERR_INVALID_ARG, f"{where}: the tensors must lie on one GPU (got {sorted(str(x) for x in devices)})")
+    return _refused(where)
+
+
+def _n(t, dim=0):
+    return int(t.shape[dim]) if isinstance(t, torch.Tensor) and t.dim() > dim else None
+
+
+def _workspace_of(need: int, device):
+    return torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+
+
+def page_fork_workspace_bytes(n_seqs: int, n_out: int, n_phys: int) -> int:
+    """oomb_page_fork_workspace_bytes."""
+    return int(lib().oomb_page_fork_workspace_bytes(int(n_seqs), int(n_out), int(n_phys)))
+
+
+def page_fork(page_tables, seq_lens, parents, refs, page_size: int, grow=None, tables_out=None, lens_out=None, refs_out=None, copies=None, status=None,
+              workspace=None) -> PageFork:
+    """oomb_page_fork: the sequences of the next step, one per entry of parents (a sequence, FORK_BEGINS or FORK_NONE), each with room for
+    grow more tokens.  refs is updated in place unless refs_out is given.  page_copy(pools, result.copies) then copies the partly filled pages."""
+    for name, t, dims in (("page_tables", page_tables, 2), ("seq_lens", seq_lens, 1), ("parents", parents, 1), ("refs", refs, 1)):
+        if not isinstance(t, torch.Tensor) or t.dim() != dims:
+            raise OombError(ERR_INVALID_ARG, f"oomb_page_fork: {name} must be a tensor of {dims} dims")
+    n_out, dev = int(parents.shape[0]), page_tables.device
+    if tables_out is None:
+        tables_out = torch.empty((n_out, page_tables.shape[1]), dtype=torch.int32, device=dev)
+    if lens_out is None:
+        lens_out = torch.empty((n_out,), dtype=torch.int32, device=dev)
+    if refs_out is None:
+        refs_out = refs
+    if copies is None:
+        copies = torch.empty((n_out, 3), dtype=torch.int32, device=dev)
+    if status is None:
+        status = torch.empty((2,), dtype=torch.int32, device=dev)
+    if workspace is None:
+        workspace = _workspace_of(page_fork_workspace_bytes(page_tables.shape[0], n_out, refs.shape[0]), dev)
+    st = (_nb or _native()).page_fork(int(page_size), page_tables, seq_lens, parents, grow, refs, tables_out, lens_out, refs_out, copies, status, workspace)
+    if st < 0:
+        S, n_phys = _n(page_tables), _n(refs)
+        raise _gen_refused("oomb_page_fork", [("page_tables", page_tables, (None, None)), ("seq_lens", seq_lens, (S,)), ("parents", parents, (n_out,)),
+                                              ("grow", grow, (n_out,)), ("refs", refs, (None,)), ("tables_out", tables_out, (n_out, None)),
+                                              ("lens_out", lens_out, (n_out,)), ("refs_out", refs_out, (n_phys,)), ("copies", copies, (n_out, 3)),
+                                              ("status", status, (2,))], others=[("workspace", workspace)])
+    if st != OK:
+        raise OombError(st, "oomb_page_fork")
+    return PageFork(tables_out, lens_out, refs_out, copies, status)
+
+
+def page_compact_workspace_bytes(n_phys: int) -> int:
+    """oomb_page_compact_workspace_bytes."""
+    return int(lib().oomb_page_compact_workspace_bytes(int(n_phys)))
+
+
+def page_compact(page_tables, seq_lens, refs, page_size: int, tables_out=None, refs_out=None, moves=None, page_map=None, status=None, workspace=None) -> PageCompact:
+    """oomb_page_compact: the used pages renumbered to the lowest numbers.  page_tables and refs are updated in place unless others are given.
+    page_copy(pools, result.moves, count=result.status[1:]) then moves what they hold."""
+    for name, t, dims in (("page_tables", page_tables, 2), ("seq_lens", seq_lens, 1), ("refs", refs, 1)):
+        if not isinstance(t, torch.Tensor) or t.dim() != dims:
+            raise OombError(ERR_INVALID_ARG, f"oomb_page_compact: {name} must be a tensor of {dims} dims")
+    n_phys, dev = int(refs.shape[0]), page_tables.device
+    if tables_out is None:
+        tables_out = page_tables
+    if refs_out is None:
+        refs_out = refs
+    if moves is None:
+        moves = torch.empty((max(1, n_phys // 2), 3), dtype=torch.int32, device=dev)
+    if page_map is None:
+        page_map = torch.empty((n_phys,), dtype=torch.int32, device=dev)
+    if status is None:
+        status = torch.empty((2,), dtype=torch.int32, device=dev)
+    if workspace is None:
+        workspace = _workspace_of(page_compact_workspace_bytes(n_phys), dev)
+    st = (_nb or _native()).page_compact(int(page_size), page_tables, seq_lens, refs, tables_out, refs_out, moves, page_map, status, workspace)
+    if st < 0:
+        raise _gen_refused("oomb_page_compact", [("page_tables", page_tables, (None, None)), ("seq_lens", seq_lens, (_n(page_tables),)), ("refs", refs, (None,)),
+                                                 ("tables_out", tables_out, (_n(page_tables), _n(page_tables, 1))), ("refs_out", refs_out, (n_phys,)),
+                                                 ("moves", moves, (None, 3)), ("page_map", page_map, (n_phys,)), ("status", status, (2,))],
+                           others=[("workspace", workspace)])
+    if st != OK:
+        raise OombError(st, "oomb_page_compact")
+    return PageCompact(tables_out, refs_out, moves, page_map, status)
+
+
+def page_copy(pools, copies, count=None) -> None:
+    """oomb_page_copy: the listed pages ([n][3] int32: source, destination, tokens) in every pool of a list: [n_phys][Hkv][P][D] of one shape, type
+    and strides, or kvq_pools.  count [1] int32 on the device: how many of the list (default: all)."""
+    if isinstance(pools, torch.Tensor):
+        pools = (pools,)
+    st = (_nb or _native()).page_copy(pools, copies, count)
+    if st < 0:
+        where = "oomb_page_copy"
+        pools = list(pools)
+        if not pools or any(not isinstance(t, torch.Tensor) or t.dim() not in (3, 4) or t.shape != pools[0].shape or t.stride() != pools[0].stride() or
+                            t.dtype != pools[0].dtype or t.stride(-1) != 1 or (t.dim() == 3 and t.dtype != torch.uint8) for t in pools):
+            raise OombError(ERR_INVALID_ARG, f"{where}: pools must be [n_phys][Hkv][P][D] (or kvq_pools) of one shape, type and strides")
+        raise _gen_refused(where, [("copies", copies, (None, 3)), ("count", count, (1,))], others=[("pool", t) for t in pools])
+    if st != OK:
+        raise OombError(st, "oomb_page_copy")
+
+
+def _beam_desc(logits, groups: int, n_out: int, pad_token: int = 0) -> BeamDesc:
+    if not isinstance(logits, torch.Tensor) or logits.dim() not in (2, 3) or logits.dtype not in (torch.float32, torch.bfloat16) or \
+            groups <= 0 or logits.shape[:-1].numel() % groups:
+        raise OombError(ERR_INVALID_ARG, "oomb_beam_topk: logits must be [groups * beams][vocab] (or [groups][beams][vocab]) float32 or bfloat16")
+    rows = logits.shape[:-1].numel()
+    return BeamDesc(groups, rows // groups, int(logits.shape[-1]), int(n_out), _dt(logits.dtype), int(pad_token), logits.stride(-2) if rows > 1 else logits.shape[-1])
+
+
+def beam_workspace_bytes(logits, groups: int, n_out: int) -> int:
+    """oomb_beam_workspace_bytes."""
+    return int(lib().oomb_beam_workspace_bytes(ctypes.byref(_beam_desc(logits, int(groups), n_out))))
+
+
+def beam_topk(logits, scores, n_out: int, done=None, pad_token: int = 0, parents=None, tokens=None, scores_out=None, workspace=None):
+    """oomb_beam_topk: of every group the n_out best continuations of its beams.  logits [groups * beams][vocab] or [groups][beams][vocab]; scores
+    [groups][beams] float32; done [groups][beams] int32.  Returns (parents [groups][n_out] int32 rows of logits, tokens int32, scores float32)."""
+    if not isinstance(scores, torch.Tensor) or scores.dim() != 2 or not isinstance(logits, torch.Tensor):
+        raise OombError(ERR_INVALID_ARG, "oomb_beam_topk: scores must be float32 [groups][beams]")
+    groups, dev = int(scores.shape[0]), logits.device
+    if logits.dim() == 3:
+        if logits.shape[0] != groups or (logits.shape[0] > 1 and logits.shape[1] > 1 and logits.stride(0) != logits.shape[1] * logits.stride(1)):
+            raise OombError(ERR_INVALID_ARG, "oomb_beam_topk: logits [groups][beams][vocab] must have rows at equal distances")
+        logits = logits.flatten(0, 1)
+    desc = _beam_desc(logits, groups, n_out, pad_token)
+    if parents is None:
+        parents = torch.empty((groups, n_out), dtype=torch.int32, device=dev)
+    if tokens is None:
+        tokens = torch.empty((groups, n_out), dtype=torch.int32, device=dev)
+    if scores_out is None:
+        scores_out = torch.empty((groups, n_out), dtype=torch.float32, device=dev)
+    if workspace is None:
+        workspace = _workspace_of(int(lib().oomb_beam_workspace_bytes(ctypes.byref(desc))), dev)
+    st = (_nb or _native()).beam_topk(desc, logits, scores, done, parents, tokens, scores_out, workspace)
+    if st < 0:
+        W = desc.n_beams
+        if logits.stride(-1) != 1 and logits.shape[-1] > 1:
+            raise OombError(ERR_INVALID_ARG, "oomb_beam_topk: the vocabulary of logits must be contiguous")
+        raise _gen_refused("oomb_beam_topk", [("done", done, (groups, W)), ("parents", parents, (groups, n_out)), ("tokens", tokens, (groups, n_out))],
+                           [("scores", scores, (groups, W)), ("scores_out", scores_out, (groups, n_out))], [("logits", logits), ("workspace", workspace)])
+    if st != OK:
+        raise OombError(st, "oomb_beam_topk")
+    return parents, tokens, scores_out

@@ -12,7 +12,8 @@ OUT = os.path.join(HERE, "liboomb.so")
 BINDING = os.path.join(HERE, "_binding.so")
 SOURCES = ["api.hip", "score_topk.hip", "vote_topk.hip", "kv_manager.hip", "page_pool.hip", "offload.hip", "check.hip", "attn_generic.hip", "kv_layout.hip", "qp_lists.hip", "attn_fwd_mfma.hip", "attn_bwd_mfma.hip", "attn_bwd_dkv_mfma.hip", "profile.hip", "calibrate.hip",
            "api_rows.hip", "rope_append.hip", "attn_kvq.hip", "attn_kvq_bf16_128.hip", "attn_kvq_bf16_64.hip", "attn_kvq_f32_128.hip", "attn_kvq_f32_64.hip",
-           "attn_rows.hip", "attn_rows_bf16_128.hip", "attn_rows_bf16_64.hip", "attn_rows_f32_128.hip", "attn_rows_f32_64.hip"]
+           "attn_rows.hip", "attn_rows_bf16_128.hip", "attn_rows_bf16_64.hip", "attn_rows_f32_128.hip", "attn_rows_f32_64.hip",
+           "api_gen.hip", "page_fork.hip", "beam_topk.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-command-line-argument", "-Wno-unknown-warning-option"]

@@ -5,6 +5,8 @@
 // then says which, or takes the call itself --, or -2 if the page lists have to be copied first.  So it does where torch throws (strides of a 0-dim or sparse tensor, the
 // address of a tensor without storage): no exception leaves this file.  The interpreter lock is released during the
 // call of the library.
+#include <vector>
+
 #include <c10/core/DeviceGuard.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -345,6 +347,96 @@ template <bool KVQ> PyObject* attn_fwd_packed(PyObject*, PyObject* const* a, Py_
                                                                        (float*)ptr(lse), ptr(ws), bytes(ws), st));
 }
 
+// ---- generation -------------------------------------------------------------------------------------------------
+bool ints2(const at::Tensor* t) { return t && t->scalar_type() == at::kInt && t->dim() == 2 && (t->size(1) <= 1 || t->stride(1) == 1); }
+bool ints1(const at::Tensor* t, int64_t n) { return t && ints(t, n); }
+bool triples(const at::Tensor* t) { return t && t->scalar_type() == at::kInt && t->dim() == 2 && t->size(1) == 3 && t->is_contiguous(); }
+bool fits32(int64_t x) { return x > 0 && x <= INT32_MAX; }
+#define OOMB_GEN_ARGS(n) if (nargs != (n)) { PyErr_SetString(PyExc_TypeError, "wrong number of arguments"); return nullptr; } \
+  bool bad = false; void* st = nullptr; c10::OptionalDeviceGuard guard
+
+// the tables, lengths and counts of a call on pages; stride of a single row: its length
+bool pages_desc(const at::Tensor* pt, const at::Tensor* lens, const at::Tensor* refs, const at::Tensor* to, const at::Tensor* refs_out, long page, oomb_pages_desc* d) {
+  if (!ints2(pt) || !ints2(to) || !lens || !refs || !fits32(pt->size(0)) || !fits32(to->size(0)) || page <= 0 || page > INT32_MAX) return false;
+  if (!ints1(lens, pt->size(0)) || refs->dim() != 1 || !ints1(refs, refs->size(0)) || !ints1(refs_out, refs->size(0))) return false;
+  *d = {(int32_t)pt->size(0), (int32_t)to->size(0), (int32_t)page, 0, pt->size(1), pt->size(0) > 1 ? pt->stride(0) : pt->size(1), to->size(1),
+        to->size(0) > 1 ? to->stride(0) : to->size(1), refs->size(0)};
+  return true;
+}
+
+// page_fork(page_size, page_tables, seq_lens, parents, grow, refs, tables_out, lens_out, refs_out, copies, status, workspace)
+PyObject* page_fork(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  OOMB_GEN_ARGS(12);
+  const long page = PyLong_AsLong(a[0]);
+  if (PyErr_Occurred()) { PyErr_Clear(); return status(-1); }
+  const at::Tensor *pt = tensor(a[1], bad), *lens = tensor(a[2], bad), *par = tensor(a[3], bad), *grow = tensor(a[4], bad), *refs = tensor(a[5], bad), *to = tensor(a[6], bad),
+                   *lo = tensor(a[7], bad), *ro = tensor(a[8], bad), *cp = tensor(a[9], bad), *stat = tensor(a[10], bad), *ws = tensor(a[11], bad);
+  oomb_pages_desc d;
+  if (bad || !pages_desc(pt, lens, refs, to, ro, page, &d) || !ints1(par, d.n_out) || !ints(grow, d.n_out) || !ints1(lo, d.n_out) || !triples(cp) ||
+      cp->size(0) != d.n_out || !ints1(stat, 2) || (ws && !ws->is_contiguous()) || !place({pt, lens, par, grow, refs, to, lo, ro, cp, stat, ws}, &st, &guard))
+    return status(-1);
+  OOMB_CALL(oomb_page_fork(&d, (const int32_t*)ptr(pt), (const int32_t*)ptr(lens), (const int32_t*)ptr(par), (const int32_t*)ptr(grow), (const int32_t*)ptr(refs),
+                           (int32_t*)ptr(to), (int32_t*)ptr(lo), (int32_t*)ptr(ro), (int32_t*)ptr(cp), (int32_t*)ptr(stat), ptr(ws), bytes(ws), st));
+}
+
+// page_compact(page_size, page_tables, seq_lens, refs, tables_out, refs_out, moves, page_map, status, workspace)
+PyObject* page_compact(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  OOMB_GEN_ARGS(10);
+  const long page = PyLong_AsLong(a[0]);
+  if (PyErr_Occurred()) { PyErr_Clear(); return status(-1); }
+  const at::Tensor *pt = tensor(a[1], bad), *lens = tensor(a[2], bad), *refs = tensor(a[3], bad), *to = tensor(a[4], bad), *ro = tensor(a[5], bad), *mv = tensor(a[6], bad),
+                   *map = tensor(a[7], bad), *stat = tensor(a[8], bad), *ws = tensor(a[9], bad);
+  oomb_pages_desc d;
+  if (bad || !pages_desc(pt, lens, refs, to, ro, page, &d) || !triples(mv) || !ints1(map, d.num_phys_pages) || !ints1(stat, 2) || (ws && !ws->is_contiguous()) ||
+      !place({pt, lens, refs, to, ro, mv, map, stat, ws}, &st, &guard))
+    return status(-1);
+  OOMB_CALL(oomb_page_compact(&d, (const int32_t*)ptr(pt), (const int32_t*)ptr(lens), (const int32_t*)ptr(refs), (int32_t*)ptr(to), (int32_t*)ptr(ro), (int32_t*)ptr(mv),
+                              mv->size(0), (int32_t*)ptr(map), (int32_t*)ptr(stat), ptr(ws), bytes(ws), st));
+}
+
+// page_copy(pools, copies, count); pools: a tuple or a list of [n_phys][Hkv][P][D], or of uint8 [n_phys][Hkv][tile]
+PyObject* page_copy(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  OOMB_GEN_ARGS(3);
+  const at::Tensor *cp = tensor(a[1], bad), *cnt = tensor(a[2], bad);
+  if (bad || !triples(cp) || !ints(cnt, 1) || (!PyTuple_Check(a[0]) && !PyList_Check(a[0]))) return status(-1);
+  const Py_ssize_t n = PySequence_Fast_GET_SIZE(a[0]);
+  if (n < 1 || n > 4096) return status(-1);
+  std::vector<void*> at((size_t)n);
+  const at::Tensor* one = nullptr;
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    const at::Tensor* t = tensor(PySequence_Fast_GET_ITEM(a[0], i), bad);
+    if (bad || !t || (one && !like(t, *one, one->scalar_type())) || (one && t->device() != one->device())) return status(-1);
+    if (!one) one = t;
+    at[(size_t)i] = t->data_ptr();
+  }
+  const bool tiles = one->dim() == 3 && one->scalar_type() == at::kByte;
+  if (one->dim() != (tiles ? 3 : 4) || one->stride(-1) != 1 || !fits32(one->size(1)) || !fits32(one->size(2)) || !place({one, cp, cnt}, &st, &guard)) return status(-1);
+  const int64_t es = (int64_t)one->element_size(), row = one->size(-1) * es;
+  if (!fits32(row)) return status(-1);
+  const oomb_copy_desc d = {(int32_t)n, (int32_t)one->size(1), tiles ? 1 : (int32_t)one->size(2), (int32_t)row, one->size(0), one->stride(0) * es, one->stride(1) * es,
+                            tiles ? 0 : one->size(2) > 1 ? one->stride(2) * es : row, cp->size(0)};
+  OOMB_CALL(oomb_page_copy(&d, at.data(), (const int32_t*)ptr(cp), (const int32_t*)ptr(cnt), st));
+}
+
+// beam_topk(desc, logits, scores, done, parents, tokens, scores_out, workspace)
+PyObject* beam_topk(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+  OOMB_GEN_ARGS(8);
+  DescOf<oomb_beam_desc> desc(a[0]);
+  if (!desc.d) return status(-1);
+  const oomb_beam_desc& d = *desc.d;
+  const at::Tensor *x = tensor(a[1], bad), *sc = tensor(a[2], bad), *done = tensor(a[3], bad), *par = tensor(a[4], bad), *tok = tensor(a[5], bad), *out = tensor(a[6], bad),
+                   *ws = tensor(a[7], bad);
+  const int64_t rows = (int64_t)d.n_groups * d.n_beams, outs = (int64_t)d.n_groups * d.n_out;
+  if (bad || !x || x->scalar_type() != type_of(d.dtype) || x->dim() != 2 || x->size(0) != rows || x->size(1) != d.vocab || x->stride(1) != 1 ||
+      (rows > 1 && x->stride(0) != d.row_stride) || !sc || sc->scalar_type() != at::kFloat || sc->numel() != rows || !sc->is_contiguous() ||
+      (done && (done->scalar_type() != at::kInt || done->numel() != rows || !done->is_contiguous())) || !par || !tok || !out ||
+      par->scalar_type() != at::kInt || tok->scalar_type() != at::kInt || out->scalar_type() != at::kFloat || par->numel() != outs || tok->numel() != outs ||
+      out->numel() != outs || !par->is_contiguous() || !tok->is_contiguous() || !out->is_contiguous() || (ws && !ws->is_contiguous()) ||
+      !place({x, sc, done, par, tok, out, ws}, &st, &guard))
+    return status(-1);
+  OOMB_CALL(oomb_beam_topk(&d, ptr(x), (const float*)ptr(sc), (const int32_t*)ptr(done), (int32_t*)ptr(par), (int32_t*)ptr(tok), (float*)ptr(out), ptr(ws), bytes(ws), st));
+}
+
 #define OOMB_METHOD(name, fn) {name, (PyCFunction)(void (*)(void))(guarded<fn>), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     OOMB_METHOD("make_desc", make_desc),
@@ -364,6 +456,10 @@ PyMethodDef methods[] = {
     OOMB_METHOD("kvq_read", kvq_read),
     OOMB_METHOD("attn_fwd_kvq", attn_fwd_packed<true>),
     OOMB_METHOD("attn_fwd_rows", attn_fwd_packed<false>),
+    OOMB_METHOD("page_fork", page_fork),
+    OOMB_METHOD("page_compact", page_compact),
+    OOMB_METHOD("page_copy", page_copy),
+    OOMB_METHOD("beam_topk", beam_topk),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
