@@ -2,13 +2,13 @@
 //
 //   candidate(w, v) = score[w] + x[w][v] - log sum_u exp(x[w][u])
 //
-// Within a row the order is that of the logits, so the first kernel needs no log-sum: a workgroup reads a slice of a row once, for the maximum and the
-// sum of exponentials against it, and for the slice's best.  The second kernel, one workgroup per group, adds the slices' sums, takes the candidates in 64 bits and keeps the best.
-// Ties go to the lowest w * vocab + v throughout.
-//
-// The best K of many: the K-th best of the threads' maxima is a bound that K values reach at least, and few others: these are written to the LDS and
-// each one's rank is counted.
+// The first kernel reads the logits once, a slice of a row per workgroup: for each thread the maximum of its elements (a "cell" of the slice) and their sum of
+// exponentials against it.  The second one, a workgroup per group, adds the sums, which makes candidates of different beams comparable, and looks for the K best
+// through the cells: the K-th best cell maximum is a bound that K candidates reach at least; only the few cells that reach it are read again, and the rank of
+// each of their values above the bound is counted.  Candidates are compared in 64 bits, ties go to the lowest w * vocab + v.
+// Where very many values are equal the bound does not sort them out; then a group is walked in order of its places, the K best so far in hand.
 #include <algorithm>
+#include <cfloat>
 
 #include "gen.h"
 
@@ -16,10 +16,17 @@ namespace oomb {
 
 namespace {
 
-constexpr int THREADS = 256;
+constexpr int THREADS = 256;                    // of the first kernel
 constexpr int LOADS = 4;                        // of 16 bytes, of a thread at a time
 constexpr int MOST_LISTS = 256;                 // slices of a group's rows
 constexpr int MOST_SLICES = 64;
+constexpr int GROUP_THREADS = 1024;             // of the second
+constexpr int GROUP_WAVES = GROUP_THREADS / 64;
+constexpr int HELD = 16;                        // cells that a thread of it keeps in registers
+constexpr int CELLS = 4096;                     // that reach a wave's bound
+constexpr int HOLDERS = 1024;                   // of them, that reach the bound
+constexpr int ROOM = GROUP_THREADS;             // candidates that do
+constexpr int PARTS = 8;                        // threads that count a rank together
 template <typename T> constexpr int VEC = 16 / (int)sizeof(T);
 template <typename T> constexpr int EACH = LOADS * VEC<T>;       // elements of a thread at a time
 template <typename T> constexpr int TILE = THREADS * EACH<T>;
@@ -28,13 +35,12 @@ template <typename T> constexpr int TILE = THREADS * EACH<T>;
 constexpr float LOG2E_HI = 1.44269502162933349609375f, LOG2E_LO = 1.925963033500011e-8f;
 __device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(__builtin_fmaf(d, LOG2E_HI, d * LOG2E_LO)); }
 
-struct BeamWs { double* sums; float* tops; float* vals; int32_t* ids; };   // of a (row, slice): sum against the maximum, maximum, its K best, descending
-__host__ __device__ BeamWs beam_ws(void* ws, int64_t lists, int k) {
+struct BeamWs { double* sums; float* tops; float* cells; };   // of a (row, slice): sum against the maximum, maximum, [THREADS] maxima
+__host__ __device__ BeamWs beam_ws(void* ws, int64_t lists) {
   BeamWs w;
   w.sums = (double*)ws;
   w.tops = (float*)(w.sums + lists);
-  w.vals = w.tops + lists;
-  w.ids = (int32_t*)(w.vals + lists * k);
+  w.cells = w.tops + lists;
   return w;
 }
 
@@ -51,124 +57,86 @@ template <> __device__ __forceinline__ void unpack<bf16_t>(const uint4& v, float
   }
 }
 
-__device__ __forceinline__ bool better(float a, int i, float b, int j) { return a > b || (a == b && i < j); }
+// A row.  Positions count from the 16-byte boundary at or before its first element, which lies `lead` elements behind it.
+template <typename T> struct Row {
+  const T* from;                                 // (only ever read inside the row)
+  int lead;
+  int64_t end;
+  __device__ __forceinline__ Row(const BeamParams& p, int64_t row) {
+    const T* x = (const T*)p.logits + row * p.row_stride;
+    lead = (int)(((uintptr_t)x & 15) / sizeof(T));
+    from = x - lead;
+    end = (int64_t)lead + p.vocab;
+  }
+  // 16 bytes at a position; what lies outside the row: -infinity
+  __device__ __forceinline__ uint4 load(int64_t at) const {
+    if (at >= lead && at + VEC<T> <= end) return *reinterpret_cast<const uint4*>(from + at);
+    uint32_t word[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (sizeof(T) == 4) {
+        word[j] = at + j >= lead && at + j < end ? __float_as_uint(from[at + j]) : 0xff800000u;
+      } else {
+        const int64_t lo = at + 2 * j, hi = lo + 1;
+        word[j] = (lo >= lead && lo < end ? (uint32_t)from[lo] : 0xff80u) | (hi >= lead && hi < end ? (uint32_t)from[hi] : 0xff80u) << 16;
+      }
+    }
+    return make_uint4(word[0], word[1], word[2], word[3]);
+  }
+};
+// piece i of a slice, of a thread
+template <typename T> __device__ __forceinline__ int64_t place_of(int slice, int slice_tiles, int i, int thread) {
+  return (int64_t)slice * slice_tiles * TILE<T> + ((int64_t)i * THREADS + thread) * VEC<T>;
+}
 
-// One slice of one row.  Positions count from the 16-byte boundary at or before the row's first element, which lies `lead` elements behind it.
 template <typename T>
-__global__ __launch_bounds__(THREADS) void beam_rows_kernel(BeamParams p, void* ws, int slices, int slice_tiles) {
-  const int row = blockIdx.x / slices, slice = blockIdx.x - row * slices, K = p.n_out, tid = threadIdx.x;
+__global__ __launch_bounds__(THREADS, 4) void beam_rows_kernel(BeamParams p, void* ws, int slices, int slice_tiles) {
+  const int row = blockIdx.x / slices, slice = blockIdx.x - row * slices, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (p.done && p.done[row]) return;
   const float score = p.scores[row];
   if (!(fabsf(score) < INFINITY)) return;
-  const BeamWs w = beam_ws(ws, (int64_t)p.n_groups * p.n_beams * slices, K);
-  __shared__ float top_of[THREADS];
-  __shared__ int id_of[THREADS];
-  __shared__ float bound;
-  __shared__ int bound_id, n_cand;
-  __shared__ double wave_sum[THREADS / 64];
-  __shared__ float wave_top[THREADS / 64];
-  extern __shared__ __align__(16) char room[];
-  float* cand = (float*)room;                    // [K * EACH + K]
-  int* cand_id = (int*)(cand + K * EACH<T> + K);
-  float* best = (float*)(cand_id + K * EACH<T> + K);   // [K], descending; ids from 0 to n_best - 1
-  int* best_id = (int*)(best + K);
-
-  const T* x = (const T*)p.logits + (int64_t)row * p.row_stride;
-  const int lead = (int)(((uintptr_t)x & 15) / sizeof(T));
-  const T* from = x - lead;                      // (only ever read inside the row)
-  const int64_t end = (int64_t)lead + p.vocab, first = (int64_t)slice * slice_tiles * TILE<T>;
+  constexpr int WAVES = THREADS / 64;
+  __shared__ double wave_sum[WAVES];
+  __shared__ float wave_top[WAVES];
+  const Row<T> x(p, row);
   float top = -INFINITY, sum = 0.0f;             // of this thread's elements
-  int n_best = 0;
-  float worst = -INFINITY;                       // the K-th best so far; what equals it comes later and loses
+  uint4 raw[LOADS];
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) raw[i] = x.load(place_of<T>(slice, slice_tiles, i, tid));
   for (int t = 0; t < slice_tiles; ++t) {
-    const int64_t base = first + (int64_t)t * TILE<T>;
-    if (base >= end) break;
+    const int64_t base = place_of<T>(slice, slice_tiles, t * LOADS, 0);
+    if (base >= x.end) break;
     float f[EACH<T>];
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int64_t at = base + ((int64_t)i * THREADS + tid) * VEC<T>;
-      if (at >= lead && at + VEC<T> <= end) {
-        unpack<T>(*reinterpret_cast<const uint4*>(from + at), f + i * VEC<T>);
-      } else {
+    for (int i = 0; i < LOADS; ++i) unpack<T>(raw[i], f + i * VEC<T>);
+    if (t + 1 < slice_tiles && base + TILE<T> < x.end) {
 #pragma unroll
-        for (int j = 0; j < VEC<T>; ++j) f[i * VEC<T> + j] = at + j >= lead && at + j < end ? Elem<T>::load(from + at + j) : -INFINITY;
-      }
+      for (int i = 0; i < LOADS; ++i) raw[i] = x.load(place_of<T>(slice, slice_tiles, (t + 1) * LOADS + i, tid));
     }
     float here = f[0];
-    int where = 0;
 #pragma unroll
-    for (int j = 1; j < EACH<T>; ++j) {
-      where = f[j] > here || !(here == here) ? j : where;
-      here = fmaxf(here, f[j]);
-    }
-    const float to = fmaxf(top, here);
-    if (to > -INFINITY) {
-      sum *= exp_of(top - to);                   // (top -infinity: 0)
-      float s4[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int j = 1; j < EACH<T>; ++j) here = fmaxf(here, f[j]);   // (not a NaN, unless all are)
+    const float to = fmaxf(top, here), ref = to == -INFINITY ? 0.0f : to;
+    float s4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < EACH<T>; ++j) s4[j & 3] += exp_of(f[j] - to);
-      sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
-      top = to;
-    } else {
-#pragma unroll
-      for (int j = 0; j < EACH<T>; ++j) sum += f[j] == f[j] ? 0.0f : f[j];   // NaN
-    }
-    if (!__syncthreads_or(here > worst)) continue;
-
-    // the bound: the K-th best of the threads' maxima
-    auto id_at = [&](int j) { return (int)(base + ((int64_t)(j / VEC<T>) * THREADS + tid) * VEC<T> + j % VEC<T> - lead); };
-    const int here_id = id_at(where);
-    top_of[tid] = here;
-    id_of[tid] = here_id;
-    if (tid == 0) { n_cand = 0; bound = -INFINITY; bound_id = 0x7fffffff; }
-    __syncthreads();
-    int rank = 0;
-    for (int i = 0; i < THREADS; ++i) rank += better(top_of[i], id_of[i], here, here_id);
-    if (rank == K - 1 && here > -INFINITY) { bound = here; bound_id = here_id; }
-    __syncthreads();
-    const float b = bound;
-    const int b_id = bound_id;
-    if (here > worst && !better(b, b_id, here, here_id)) {
-#pragma unroll
-      for (int j = 0; j < EACH<T>; ++j)
-        if (f[j] > worst && !better(b, b_id, f[j], id_at(j))) {
-          const int c = atomicAdd(&n_cand, 1);
-          cand[c] = f[j];
-          cand_id[c] = id_at(j);
-        }
-    }
-    __syncthreads();
-    const int fresh = n_cand, all = fresh + n_best;
-    for (int i = tid; i < n_best; i += THREADS) { cand[fresh + i] = best[i]; cand_id[fresh + i] = best_id[i]; }
-    __syncthreads();
-    for (int c = tid; c < all; c += THREADS) {
-      const float v = cand[c];
-      const int id = cand_id[c];
-      int r = 0;
-      for (int i = 0; i < all; ++i) r += better(cand[i], cand_id[i], v, id);
-      if (r < K) { best[r] = v; best_id[r] = id; }
-    }
-    __syncthreads();
-    n_best = min(all, K);
-    if (n_best == K) worst = best[K - 1];
+    for (int j = 0; j < EACH<T>; ++j) s4[j & 3] += exp_of(f[j] - ref);
+    sum = sum * (top == to ? 1.0f : exp_of(top - ref)) + ((s4[0] + s4[1]) + (s4[2] + s4[3]));
+    top = to;
   }
-
   const int64_t list = (int64_t)row * slices + slice;
-  for (int i = tid; i < K; i += THREADS) {
-    w.vals[list * K + i] = i < n_best ? best[i] : -INFINITY;
-    w.ids[list * K + i] = i < n_best ? best_id[i] : -1;
-  }
-  // the slice's maximum and sum
+  const BeamWs w = beam_ws(ws, (int64_t)p.n_groups * p.n_beams * slices);
+  w.cells[list * THREADS + tid] = top;
   float m = top;
 #pragma unroll
   for (int k = 1; k < 64; k *= 2) m = fmaxf(m, __shfl_xor(m, k, 64));
-  if ((tid & 63) == 0) wave_top[tid >> 6] = m;
+  if (lane == 0) wave_top[wave] = m;
   __syncthreads();
-  m = fmaxf(fmaxf(wave_top[0], wave_top[1]), fmaxf(wave_top[2], wave_top[3]));
-  double s = top > -INFINITY ? (double)sum * (double)exp_of(top - m) : (double)sum;
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) m = fmaxf(m, wave_top[i]);
+  double s = (double)(top > -INFINITY ? sum * exp_of(top - m) : sum);
 #pragma unroll
   for (int k = 1; k < 64; k *= 2) s += __shfl_xor(s, k, 64);
-  if ((tid & 63) == 0) wave_sum[tid >> 6] = s;
+  if (lane == 0) wave_sum[wave] = s;
   __syncthreads();
   if (tid == 0) {
     w.tops[list] = m;
@@ -176,97 +144,214 @@ __global__ __launch_bounds__(THREADS) void beam_rows_kernel(BeamParams p, void* 
   }
 }
 
-__device__ __forceinline__ bool better64(double a, int i, double b, int j) { return a > b || (a == b && i < j); }
+// a double as a number in the same order (-0 as 0); 0: nothing (below every value)
+__device__ __forceinline__ uint64_t ordered64(double v) {
+  const uint64_t u = (uint64_t)__double_as_longlong(v + 0.0);
+  return u ^ ((uint64_t)((int64_t)u >> 63) | 1ull << 63);
+}
+__device__ __forceinline__ double unordered64(uint64_t k) { return __longlong_as_double((long long)(k ^ ((uint64_t)((int64_t)~k >> 63) | 1ull << 63))); }
 
-// One group: lists in order of beam and slice, so that of equal candidates the one of the lower list, and in it the first, wins.
-__global__ __launch_bounds__(THREADS) void beam_group_kernel(BeamParams p, void* ws, int slices) {
-  const int group = blockIdx.x, K = p.n_out, tid = threadIdx.x, lists = p.n_beams * slices;
-  const BeamWs w = beam_ws(ws, (int64_t)p.n_groups * p.n_beams * slices, K);
+// Candidates in the LDS: a value, and where it stands: beam << 32 | token.
+struct Cands {
+  uint64_t val[ROOM + BEAM_MOST_OUT + 8 * PARTS];
+  uint64_t at[ROOM + BEAM_MOST_OUT + 8 * PARTS];
+  uint64_t best_val[BEAM_MOST_OUT], best_at[BEAM_MOST_OUT];   // in order
+};
+// The K best of `fresh` candidates and of the n_best best so far, in order; the new n_best.  (By every thread of a workgroup; no candidate twice.)
+__device__ int keep_best(Cands& c, int fresh, int n_best, int K) {
+  const int tid = threadIdx.x, all = fresh + n_best;
+  if (tid < n_best) { c.val[fresh + tid] = c.best_val[tid]; c.at[fresh + tid] = c.best_at[tid]; }
+  if (tid >= 64 && tid < 64 + 8 * PARTS) c.val[all + tid - 64] = 0;   // (loops of eight)
+  __syncthreads();
+  for (int i0 = 0; i0 < all; i0 += GROUP_THREADS / PARTS) {
+    const int i = i0 + tid / PARTS;
+    const uint64_t v = c.val[min(i, all)], at = c.at[min(i, all)];
+    int r = 0;
+    for (int k = 8 * (tid % PARTS); k < all; k += 8 * PARTS) {
+      uint64_t v8[8], at8[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) { v8[j] = c.val[k + j]; at8[j] = c.at[k + j]; }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) r += (int)(v8[j] > v) | ((int)(v8[j] == v) & (int)(at8[j] < at));
+    }
+#pragma unroll
+    for (int k = 1; k < PARTS; k *= 2) r += __shfl_xor(r, k, 64);
+    if (i < all && tid % PARTS == 0 && r < K) { c.best_val[r] = v; c.best_at[r] = at; }
+  }
+  __syncthreads();
+  return min(all, K);
+}
+
+template <typename T> __global__ __launch_bounds__(GROUP_THREADS) void beam_group_kernel(BeamParams p, void* ws, int slices, int slice_tiles) {
+  const int group = blockIdx.x, K = p.n_out, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lists = p.n_beams * slices, n_cells = lists * THREADS;
+  const BeamWs w = beam_ws(ws, (int64_t)p.n_groups * p.n_beams * slices);
   __shared__ double base[BEAM_MOST_BEAMS];       // score less log-sum; -infinity: the row offers nothing
-  __shared__ double key[MOST_LISTS];
-  __shared__ int ended[BEAM_MOST_BEAMS], n_cand;
-  __shared__ double bound;
-  __shared__ int bound_list;
-  extern __shared__ __align__(16) char room[];
-  double* cand = (double*)room;                  // [K * K + K]
-  int* cand_at = (int*)(cand + K * K + K);       // list * K + place
-  for (int beam = tid >> 6; beam < p.n_beams; beam += THREADS / 64) {
-    const int lane = tid & 63;
+  __shared__ uint8_t beam_of[MOST_LISTS];
+  __shared__ uint32_t wave_bound[GROUP_WAVES], bound;
+  __shared__ __align__(16) uint32_t cell_key[CELLS + 8 * PARTS];
+  __shared__ uint32_t cell_id[CELLS];
+  __shared__ uint32_t holder[HOLDERS];
+  __shared__ uint64_t ended_val[BEAM_MOST_BEAMS], ended_at[BEAM_MOST_BEAMS];
+  __shared__ int n_cell, n_hold, n_cand;
+  __shared__ uint64_t top_val;
+  __shared__ __align__(16) Cands c;
+  const float* cells = w.cells + (int64_t)group * n_cells;
+  float held[HELD];                              // (on their way while the log-sums are formed; of a row that offers nothing they are not used)
+#pragma unroll
+  for (int j = 0; j < HELD; ++j) held[j] = cells[min(tid + j * GROUP_THREADS, n_cells - 1)];
+  if (tid < lists) beam_of[tid] = (uint8_t)(tid / slices);
+  if (tid == 0) { n_cell = n_hold = n_cand = 0; bound = 0; top_val = 0; }
+  __syncthreads();
+  for (int beam = wave; beam < p.n_beams; beam += GROUP_WAVES) {
     const int64_t row = (int64_t)group * p.n_beams + beam;
-    const float score = p.scores[row];
+    const bool mine = lane < slices;             // (at most 64)
+    const float score = p.scores[row], t = mine ? w.tops[row * slices + lane] : -INFINITY;
     const int over = p.done ? p.done[row] : 0;
+    const double part = mine ? w.sums[row * slices + lane] : 0.0;
     const bool alive = fabsf(score) < INFINITY;
-    float m = -INFINITY;
-    double s = 0.0, z = 0.0;
+    double z = INFINITY;
     if (alive && !over) {
-      const bool mine = lane < slices;           // (at most 64)
-      const float t = mine ? w.tops[row * slices + lane] : -INFINITY;
-      m = t;
+      float m = t;
 #pragma unroll
       for (int k = 1; k < 64; k *= 2) m = fmaxf(m, __shfl_xor(m, k, 64));
-      const double part = mine ? w.sums[row * slices + lane] : 0.0;
-      s = t > -INFINITY ? part * exp((double)t - (double)m) : part;
+      double s = t > -INFINITY ? part * exp((double)t - (double)m) : part;
 #pragma unroll
       for (int k = 1; k < 64; k *= 2) s += __shfl_xor(s, k, 64);
       z = (double)m + log(s);
     }
     if (lane == 0) {
-      ended[beam] = alive && over;
-      base[beam] = alive && !over && fabs(z) < (double)INFINITY ? (double)score - z : -(double)INFINITY;
+      base[beam] = fabs(z) < (double)INFINITY ? (double)score - z : -(double)INFINITY;
+      if (alive && over) {                       // a beam that has ended offers one candidate
+        const int i = atomicAdd(&n_cand, 1);
+        c.val[i] = ended_val[i] = ordered64((double)score);
+        c.at[i] = ended_at[i] = (uint64_t)beam << 32 | (uint32_t)p.pad_token;
+      }
     }
   }
-  if (tid == 0) { n_cand = 0; bound = -(double)INFINITY; bound_list = 0x7fffffff; }
   __syncthreads();
-  // candidate `at` of a list; an ended beam has one, in its first list
-  auto value = [&](int list, int at) -> double {
-    const int beam = list / slices;
-    if (ended[beam]) return list == beam * slices && at == 0 ? (double)p.scores[(int64_t)group * p.n_beams + beam] : -(double)INFINITY;
-    if (!(base[beam] > -(double)INFINITY)) return -(double)INFINITY;
-    return base[beam] + (double)w.vals[((int64_t)group * lists + list) * K + at];
+  const int n_ended = n_cand;
+  auto value = [&](int beam, float x) -> uint64_t {   // 0: nothing
+    const double v = base[beam] + (double)x;
+    return x > -INFINITY && v > -(double)INFINITY ? ordered64(v) : 0;
   };
-  // With K or more lists their firsts give the bound; fewer are compared at the depth where they hold K together.
-  const int depth = (K + lists - 1) / lists - 1, want = (K + depth) / (depth + 1);
-  const double mine = tid < lists ? value(tid, depth) : -(double)INFINITY;
-  if (tid < lists) key[tid] = mine;
+  auto cell = [&](int i, float x) -> uint32_t { return i < n_cells ? (uint32_t)(value(beam_of[i / THREADS], x) >> 32) : 0; };
+  uint32_t mine = 0;
+#pragma unroll
+  for (int j = 0; j < HELD; ++j) mine = max(mine, cell(tid + j * GROUP_THREADS, held[j]));
+  for (int i = tid + HELD * GROUP_THREADS; i < n_cells; i += GROUP_THREADS) mine = max(mine, cell(i, cells[i]));
+  // A bound that K cells reach at least: of the waves' K-th best threads the best; to 12 bits of a mantissa
+  uint32_t limit = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 8; --bit) {
+    const uint32_t with = limit | 1u << bit;
+    limit = __builtin_popcountll(__ballot(mine >= with)) >= K ? with : limit;
+  }
+  if (lane == 0) wave_bound[wave] = limit;
   __syncthreads();
-  if (tid < lists && mine > -(double)INFINITY) {
-    int rank = 0;
-    for (int i = 0; i < lists; ++i) rank += better64(key[i], i, mine, tid);
-    if (rank == want - 1) { bound = mine; bound_list = tid; }
+  limit = 1;
+#pragma unroll
+  for (int i = 0; i < GROUP_WAVES; ++i) limit = max(limit, wave_bound[i]);
+  auto note = [&](int i, float x) __attribute__((always_inline)) {
+    const uint32_t key = cell(i, x);
+    if (key < limit) return;
+    const int to = atomicAdd(&n_cell, 1);
+    if (to < CELLS) { cell_key[to] = key; cell_id[to] = i; }
+  };
+  if (mine >= limit) {
+#pragma unroll
+    for (int j = 0; j < HELD; ++j) note(tid + j * GROUP_THREADS, held[j]);
+    for (int i = tid + HELD * GROUP_THREADS; i < n_cells; i += GROUP_THREADS) note(i, cells[i]);
   }
   __syncthreads();
-  if (tid < lists) {
-    const double b = bound;
-    const int b_list = bound_list;
-    for (int i = 0; i < K; ++i) {
-      const double v = value(tid, i);
-      // (in its own list the bound lies at `depth`: what is there and before it counts, and equals behind it do not)
-      if (!(v > -(double)INFINITY) || better64(b, b_list, v, tid) || (tid == b_list && i > depth)) break;
-      const int c = atomicAdd(&n_cand, 1);
-      cand[c] = v;
-      cand_at[c] = tid * K + i;
+  const int noted = n_cell;
+  int n_best = 0;
+  bool found = noted <= CELLS;
+  if (found) {
+    // the K-th best of them (equal ones in any order: what equals it counts)
+    if (tid < 8 * PARTS) cell_key[noted + tid] = 0;
+    __syncthreads();
+    for (int i0 = 0; i0 < noted; i0 += GROUP_THREADS / PARTS) {
+      const int i = i0 + tid / PARTS;
+      const uint32_t key = cell_key[min(i, noted)];
+      int more = 0, same = 0;
+      for (int k = 8 * (tid % PARTS); k < noted; k += 8 * PARTS) {
+        uint32_t k8[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) k8[j] = cell_key[k + j];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { more += k8[j] > key; same += k8[j] == key; }
+      }
+#pragma unroll
+      for (int k = 1; k < PARTS; k *= 2) { more += __shfl_xor(more, k, 64); same += __shfl_xor(same, k, 64); }
+      if (i < noted && more < K && more + same >= K) bound = key;   // (whoever writes writes the same)
+    }
+    __syncthreads();
+    for (int i = tid; i < noted; i += GROUP_THREADS)
+      if (cell_key[i] >= bound) {
+        const int to = atomicAdd(&n_hold, 1);
+        if (to < HOLDERS) holder[to] = cell_id[i];
+      }
+    __syncthreads();
+    const int n_holders = n_hold;
+    found = n_holders <= HOLDERS;
+    if (found) {
+      // their values once more, a piece of 16 bytes a thread
+      const uint64_t least = max((uint64_t)bound << 32, 1ull);
+      const int each = slice_tiles * LOADS;
+      for (int e = tid; e < n_holders * each; e += GROUP_THREADS) {
+        const int h = e / each, i = e - h * each, id = holder[h], list = id / THREADS, beam = beam_of[list];
+        const Row<T> x(p, (int64_t)group * p.n_beams + beam);
+        const int64_t at = place_of<T>(list - beam * slices, slice_tiles, i, id % THREADS);
+        float f[VEC<T>];
+        unpack<T>(x.load(at), f);
+#pragma unroll
+        for (int j = 0; j < VEC<T>; ++j) {
+          const uint64_t v = value(beam, f[j]);
+          if (v < least) continue;
+          const int to = atomicAdd(&n_cand, 1);
+          if (to < ROOM) { c.val[to] = v; c.at[to] = (uint64_t)beam << 32 | (uint32_t)(at + j - x.lead); }
+        }
+      }
+      __syncthreads();
+      found = n_cand <= ROOM;
+      if (found) n_best = keep_best(c, n_cand, 0, K);
     }
   }
-  __syncthreads();
-  const int all = n_cand;
-  for (int c = tid; c < all; c += THREADS) {
-    const double v = cand[c];
-    const int at = cand_at[c];
-    int r = 0;
-    for (int i = 0; i < all; ++i) r += better64(cand[i], cand_at[i], v, at);
-    if (r < K) {
-      const int list = at / K, beam = list / slices;
-      const int64_t to = (int64_t)group * K + r;
-      p.parents[to] = group * p.n_beams + beam;
-      p.tokens[to] = ended[beam] ? p.pad_token : w.ids[((int64_t)group * lists) * K + at];
-      p.best[to] = (float)v;
+  if (!found) {
+    // Very many equal values.  Every place in order, what is no better than the K-th best so far left out, until nothing better can come.
+    if (tid < n_ended) { c.val[tid] = ended_val[tid]; c.at[tid] = ended_at[tid]; }
+    for (int i = tid; i < n_cells; i += GROUP_THREADS) {
+      const uint64_t v = value(beam_of[i / THREADS], cells[i]);
+      if (v) atomicMax((unsigned long long*)&top_val, (unsigned long long)v);
+    }
+    __syncthreads();
+    n_best = keep_best(c, n_ended, 0, K);
+    for (int beam = 0; beam < p.n_beams; ++beam) {
+      if (!(base[beam] > -(double)INFINITY)) continue;
+      const Row<T> x(p, (int64_t)group * p.n_beams + beam);
+      for (int64_t v0 = 0; v0 < p.vocab; v0 += GROUP_THREADS) {
+        const uint64_t worst = n_best == K ? c.best_val[K - 1] : 0;
+        if (worst >= top_val) break;
+        const int64_t at = v0 + tid;
+        const uint64_t v = at < p.vocab ? value(beam, Elem<T>::load(x.from + x.lead + at)) : 0;
+        if (tid == 0) n_cand = 0;
+        if (!__syncthreads_or(v > worst)) continue;
+        if (v > worst) {
+          const int to = atomicAdd(&n_cand, 1);
+          c.val[to] = v;
+          c.at[to] = (uint64_t)beam << 32 | (uint32_t)at;
+        }
+        __syncthreads();
+        n_best = keep_best(c, n_cand, n_best, K);
+      }
     }
   }
-  for (int r = all + tid; r < K; r += THREADS) {
-    const int64_t to = (int64_t)group * K + r;
-    p.parents[to] = -1;
-    p.tokens[to] = -1;
-    p.best[to] = -INFINITY;
+  if (tid < K) {
+    const int64_t to = (int64_t)group * K + tid;
+    const bool is = tid < n_best;
+    p.parents[to] = is ? group * p.n_beams + (int)(c.best_at[tid] >> 32) : -1;
+    p.tokens[to] = is ? (int)(uint32_t)c.best_at[tid] : -1;
+    p.best[to] = is ? (float)unordered64(c.best_val[tid]) : -INFINITY;
   }
 }
 
@@ -276,7 +361,7 @@ template <typename T> Cut cut_of(const BeamParams& p) {
   const int64_t rows = (int64_t)p.n_groups * p.n_beams;
   const int tiles = (int)(((int64_t)p.vocab + VEC<T> - 1 + TILE<T> - 1) / TILE<T>);   // (a row may begin anywhere in 16 bytes)
   int most = std::min(MOST_SLICES, MOST_LISTS / p.n_beams);
-  const int64_t wanted = (2048 + rows - 1) / rows;
+  const int64_t wanted = (1024 + rows - 1) / rows;
   most = (int)std::min<int64_t>(most, std::max<int64_t>(1, wanted));
   const int each = (tiles + std::min(tiles, most) - 1) / std::min(tiles, most);
   return {(tiles + each - 1) / each, each};
@@ -285,15 +370,14 @@ Cut cut_of(const BeamParams& p, bool is_bf16) { return is_bf16 ? cut_of<bf16_t>(
 
 template <typename T> hipError_t run(const BeamParams& p, void* ws, hipStream_t st) {
   const Cut c = cut_of<T>(p);
-  const size_t K = p.n_out, rows_lds = (K * EACH<T> + 2 * K) * 8, group_lds = (K * K + K) * 12;
   {
     ProfScope prof_("beam_rows", st);
-    beam_rows_kernel<T><<<dim3((unsigned)(p.n_groups * p.n_beams * c.slices)), dim3(THREADS), rows_lds, st>>>(p, ws, c.slices, c.tiles);
+    beam_rows_kernel<T><<<dim3((unsigned)(p.n_groups * p.n_beams * c.slices)), dim3(THREADS), 0, st>>>(p, ws, c.slices, c.tiles);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   ProfScope prof_("beam_group", st);
-  beam_group_kernel<<<dim3((unsigned)p.n_groups), dim3(THREADS), group_lds, st>>>(p, ws, c.slices);
+  beam_group_kernel<T><<<dim3((unsigned)p.n_groups), dim3(GROUP_THREADS), 0, st>>>(p, ws, c.slices, c.tiles);
   return hipGetLastError();
 }
 
@@ -301,9 +385,11 @@ template <typename T> hipError_t run(const BeamParams& p, void* ws, hipStream_t 
 
 size_t beam_workspace_bytes(const BeamParams& p, bool is_bf16) {
   const int64_t lists = (int64_t)p.n_groups * p.n_beams * cut_of(p, is_bf16).slices;
-  return (size_t)(lists * (12 + 8 * (int64_t)p.n_out));
+  return (size_t)(lists * (12 + 4 * THREADS));
 }
-int64_t beam_blocks(const BeamParams& p, bool is_bf16) { return (int64_t)p.n_groups * p.n_beams * cut_of(p, is_bf16).slices; }
+int64_t beam_blocks(const BeamParams& p, bool is_bf16) {   // (in workgroups of 256 threads)
+  return std::max((int64_t)p.n_groups * p.n_beams * cut_of(p, is_bf16).slices, (int64_t)p.n_groups * (GROUP_THREADS / 256));
+}
 hipError_t launch_beam_topk(const BeamParams& p, bool is_bf16, void* ws, hipStream_t st) { return is_bf16 ? run<bf16_t>(p, ws, st) : run<float>(p, ws, st); }
 
 }  // namespace oomb

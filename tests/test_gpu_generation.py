@@ -241,6 +241,15 @@ def test_beam_of_equal_logits_takes_the_lowest():
     _verify_beam(x, s, 33, _beam(x, s, 33))
 
 
+def test_beam_of_zeros_of_either_sign():
+    """They are equal: the lowest place wins."""
+    for V in (200, 9000, 30000):
+        x = torch.where(torch.arange(V) % 3 == 0, 0.0, -0.0).expand(2, 2, V).contiguous()
+        x[1, :, ::7] = -1.0
+        s = torch.zeros((2, 2))
+        _verify_beam(x, s, 20, _beam(x, s, 20))
+
+
 @pytest.mark.parametrize("order", ["rising", "falling", "steps"])
 def test_beam_of_sorted_logits(order):
     """Every tile brings better ones, or none, or blocks of equal ones."""
