@@ -198,7 +198,8 @@ template <typename T> __global__ __launch_bounds__(GROUP_THREADS) void beam_grou
   const float* cells = w.cells + (int64_t)group * n_cells;
   float held[HELD];                              // (on their way while the log-sums are formed; of a row that offers nothing they are not used)
 #pragma unroll
-  for (int j = 0; j < HELD; ++j) held[j] = cells[min(tid + j * GROUP_THREADS, n_cells - 1)];
+  for (int j = 0; j < HELD; ++j)
+    if (j * GROUP_THREADS < n_cells) held[j] = cells[min(tid + j * GROUP_THREADS, n_cells - 1)];
   if (tid < lists) beam_of[tid] = (uint8_t)(tid / slices);
   if (tid == 0) { n_cell = n_hold = n_cand = 0; bound = 0; top_val = 0; }
   __syncthreads();
@@ -235,9 +236,12 @@ template <typename T> __global__ __launch_bounds__(GROUP_THREADS) void beam_grou
     return x > -INFINITY && v > -(double)INFINITY ? ordered64(v) : 0;
   };
   auto cell = [&](int i, float x) -> uint32_t { return i < n_cells ? (uint32_t)(value(beam_of[i / THREADS], x) >> 32) : 0; };
-  uint32_t mine = 0;
+  uint32_t mine = 0, keys[HELD];
 #pragma unroll
-  for (int j = 0; j < HELD; ++j) mine = max(mine, cell(tid + j * GROUP_THREADS, held[j]));
+  for (int j = 0; j < HELD; ++j) {
+    keys[j] = 0;
+    if (j * GROUP_THREADS < n_cells) mine = max(mine, keys[j] = cell(tid + j * GROUP_THREADS, held[j]));
+  }
   for (int i = tid + HELD * GROUP_THREADS; i < n_cells; i += GROUP_THREADS) mine = max(mine, cell(i, cells[i]));
   // A bound that K cells reach at least: of the waves' K-th best threads the best; to 12 bits of a mantissa
   uint32_t limit = 0;
@@ -251,16 +255,16 @@ template <typename T> __global__ __launch_bounds__(GROUP_THREADS) void beam_grou
   limit = 1;
 #pragma unroll
   for (int i = 0; i < GROUP_WAVES; ++i) limit = max(limit, wave_bound[i]);
-  auto note = [&](int i, float x) __attribute__((always_inline)) {
-    const uint32_t key = cell(i, x);
+  auto note = [&](int i, uint32_t key) __attribute__((always_inline)) {
     if (key < limit) return;
     const int to = atomicAdd(&n_cell, 1);
     if (to < CELLS) { cell_key[to] = key; cell_id[to] = i; }
   };
   if (mine >= limit) {
 #pragma unroll
-    for (int j = 0; j < HELD; ++j) note(tid + j * GROUP_THREADS, held[j]);
-    for (int i = tid + HELD * GROUP_THREADS; i < n_cells; i += GROUP_THREADS) note(i, cells[i]);
+    for (int j = 0; j < HELD; ++j)
+      if (j * GROUP_THREADS < n_cells) note(tid + j * GROUP_THREADS, keys[j]);
+    for (int i = tid + HELD * GROUP_THREADS; i < n_cells; i += GROUP_THREADS) note(i, cell(i, cells[i]));
   }
   __syncthreads();
   const int noted = n_cell;
