@@ -15,7 +15,7 @@
 // maximum is formed on the way, and sums stay far inside a float.
 //
 // The waves of a workgroup share a row block and split its tokens; long caches are cut into parts of equal work over workgroups, counted on the
-// device from the lengths as they are, and rows_combine adds a row's parts in their order.
+// device from the lengths as they are, and attn_combine adds a row's parts in their order.
 #pragma once
 #include <type_traits>
 
@@ -23,13 +23,154 @@
 #include "launch.h"
 #include "mfma_common.h"
 #include "rows.h"
-#include "rows_parts.h"
 
 namespace oomb {
 
 namespace {
 
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float MOST = 512.0f;           // of a lane's weights of a step, before the reference moves
+constexpr int NO_TOKEN = 0x7fffff00;     // position of the tokens of a tile that does not exist
+constexpr int PAD = 4;                   // floats between the rows of a merge buffer: conflict-free for 16-byte accesses
+constexpr int COMBINE_THREADS = 256;
 constexpr int WGS = 512;                 // workgroups that a call is cut into
+
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ f32x4 mfma16(const u32x4& a, const u32x4& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma4(uint32_t a, uint32_t b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a), __uint_as_float(b), c, 0, 0, 0);
+}
+__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+// what is left of a and b after their bf16 roundings, packed as `w`
+__device__ __forceinline__ void less(float& a, float& b, uint32_t w) {
+  a -= __uint_as_float(w << 16);
+  b -= __uint_as_float(w & 0xffff0000u);
+}
+// whether a half (of a word of two bf16) or a float is an infinity or a NaN
+__device__ __forceinline__ bool wild16(uint32_t w, int half) { return ((half ? w >> 16 : w) & 0x7f80u) == 0x7f80u; }
+__device__ __forceinline__ bool wild32(uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u; }
+// A page of one head: buffer loads take its base, a lane's offset and the tile's from three registers, so that addresses cost next to no
+// instruction.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t page_buffer(const unsigned char* base, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base), 0, bytes, 0x00027000);
+}
+
+// ---- how a call is cut --------------------------------------------------------------------------------------------------
+// (sequence, KV head) e has blocks of its rows, and every block is cut into the same number of parts, so that parts are of about equal work in the
+// whole call: counted on the device from the rows and lengths as they are.
+struct AttnArgs {
+  int block_rows, step;        // rows of a block; tokens that the work is counted in
+  int split;                   // whether blocks may be cut
+  int target, min_steps;       // workgroups to aim at; steps of a part at least
+  int2* parts;                 // [sequence * Hkv + KV head]: its first workgroup, parts of each of its blocks
+  float* part;                 // [workgroup][row of the block][D] sums
+  float* part_ml;              // [workgroup][row of the block][2]: reference, sum
+  int blocks;                  // workgroups of the launch
+};
+struct Load { int blocks, steps; };   // of (sequence, KV head) e; steps: a bound of what its rows see
+__device__ __forceinline__ Load load_of(const RowsParams& p, const AttnArgs& a, int e) {   // (no branch on a lane's values: a lane asks for several)
+  const Seq s = seq_of(p, e / p.Hkv);
+  const int64_t tokens = p.sel ? (int64_t)min(max(p.sel_count[e], 0), p.sel_stride) * p.P : s.len;
+  const int steps = (int)((min(tokens, (int64_t)p.max_len) + a.step - 1) / a.step);
+  return {(int)(((int64_t)s.n * p.G + a.block_rows - 1) / a.block_rows), max(steps, 1)};
+}
+struct Item { int e, block, first, index, count; };   // e, block of its rows, the block's first workgroup, this one of it, its number of parts
+// Workgroup x's item, by every lane of a wave; e < 0: there are fewer.
+__device__ __forceinline__ Item item_at(const RowsParams& p, const AttnArgs& a, int x, int lane) {
+  const int n = p.n_seqs * p.Hkv;
+  constexpr int HELD = 4;   // of a lane, loaded together (256 in all; more are asked for again)
+  Load held[HELD];
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) held[i] = 64 * i < n ? load_of(p, a, min(64 * i + lane, n - 1)) : Load{0, 1};
+  float total = 0.0f;
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    if (64 * i + lane >= n) held[i].blocks = 0;
+    total += (float)held[i].blocks * (float)held[i].steps;
+  }
+  for (int e = 64 * HELD + lane; e < n; e += 64) {
+    const Load l = load_of(p, a, e);
+    total += (float)l.blocks * (float)l.steps;
+  }
+#pragma unroll
+  for (int w = 1; w < 64; w *= 2) total += __shfl_xor(total, w, 64);
+  const int per = a.split ? max(a.min_steps, (int)(total / (float)a.target) + 1) : 0x7fffffff;   // (the same sum in every wave)
+  int before = 0;
+  for (int e0 = 0; e0 < n; e0 += 64) {
+    Load l{0, 1};
+    if (e0 >= 64 * HELD) {
+      if (e0 + lane < n) l = load_of(p, a, e0 + lane);
+    } else {
+#pragma unroll
+      for (int i = 0; i < HELD; ++i)
+        if (e0 == 64 * i) l = held[i];
+    }
+    const int parts = a.split ? (int)(((uint32_t)l.steps + (uint32_t)per - 1) / (uint32_t)per) : 1;
+    const int own = (int)min((int64_t)l.blocks * parts, (int64_t)1 << 24);   // (a launch holds fewer; row_starts may be anything)
+    int upto = own;
+#pragma unroll
+    for (int w = 1; w < 64; w *= 2) {
+      const int y = __shfl_up(upto, w, 64);
+      if (lane >= w) upto += y;
+    }
+    const uint64_t past = __ballot(before + upto > x);
+    if (past) {
+      const int at = __builtin_ctzll(past), count = __builtin_amdgcn_readlane(parts, at), blocks = __builtin_amdgcn_readlane(l.blocks, at);
+      const int start = before + __builtin_amdgcn_readlane(upto - own, at), nth = (x - start) / count, index = x - start - nth * count;
+      return {e0 + at, blocks - 1 - nth, x - index, index, count};   // (the last rows, which see the most, first)
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return {-1, 0, 0, 0, 0};
+}
+// What the sum of parts needs to know of e; by the workgroup of its last block's first part.
+__device__ __forceinline__ void note_parts(const RowsParams& p, const AttnArgs& a, const Item& it, int n_rows) {
+  if (a.split && it.index == 0 && it.block == (n_rows - 1) / a.block_rows && threadIdx.x == 0) a.parts[it.e] = make_int2(it.first, it.count);
+}
+
+// The tiles of 16 tokens that a row at max_pos sees: all up to it, or the listed ones of pages that begin at or before it.
+struct Tiles { int entries, tiles; };
+__device__ __forceinline__ Tiles tiles_to(const RowsParams& p, int e, const int32_t* list, int max_pos, int lane) {
+  if (max_pos < 0) return {0, 0};
+  if (!list) return {(max_pos >> p.log2_p) + 1, (max_pos >> 4) + 1};
+  for (int end = min(max(p.sel_count[e], 0), p.sel_stride); end > 0;) {   // (ascending: the last such entry is near the end)
+    const int base = max(end - 64, 0), at = base + lane;
+    const int id = at < end ? list[at] : -1;
+    const uint64_t seen = __ballot(id >= 0 && id <= (max_pos >> p.log2_p));
+    if (seen) {
+      const int entries = base + 64 - __builtin_clzll(seen);
+      return {entries, entries << (p.log2_p - 4)};
+    }
+    end = base;
+  }
+  return {0, 0};
+}
+
+// Pages of 64 consecutive entries, one per lane: logical page (-1: there is nothing) and where it lies in the pools.
+struct Window {
+  int first, log;
+  uint32_t lo, hi;
+  __device__ __forceinline__ void fill(const RowsParams& p, int b, const int32_t* list, int n_entries, int e0, int lane, int es) {
+    first = e0;
+    const int e = e0 + lane, n_pages = (p.max_len + p.P - 1) >> p.log2_p;
+    log = e < n_entries ? (list ? list[e] : e) : -1;
+    const int phys = log >= 0 && log < n_pages ? page_of(p, b, log) : -1;
+    if (phys < 0) log = -1;
+    const uint64_t at = (uint64_t)max(phys, 0) * (uint64_t)p.pool_page_stride * es;
+    lo = (uint32_t)at;
+    hi = (uint32_t)(at >> 32);
+  }
+  __device__ __forceinline__ int page(int e) const { return __builtin_amdgcn_readlane(log, e - first); }
+  __device__ __forceinline__ uint64_t where(int e) const {
+    return (uint32_t)__builtin_amdgcn_readlane(lo, e - first) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, e - first) << 32;
+  }
+};
 
 template <typename T, int D> struct Shape {
   static constexpr bool BF = sizeof(T) == 2;
@@ -43,16 +184,6 @@ template <typename T, int D> struct Raw {
   u32x4 k[Shape<T, D>::TILES][Shape<T, D>::KC];
   uint32_t v[Shape<T, D>::TILES][4][Shape<T, D>::VW];
 };
-
-__device__ __forceinline__ f32x4 mfma4(uint32_t a, uint32_t b, const f32x4& c) {
-  return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a), __uint_as_float(b), c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 mfma16v(const u32x4& a, const u32x4& b, const f32x4& c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-// whether a half (of a word of two bf16) or a float is an infinity or a NaN
-__device__ __forceinline__ bool wild16(uint32_t w, int half) { return ((half ? w >> 16 : w) & 0x7f80u) == 0x7f80u; }
-__device__ __forceinline__ bool wild32(uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u; }
 
 // tile i of a step: `at` is the offset of its first token in the page, `tok` that from token to token
 template <typename T, int D, bool STREAM>
@@ -91,15 +222,13 @@ __global__ __launch_bounds__(64 * W, 2) void attn_rows_kernel(RowsParams p, Attn
   constexpr int TILES = S::TILES, KC = S::KC, VW = S::VW, NJ = S::NJ, NZ = S::NZ, ES = S::ES, ROWS = 16 * RT;
   const int lane = threadIdx.x & 63, m = lane & 15, kg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int px = blockIdx.x / a.row_blocks, block = blockIdx.x - px * a.row_blocks;
-  const Part part = part_at(p, a, px, lane);
-  if (part.e < 0) return;
-  const int b = part.e / p.Hkv, g = part.e - b * p.Hkv;
+  const Item item = item_at(p, a, blockIdx.x, lane);
+  if (item.e < 0) return;
+  const int b = item.e / p.Hkv, g = item.e - b * p.Hkv;
   const Seq s = seq_of(p, b);
-  if (a.split && part.index == 0 && block == 0 && threadIdx.x == 0) a.parts[part.e] = make_int2(part.first, part.count);
   const int n_rows = s.n * p.G;
-  const int r0 = block * ROWS;
-  if (r0 >= n_rows) return;
+  note_parts(p, a, item, n_rows);
+  const int r0 = item.block * ROWS;
   const int r_last = min(r0 + ROWS, n_rows) - 1;
   const int min_pos = s.pos + r0 / p.G, max_pos = s.pos + r_last / p.G;
 
@@ -115,31 +244,11 @@ __global__ __launch_bounds__(64 * W, 2) void attn_rows_kernel(RowsParams p, Attn
     for (int c = 0; c < KC; ++c) q[rt][c] = *reinterpret_cast<const u32x4*>(row + c * (64 / ES));
   }
 
-  // the tiles that some row sees: entries of the list up to the last row's page
-  const int log_tpp = p.log2_p - 4, n_pages = (p.max_len + p.P - 1) >> p.log2_p;
-  const int32_t* list = p.sel ? p.sel + (int64_t)part.e * p.sel_stride : nullptr;
-  int n_entries = 0, n_tiles = 0;
-  if (max_pos >= 0) {
-    if (list) {
-      int e = min(max(p.sel_count[part.e], 0), p.sel_stride);
-      while (e > 0) {      // (ascending: the last entry that begins at or before max_pos is near the end)
-        const int base = max(e - 64, 0), at = base + lane;
-        const int id = at < e ? list[at] : -1;
-        const uint64_t seen = __ballot(id >= 0 && id <= (max_pos >> p.log2_p));
-        if (seen) {
-          n_entries = base + 64 - __builtin_clzll(seen);
-          break;
-        }
-        e = base;
-      }
-      n_tiles = n_entries << log_tpp;
-    } else {
-      n_tiles = (max_pos >> 4) + 1;
-      n_entries = (max_pos >> p.log2_p) + 1;
-    }
-  }
-  const int n_steps = (n_tiles + TILES - 1) / TILES;
-  const int parts = part.count * W, mine = part.index * W + wave;
+  const int log_tpp = p.log2_p - 4;
+  const int32_t* list = p.sel ? p.sel + (int64_t)item.e * p.sel_stride : nullptr;
+  const Tiles seen = tiles_to(p, item.e, list, max_pos, lane);
+  const int n_steps = (seen.tiles + TILES - 1) / TILES;
+  const int parts = item.count * W, mine = item.index * W + wave;
   const int each = (int)((uint32_t)n_steps / (uint32_t)parts), more = n_steps - each * parts;   // (one more for the first `more`)
   int u = each * mine + min(mine, more);
   const int u_end = u + each + (mine < more);
@@ -155,19 +264,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_rows_kernel(RowsParams p, Attn
   }
   const float scale = p.sm_scale * LOG2E;
 
-  // pages of 64 consecutive entries, one per lane: logical page (-1: there is nothing) and where it lies in the pools
-  int win = 0, w_log = -1;
-  uint32_t w_lo = 0, w_hi = 0;
-  auto window = [&](int e0) __attribute__((always_inline)) {
-    win = e0;
-    const int e = e0 + lane;
-    w_log = e < n_entries ? (list ? list[e] : e) : -1;
-    const int phys = w_log >= 0 && w_log < n_pages ? page_of(p, b, w_log) : -1;
-    if (phys < 0) w_log = -1;
-    const uint64_t at = (uint64_t)max(phys, 0) * (uint64_t)p.pool_page_stride * ES;
-    w_lo = (uint32_t)at;
-    w_hi = (uint32_t)(at >> 32);
-  };
+  Window win;
   const unsigned char* kbase = (const unsigned char*)p.k_pool + (int64_t)g * p.pool_head_stride * ES;
   const unsigned char* vbase = (const unsigned char*)p.v_pool + (int64_t)g * p.pool_head_stride * ES;
   const int tok = (int)p.pool_tok_stride * ES, page_bytes = (p.P - 1) * tok + D * ES;
@@ -176,9 +273,9 @@ __global__ __launch_bounds__(64 * W, 2) void attn_rows_kernel(RowsParams p, Attn
 #pragma unroll
     for (int i = 0; i < (WIDE ? 1 : TILES); ++i) {
       const int t = TILES * step + i, e = t >> log_tpp, off = (t & ((1 << log_tpp) - 1)) << 4;
-      if (e - win >= 64) window(e);
-      const int at = e - win, page = __builtin_amdgcn_readlane(w_log, at);
-      const uint64_t where = (uint32_t)__builtin_amdgcn_readlane(w_lo, at) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(w_hi, at) << 32;
+      if (e - win.first >= 64) win.fill(p, b, list, seen.entries, e, lane, ES);
+      const int page = win.page(e);
+      const uint64_t where = win.where(e);
       const __amdgpu_buffer_rsrc_t kp = page_buffer(kbase + where, page_bytes), vp = page_buffer(vbase + where, page_bytes);
       t0[i] = page < 0 ? NO_TOKEN : (page << p.log2_p) + off;
       load_tile<T, D, STREAM>(kp, vp, off * tok, tok, k_lane, v_lane, r, i);
@@ -233,7 +330,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_rows_kernel(RowsParams p, Attn
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
           if constexpr (S::BF) {
-            st[rt][i] = mfma16v(raw.k[i][c], q[rt][c], st[rt][i]);
+            st[rt][i] = mfma16(raw.k[i][c], q[rt][c], st[rt][i]);
           } else {
 #pragma unroll
             for (int x = 0; x < 4; ++x) st[rt][i] = mfma4(raw.k[i][c][x], q[rt][c][x], st[rt][i]);
@@ -263,8 +360,8 @@ __global__ __launch_bounds__(64 * W, 2) void attn_rows_kernel(RowsParams p, Attn
         float top = -INFINITY;
 #pragma unroll
         for (int e = 0; e < NZ; ++e) {
-          const bool seen = !masked || t0[e >> 2] + 4 * kg + (e & 3) <= pos[rt];
-          top = fmaxf(top, seen ? st[rt][e >> 2][e & 3] * scale : -INFINITY);
+          const bool visible = !masked || t0[e >> 2] + 4 * kg + (e & 3) <= pos[rt];
+          top = fmaxf(top, visible ? st[rt][e >> 2][e & 3] * scale : -INFINITY);
         }
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
@@ -281,7 +378,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_rows_kernel(RowsParams p, Attn
     for (int rt = 0; rt < RT; ++rt) sum[rt] += all[rt];
 
     if constexpr (S::BF) {
-      uint4 pf[RT][2];
+      u32x4 pf[RT][2];
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -292,12 +389,12 @@ __global__ __launch_bounds__(64 * W, 2) void attn_rows_kernel(RowsParams p, Attn
             w[e] = pack2_bf16(z[rt][2 * e], z[rt][2 * e + 1]);
             if (t == 0) less(z[rt][2 * e], z[rt][2 * e + 1], w[e]);
           }
-          pf[rt][t] = make_uint4(w[0], w[1], w[2], w[3]);
+          pf[rt][t] = u32x4{w[0], w[1], w[2], w[3]};
         }
       // V: word x holds dims 2 x and 2 x + 1 of this lane's; tokens (i, 2 y), (i, 2 y + 1) make word 2 i + y of an operand
 #pragma unroll
       for (int x = 0; x < VW; ++x) {
-        uint4 lo, hi;
+        u32x4 lo, hi;
         lo.x = low_halves(raw.v[0][0][x], raw.v[0][1][x]); lo.y = low_halves(raw.v[0][2][x], raw.v[0][3][x]);
         lo.z = low_halves(raw.v[TILES - 1][0][x], raw.v[TILES - 1][1][x]); lo.w = low_halves(raw.v[TILES - 1][2][x], raw.v[TILES - 1][3][x]);
         hi.x = high_halves(raw.v[0][0][x], raw.v[0][1][x]); hi.y = high_halves(raw.v[0][2][x], raw.v[0][3][x]);
@@ -350,7 +447,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_rows_kernel(RowsParams p, Attn
   int t0[AHEAD][TILES];
   // The wait for a step lets every later fetch fly on, if the compiler can count them: the steady loop fetches without a condition,
   // and the queries have landed before it.
-  if (u < u_end) window((TILES * u) >> log_tpp);
+  if (u < u_end) win.fill(p, b, list, seen.entries, (TILES * u) >> log_tpp, lane, ES);
   if (u + 2 * AHEAD <= u_end) {
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) fetch(u + k, raw[k], t0[k]);
@@ -415,7 +512,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_rows_kernel(RowsParams p, Attn
         y[0] += v.x; y[1] += v.y; y[2] += v.z; y[3] += v.w;
       }
       const int row = r0 + 16 * rt + r;
-      if (part.count > 1) {
+      if (item.count > 1) {
         const int64_t to_part = (int64_t)blockIdx.x * ROWS + 16 * rt + r;
         *reinterpret_cast<float4*>(a.part + to_part * D + d) = make_float4(y[0], y[1], y[2], y[3]);
         if (d == 0) *reinterpret_cast<float2*>(a.part_ml + to_part * 2) = make_float2(ref_r, sum_r);
@@ -431,80 +528,376 @@ __global__ __launch_bounds__(64 * W, 2) void attn_rows_kernel(RowsParams p, Attn
   }
 }
 
+// The parts of a row, in order: a workgroup per row and slice of DW dims, its threads in groups of DW / 4 that take every
+// (256 / (DW / 4))-th part each.  A compute unit takes in about 10 B/ns of lines that others wrote, so a few rows of many parts go in slices of a line.
+// MANY: rows of few parts, a group of threads a row.
+template <typename T, int D, int DW, bool MANY>
+__global__ __launch_bounds__(COMBINE_THREADS) void attn_combine_kernel(RowsParams p, AttnArgs a, int rows) {   // rows: of (sequence, KV head) that there can be at most
+  constexpr int LANES = DW / 4, GROUPS = COMBINE_THREADS / LANES;
+  __shared__ __align__(16) float lds[GROUPS][DW + PAD];
+  __shared__ float lds_ml[GROUPS][2];
+  const int grp = threadIdx.x / LANES, d = (threadIdx.x - grp * LANES) * 4;
+  int x = blockIdx.x;
+  const int slice = x % (D / DW);
+  x /= D / DW;
+  const int per_e = MANY ? (rows + GROUPS - 1) / GROUPS : rows;
+  const int e = x / per_e, row = MANY ? (x - e * per_e) * GROUPS + grp : x - e * per_e;
+  const int b = e / p.Hkv, g = e - b * p.Hkv;
+  const Seq s = seq_of(p, b);
+  if (row >= s.n * p.G) return;
+  const int2 parts = a.parts[e];
+  if (parts.y <= 1) return;
+  const int block = row / a.block_rows, last = (s.n * p.G - 1) / a.block_rows;
+  const int64_t first = parts.x + (int64_t)(last - block) * parts.y;
+  if (first < 0 || first + parts.y > a.blocks) return;   // (rows beyond what the bounds allow have no workgroups)
+  float ref = -INFINITY, sum = 0.0f, y[4] = {0.f, 0.f, 0.f, 0.f};
+  constexpr int AT_ONCE = 4;   // (loads in flight: a chain of single ones takes a microsecond a part)
+  const int step = MANY ? 1 : GROUPS;
+  for (int k0 = MANY ? 0 : grp; k0 < parts.y; k0 += AT_ONCE * step) {
+    float2 ml[AT_ONCE];
+    float4 v[AT_ONCE];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int64_t at = (first + min(k0 + i * step, parts.y - 1)) * a.block_rows + (row - block * a.block_rows);
+      ml[i] = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
+      v[i] = *reinterpret_cast<const float4*>(a.part + at * D + slice * DW + d);
+    }
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      if (k0 + i * step >= parts.y) break;
+      const float to = fmaxf(ref, ml[i].x);
+      const float f0 = ref == to ? 1.0f : __builtin_amdgcn_exp2f(ref - to), f1 = ml[i].x == to ? 1.0f : __builtin_amdgcn_exp2f(ml[i].x - to);
+      ref = to;
+      sum = sum * f0 + ml[i].y * f1;
+      y[0] = y[0] * f0 + v[i].x * f1; y[1] = y[1] * f0 + v[i].y * f1; y[2] = y[2] * f0 + v[i].z * f1; y[3] = y[3] * f0 + v[i].w * f1;
+    }
+  }
+  if constexpr (!MANY) {
+    *reinterpret_cast<float4*>(&lds[grp][d]) = make_float4(y[0], y[1], y[2], y[3]);
+    if (d == 0) { lds_ml[grp][0] = ref; lds_ml[grp][1] = sum; }
+    __syncthreads();
+    if (grp) return;
+    ref = -INFINITY; sum = 0.0f;
+    y[0] = y[1] = y[2] = y[3] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < GROUPS; ++k) ref = fmaxf(ref, lds_ml[k][0]);
+#pragma unroll
+    for (int k = 0; k < GROUPS; ++k) {
+      const float f = lds_ml[k][0] == ref ? 1.0f : __builtin_amdgcn_exp2f(lds_ml[k][0] - ref);
+      const float4 v = *reinterpret_cast<const float4*>(&lds[k][d]);
+      sum += lds_ml[k][1] * f;
+      y[0] += v.x * f; y[1] += v.y * f; y[2] += v.z * f; y[3] += v.w * f;
+    }
+  }
+  const int i = row / p.G, h = g * p.G + (row - i * p.G);
+  const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+  T* dst = (T*)p.q_out.data + (int64_t)(s.row + i) * p.q_out.tok_stride + (int64_t)h * p.q_out.head_stride + slice * DW + d;
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(pack2_bf16(y[0] * f, y[1] * f), pack2_bf16(y[2] * f, y[3] * f));
+  else *reinterpret_cast<float4*>(dst) = make_float4(y[0] * f, y[1] * f, y[2] * f, y[3] * f);
+  if (d == 0 && slice == 0) p.lse[(int64_t)h * p.n_rows + s.row + i] = sum == 0.0f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
+// ---- many rows: tiles of keys and values in the LDS -------------------------------------------------------------------------
+// Four waves of 32 query rows each share stages of 64 tokens (four tiles of 16, each inside a page), which come into the LDS by direct copies, one stage ahead.
+// With v_mfma_f32_32x32x16_bf16 and the row tiles of mfma_common.h: S^T = K Q^T from rows of K, O^T += V^T P^T from transposing reads of V, a lane
+// holds one query row.  The softmax as above.
+constexpr int TILE_ROWS = 128, TILE_STAGE = 64, TILE_THREADS = 256;
+constexpr int STAGE_BYTES = TILE_STAGE * 256;               // of K, and of V
+constexpr int TILE_LDS = 4 * STAGE_BYTES;                   // K and V, two stages
+
+template <int D> __global__ __launch_bounds__(TILE_THREADS, 2) void attn_tiles_kernel(RowsParams p, AttnArgs a) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  static_assert(D == 128, "rows of 256 bytes");
+  const int lane = threadIdx.x & 63, lq = lane & 31, hh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Item item = item_at(p, a, blockIdx.x, lane);
+  if (item.e < 0) return;
+  const int b = item.e / p.Hkv, g = item.e - b * p.Hkv;
+  const Seq s = seq_of(p, b);
+  const int n_rows = s.n * p.G;
+  note_parts(p, a, item, n_rows);
+  const int r0 = item.block * TILE_ROWS, w0 = r0 + 32 * wave;
+  const int r_last = min(r0 + TILE_ROWS, n_rows) - 1, w_last = min(w0 + 32, n_rows) - 1;
+  const bool has_rows = w0 < n_rows;
+  const int block_pos = s.pos + r_last / p.G;               // the last row's of the workgroup
+  const int min_pos = s.pos + w0 / p.G, max_pos = s.pos + w_last / p.G;
+  const int row = min(w0 + lq, r_last), token = row / p.G, head = g * p.G + (row - token * p.G), pos = s.pos + token;
+
+  u32x4 q[8];
+  {
+    const bf16_t* x = (const bf16_t*)p.q.data + (int64_t)(s.row + token) * p.q.tok_stride + (int64_t)head * p.q.head_stride + 8 * hh;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) q[k] = *reinterpret_cast<const u32x4*>(x + 16 * k);
+  }
+
+  const int log_tpp = p.log2_p - 4;
+  const int32_t* list = p.sel ? p.sel + (int64_t)item.e * p.sel_stride : nullptr;
+  const Tiles seen = tiles_to(p, item.e, list, block_pos, lane);
+  const int n_stages = (seen.tiles + 3) >> 2;
+  const int each = (int)((uint32_t)n_stages / (uint32_t)item.count), more = n_stages - each * item.count;   // (one more for the first `more`)
+  const int first = each * item.index + min(item.index, more), end = first + each + (item.index < more);
+
+  f32x16 acc[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) acc[j][x] = 0.f;
+  float ref = -INFINITY, sum = 0.0f;
+  const float scale = p.sm_scale * LOG2E;
+
+  const unsigned char* kbase = (const unsigned char*)p.k_pool + (int64_t)g * p.pool_head_stride * 2;
+  const unsigned char* vbase = (const unsigned char*)p.v_pool + (int64_t)g * p.pool_head_stride * 2;
+  const uint32_t row_bytes = (uint32_t)p.pool_tok_stride * 2;
+  uint32_t src_off[4];
+  row_tile_src_offsets16(lane, row_bytes, src_off);
+  Window win;
+  win.first = -64;
+  // Copies of a stage: wave w brings tile w of K and of V.  t0: positions of the four tiles' first tokens
+  auto copy = [&](int stage, int buf, int (&t0)[4]) __attribute__((always_inline)) {
+    const int t = 4 * stage, e0 = t >> log_tpp, e3 = (t + 3) >> log_tpp;
+    if (e3 - win.first >= 64 || win.first < 0) win.fill(p, b, list, seen.entries, e0, lane, 2);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int page = win.page((t + i) >> log_tpp), off = ((t + i) & ((1 << log_tpp) - 1)) << 4;
+      t0[i] = page < 0 ? NO_TOKEN : (page << p.log2_p) + off;
+    }
+    const int tw = t + wave, off = (tw & ((1 << log_tpp) - 1)) << 4;
+    const uint64_t where = win.where(tw >> log_tpp) + (uint64_t)off * row_bytes;
+    const uint32_t dst = buf * 2 * STAGE_BYTES + wave * 4096;
+    copy_rows16_to_lds(kbase + where, src_off, dst);
+    copy_rows16_to_lds(vbase + where, src_off, dst + STAGE_BYTES);
+  };
+
+  uint32_t na[8], tt[8];
+  row_tile_addrs(lq, hh, 0, na);
+  row_tile_tr_addrs(lane, STAGE_BYTES, tt);
+
+  // half a stage: 32 tokens from LDS offset `at`, whose tiles begin at positions ta and tb
+  auto unit = [&](const uint32_t at, const int ta, const int tb, const bool masked, int number) __attribute__((always_inline)) {
+    f32x16 st;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) st[x] = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      st = mfma32(__builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(smem + (na[k] + at))), __builtin_bit_cast(bf16x8, q[k]), st);
+    float z[16], all;
+    auto position = [&](int x) { return (x < 8 ? ta : tb) + 8 * ((x >> 2) & 1) + 4 * hh + (x & 3); };
+    auto weights = [&](float from) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < 16; ++x) z[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[x], scale, -from));
+      if (masked) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) z[x] = position(x) <= pos ? z[x] : 0.0f;
+      }
+      all = (((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]))) + (((z[8] + z[9]) + (z[10] + z[11])) + ((z[12] + z[13]) + (z[14] + z[15])));
+    };
+    weights(ref);
+    if (__any(!(all <= MOST))) {   // (a row's first tokens: its reference is -infinity)
+      float top = -INFINITY;
+#pragma unroll
+      for (int x = 0; x < 16; ++x) top = fmaxf(top, !masked || position(x) <= pos ? st[x] * scale : -INFINITY);
+      const float to = fmaxf(ref, half_max(top));
+      const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref - to);
+      ref = to;
+      sum *= f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) acc[j][x] *= f;
+      weights(to == -INFINITY ? 0.0f : to);   // (all that was seen may be -infinity: no weight)
+    }
+    sum += all;
+    u32x4 pf[2][2];                // [16 tokens][term]
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float &x = z[8 * u + 2 * e], &y = z[8 * u + 2 * e + 1];
+          const uint32_t w = pack2_bf16(x, y);
+          if (t == 0) less(x, y, w);
+          pf[u][t][e] = w;
+        }
+    // Tokens that not every row sees.  Their V is zero where nothing of it is seen (it may be anything), and so are their values that are not
+    // finite: a weight of zero does not stop those, so the rows that do see them get them below.
+    bool wild = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        u32x4 v = row_tile_tr_frag(smem, tt[2 * j], tt[2 * j + 1], at + 4096 * u);
+        if (masked) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int t = (u ? tb : ta) + 8 * (e >> 1) + 4 * hh + 2 * (e & 1);
+            uint32_t w = v[e];
+            const bool lo = wild16(w, 0), hi = wild16(w, 1), lo_part = t > min_pos, hi_part = t + 1 > min_pos, lo_un = t > max_pos, hi_un = t + 1 > max_pos;
+            wild |= (lo_part && !lo_un && lo) || (hi_part && !hi_un && hi);
+            w = lo_part && (lo_un || lo) ? w & 0xffff0000u : w;
+            w = hi_part && (hi_un || hi) ? w & 0x0000ffffu : w;
+            v[e] = w;
+          }
+        }
+#pragma unroll
+        for (int t = 1; t >= 0; --t) acc[j] = mfma32(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pf[u][t]), acc[j]);
+      }
+    if (masked && __any(wild)) {   // a lane holds dims 32 j + 8 (x / 4) + 4 hh + x % 4 of its row in acc[j][x]
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int base = u ? tb : ta, tile = number + u, e = tile >> log_tpp, off = (tile & ((1 << log_tpp) - 1)) << 4;
+        if (base >= NO_TOKEN) continue;
+        const unsigned char* page = vbase + (int64_t)page_of(p, b, list ? list[e] : e) * p.pool_page_stride * 2;
+        for (int t = 0; t < 16; ++t) {
+          if (base + t <= min_pos || base + t > max_pos) continue;
+          const bf16_t* v = reinterpret_cast<const bf16_t*>(page + (int64_t)(off + t) * row_bytes) + 4 * hh;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+              const float y = bf16_to_f32(v[32 * j + 8 * (x >> 2) + (x & 3)]);
+              if (wild32(__float_as_uint(y)) && base + t <= pos) acc[j][x] += y;
+            }
+        }
+      }
+    }
+  };
+
+  int t0[2][4];
+  if (first < end) copy(first, 0, t0[0]);
+  for (int stage = first; stage < end; stage += 2) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (stage + k >= end) break;
+      // this stage's copies have landed, and every wave is done with the other buffer
+      wait_copies<0>();
+      __syncthreads();
+      if (stage + k + 1 < end) copy(stage + k + 1, 1 - k, t0[1 - k]);
+      if (has_rows) {
+        const int last = max(max(t0[k][0], t0[k][1]), max(t0[k][2], t0[k][3]));
+        const uint32_t at = k * 2 * STAGE_BYTES;
+        if (last + 15 > min_pos) {
+          unit(at, t0[k][0], t0[k][1], true, 4 * (stage + k));
+          unit(at + 8192, t0[k][2], t0[k][3], true, 4 * (stage + k) + 2);
+        } else {
+          unit(at, t0[k][0], t0[k][1], false, 0);
+          unit(at + 8192, t0[k][2], t0[k][3], false, 0);
+        }
+      }
+    }
+  }
+
+  sum = half_sum(sum);
+  if (w0 + lq > w_last || !has_rows) return;
+  if (item.count > 1) {
+    const int64_t to = (int64_t)blockIdx.x * TILE_ROWS + 32 * wave + lq;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int x = 0; x < 16; x += 4)
+        *reinterpret_cast<float4*>(a.part + to * D + 32 * j + 2 * x + 4 * hh) = make_float4(acc[j][x], acc[j][x + 1], acc[j][x + 2], acc[j][x + 3]);
+    if (hh == 0) *reinterpret_cast<float2*>(a.part_ml + to * 2) = make_float2(ref, sum);
+    return;
+  }
+  const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
+  bf16_t* dst = (bf16_t*)p.q_out.data + (int64_t)(s.row + token) * p.q_out.tok_stride + (int64_t)head * p.q_out.head_stride + 4 * hh;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int x = 0; x < 16; x += 4)
+      *reinterpret_cast<uint2*>(dst + 32 * j + 2 * x) = make_uint2(pack2_bf16(acc[j][x] * f, acc[j][x + 1] * f), pack2_bf16(acc[j][x + 2] * f, acc[j][x + 3] * f));
+  if (hh == 0) p.lse[(int64_t)head * p.n_rows + s.row + token] = sum == 0.0f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
 // How a call is cut.
 struct Plan {
-  int rt, waves, stream, row_blocks, split, target, min_units;
-  int64_t parts;   // at most
+  int tiles, rt, waves, stream, split, block_rows, step, target, min_steps;
+  int64_t blocks;   // workgroups at most
 };
 Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   Plan c{};
   const int64_t rows = (int64_t)p.max_rows * p.G, heads = (int64_t)p.n_seqs * p.Hkv;
+  c.tiles = is_bf16 && p.D == 128 && rows >= 64 && p.pool_tok_stride <= (1 << 24);   // (offsets of a lane in a tile: 32 bits)
   c.rt = rows <= 16 || p.D == 128 ? 1 : 2;
-  c.row_blocks = (int)((rows + 16 * c.rt - 1) / (16 * c.rt));
+  c.block_rows = c.tiles ? TILE_ROWS : 16 * c.rt;
+  c.step = c.tiles ? TILE_STAGE : 32;
   int64_t tokens = p.max_len;
   if (sel_stride >= 0 && (int64_t)sel_stride * p.P < tokens) tokens = (int64_t)sel_stride * p.P;
-  const int64_t units = (tokens + 31) / 32;
-  c.min_units = 8;
-  const int64_t each = (units + c.min_units - 1) / c.min_units;
-  const int64_t room = WGS / c.row_blocks, aim = room - heads > room / 2 ? room - heads : room / 2;
-  const int64_t target = c.row_blocks <= 4 && aim < 2 * heads ? 2 * heads : aim;
-  c.split = units > 16 && each > 1 && target >= 2 * heads;
-  c.target = (int)(target < 1 ? 1 : target);
-  c.parts = !c.split ? heads : heads * each < target + heads ? heads * each : target + heads;
-  c.waves = c.split || (is_bf16 && rows > 64) ? 4 : 8;
+  const int64_t steps = (tokens + c.step - 1) / c.step;
+  // blocks of rows of all sequences at most
+  const int64_t each = (rows + c.block_rows - 1) / c.block_rows;
+  int64_t blocks = ((int64_t)p.n_rows * p.G / c.block_rows + p.n_seqs) * p.Hkv;
+  if (blocks > each * heads) blocks = each * heads;
+  c.min_steps = c.tiles ? 8 : 8;
+  c.split = steps > (c.tiles ? 16 : 16) && blocks < 4 * WGS;
+  c.target = WGS > 2 * blocks ? (int)(WGS - blocks) : WGS / 2 > blocks ? WGS / 2 : (int)blocks;
+  const int64_t most = (steps + c.min_steps - 1) / c.min_steps;
+  c.blocks = !c.split ? blocks : blocks * most < c.target + blocks ? blocks * most : c.target + blocks;
+  c.waves = c.split ? 4 : 8;
   const int64_t reach = heads * tokens, held = p.num_phys * p.Hkv * p.P;
   c.stream = (reach < held ? reach : held) * 2 * p.D * (is_bf16 ? 2 : 4) > (256ll << 20);
   return c;
 }
-// Rows that the combine has a workgroup for, and its workgroups (before slices, which only a few rows have); it runs where c.split.
-int combine_rows(const RowsParams& p, const Plan& c) { return c.row_blocks == 1 ? p.max_rows * p.G : 16 * c.rt; }
-int64_t combine_blocks(const RowsParams& p, const Plan& c) { return (int64_t)p.n_seqs * p.Hkv * c.row_blocks * combine_rows(p, c); }
+// The sum of parts runs where c.split: a workgroup per row (before slices, which only a few rows have), or per eight (head dim 64: sixteen).
+bool combine_many(const RowsParams& p) { return (int64_t)p.max_rows * p.G > 64; }
+int64_t combine_blocks(const RowsParams& p, const Plan& c) {
+  const int64_t rows = (int64_t)p.max_rows * p.G, heads = (int64_t)p.n_seqs * p.Hkv, at_once = 4 * COMBINE_THREADS / p.D;
+  return combine_many(p) ? heads * ((rows + at_once - 1) / at_once) : heads * rows;
+}
+size_t part_bytes(const RowsParams& p, const Plan& c) {
+  return !c.split ? 0 : (size_t)c.blocks * c.block_rows * (p.D + 2) * sizeof(float) + (size_t)p.n_seqs * p.Hkv * sizeof(int2);
+}
 
-template <typename T, int D, int RT, int W, bool WIDE, bool STREAM> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
-  AttnArgs a{c.row_blocks, c.split, c.target, c.min_units, nullptr, nullptr, nullptr};
-  const int64_t heads = (int64_t)p.n_seqs * p.Hkv, blocks = c.parts * c.row_blocks;
+template <typename T, int D, typename K> hipError_t run(const RowsParams& p, const Plan& c, K kernel, int threads, size_t lds, DeviceOnce& once, void* ws, hipStream_t st) {
+  AttnArgs a{c.block_rows, c.step, c.split, c.target, c.min_steps, nullptr, nullptr, nullptr, (int)c.blocks};
   if (c.split) {
     a.part = (float*)ws;
-    a.part_ml = a.part + blocks * 16 * RT * D;
-    a.parts = (int2*)(a.part_ml + blocks * 16 * RT * 2);
+    a.part_ml = a.part + c.blocks * c.block_rows * D;
+    a.parts = (int2*)(a.part_ml + c.blocks * c.block_rows * 2);
   }
   {
-    ProfScope prof_("attn_rows", st);
-    constexpr size_t lds = (size_t)(W * 16 * (D + PAD) + W * 16 * 2) * sizeof(float);
-    const auto kernel = attn_rows_kernel<T, D, RT, W, WIDE, STREAM>;
+    ProfScope prof_(c.tiles ? "attn_tiles" : "attn_rows", st);
     if (lds > 65536) {
-      static DeviceOnce once;
       const hipError_t e = ensure_max_dynamic_lds(once, (const void*)kernel, (int)lds);
       if (e != hipSuccess) return e;
     }
-    kernel<<<dim3((unsigned)blocks), dim3(64 * W), lds, st>>>(p, a);
+    kernel<<<dim3((unsigned)c.blocks), dim3(threads), lds, st>>>(p, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !c.split) return e;
   }
-  ProfScope prof_("rows_combine", st);
-  const int rows = combine_rows(p, c);
+  ProfScope prof_("attn_combine", st);
+  const int rows = p.max_rows * p.G;
   const int64_t wgs = combine_blocks(p, c);
-  if (wgs < 256 && c.parts > 32 * heads) rows_combine_kernel<T, D, 32><<<dim3((unsigned)(wgs * (D / 32))), dim3(COMBINE_THREADS), 0, st>>>(p, a, 16 * RT, rows);
-  else rows_combine_kernel<T, D, D><<<dim3((unsigned)wgs), dim3(COMBINE_THREADS), 0, st>>>(p, a, 16 * RT, rows);
+  if (combine_many(p)) attn_combine_kernel<T, D, D, true><<<dim3((unsigned)wgs), dim3(COMBINE_THREADS), 0, st>>>(p, a, rows);
+  else if (wgs < 256 && c.blocks > 32 * (int64_t)p.n_seqs * p.Hkv) attn_combine_kernel<T, D, 32, false><<<dim3((unsigned)(wgs * (D / 32))), dim3(COMBINE_THREADS), 0, st>>>(p, a, rows);
+  else attn_combine_kernel<T, D, D, false><<<dim3((unsigned)wgs), dim3(COMBINE_THREADS), 0, st>>>(p, a, rows);
   return hipGetLastError();
 }
-template <typename T, int D, int RT, int W> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
-  if (sizeof(T) == 2 && p.P < 32) return run<T, D, RT, W, sizeof(T) != 2, false>(p, c, ws, st);
-  if constexpr (RT == 1 && W == 4) {
-    if (c.stream) return run<T, D, RT, W, true, true>(p, c, ws, st);
-  }
-  return run<T, D, RT, W, true, false>(p, c, ws, st);
+template <typename T, int D, int RT, int W, bool WIDE, bool STREAM> hipError_t run_rows(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
+  static DeviceOnce once;
+  return run<T, D>(p, c, attn_rows_kernel<T, D, RT, W, WIDE, STREAM>, 64 * W, (size_t)(W * 16 * (D + PAD) + W * 16 * 2) * sizeof(float), once, ws, st);
 }
-template <typename T, int D, int RT> hipError_t run(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
-  return c.waves == 8 ? run<T, D, RT, 8>(p, c, ws, st) : run<T, D, RT, 4>(p, c, ws, st);
+template <typename T, int D, int RT, int W> hipError_t run_rows(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
+  if (sizeof(T) == 2 && p.P < 32) return run_rows<T, D, RT, W, sizeof(T) != 2, false>(p, c, ws, st);
+  if constexpr (RT == 1 && W == 4) {
+    if (c.stream) return run_rows<T, D, RT, W, true, true>(p, c, ws, st);
+  }
+  return run_rows<T, D, RT, W, true, false>(p, c, ws, st);
+}
+template <typename T, int D, int RT> hipError_t run_rows(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
+  return c.waves == 8 ? run_rows<T, D, RT, 8>(p, c, ws, st) : run_rows<T, D, RT, 4>(p, c, ws, st);
 }
 // (instantiated for one type and head dim per source file, which are compiled side by side)
 template <typename T, int D> hipError_t attn(const RowsParams& p, void* ws, hipStream_t st) {
   const Plan c = plan_of(p, sizeof(T) == 2, p.sel ? p.sel_stride : -1);
-  if constexpr (D == 64) {
-    if (c.rt == 2) return run<T, D, 2>(p, c, ws, st);
+  if constexpr (sizeof(T) == 2 && D == 128) {
+    static DeviceOnce once;
+    if (c.tiles) return run<T, D>(p, c, attn_tiles_kernel<D>, TILE_THREADS, TILE_LDS, once, ws, st);
   }
-  return run<T, D, 1>(p, c, ws, st);
+  if constexpr (D == 64) {
+    if (c.rt == 2) return run_rows<T, D, 2>(p, c, ws, st);
+  }
+  return run_rows<T, D, 1>(p, c, ws, st);
 }
 
 }  // namespace

@@ -3,14 +3,10 @@
 
 namespace oomb {
 
-size_t rows_attn_workspace_bytes(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
-  const Plan c = plan_of(p, is_bf16, sel_stride);
-  if (!c.split) return 0;
-  return (size_t)c.parts * c.row_blocks * 16 * c.rt * (p.D + 2) * sizeof(float) + (size_t)p.n_seqs * p.Hkv * sizeof(int2);
-}
+size_t rows_attn_workspace_bytes(const RowsParams& p, bool is_bf16, int32_t sel_stride) { return part_bytes(p, plan_of(p, is_bf16, sel_stride)); }
 int64_t rows_attn_blocks(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   const Plan c = plan_of(p, is_bf16, sel_stride);
-  const int64_t attn = c.parts * c.row_blocks * (c.waves / 4), combine = c.split ? combine_blocks(p, c) : 0;   // (in workgroups of 256 threads)
+  const int64_t attn = c.blocks * (c.tiles ? 1 : c.waves / 4), combine = c.split ? combine_blocks(p, c) : 0;   // (in workgroups of 256 threads)
   return attn > combine ? attn : combine;
 }
 
