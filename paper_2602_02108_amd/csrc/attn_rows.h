@@ -598,12 +598,27 @@ __global__ __launch_bounds__(COMBINE_THREADS) void attn_combine_kernel(RowsParam
 }
 
 // ---- many rows: tiles of keys and values in the LDS -------------------------------------------------------------------------
-// Four waves of 32 query rows each share stages of 64 tokens (four tiles of 16, each inside a page), which come into the LDS by direct copies, one stage ahead.
+// Four waves of 32 query rows each share stages of 64 tokens (four tiles of 16, each inside a page), which come into the LDS by direct copies a stage ahead.
 // With v_mfma_f32_32x32x16_bf16 and the row tiles of mfma_common.h: S^T = K Q^T from rows of K, O^T += V^T P^T from transposing reads of V, a lane
 // holds one query row.  The softmax as above.
 constexpr int TILE_ROWS = 128, TILE_STAGE = 64, TILE_THREADS = 256;
 constexpr int STAGE_BYTES = TILE_STAGE * 256;               // of K, and of V
-constexpr int TILE_LDS = 4 * STAGE_BYTES;                   // K and V, two stages
+constexpr int TILE_LDS = 4 * STAGE_BYTES + 16;              // K and V, two stages, a flag
+
+// the LDS at a byte
+template <typename V> __device__ __forceinline__ V lds_at(uint32_t at) { return *(const __attribute__((address_space(3))) V*)at; }
+// eight 16-bit words of one column of a row tile, from the addresses of rows 0 and 8 (mfma_common.h)
+__device__ __forceinline__ u32x4 column_frag(uint32_t a0, uint32_t a1) {
+  const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)a0));
+  const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)a1));
+  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
+}
+// The lane, asked for anew: what a loop full of operands does not need is not kept over it.
+__device__ __forceinline__ int lane_again() {
+  int l;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(l));
+  return l;
+}
 
 template <int D> __global__ __launch_bounds__(TILE_THREADS, 2) void attn_tiles_kernel(RowsParams p, AttnArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
@@ -618,13 +633,13 @@ template <int D> __global__ __launch_bounds__(TILE_THREADS, 2) void attn_tiles_k
   note_parts(p, a, item, n_rows);
   const int r0 = item.block * TILE_ROWS, w0 = r0 + 32 * wave;
   const int r_last = min(r0 + TILE_ROWS, n_rows) - 1, w_last = min(w0 + 32, n_rows) - 1;
-  const bool has_rows = w0 < n_rows;
   const int block_pos = s.pos + r_last / p.G;               // the last row's of the workgroup
-  const int min_pos = s.pos + w0 / p.G, max_pos = s.pos + w_last / p.G;
-  const int row = min(w0 + lq, r_last), token = row / p.G, head = g * p.G + (row - token * p.G), pos = s.pos + token;
+  const int min_pos = s.pos + min(w0, r_last) / p.G;
+  const int s0_pos = s.pos;
 
   u32x4 q[8];
   {
+    const int row = min(w0 + lq, r_last), token = row / p.G, head = g * p.G + (row - token * p.G);
     const bf16_t* x = (const bf16_t*)p.q.data + (int64_t)(s.row + token) * p.q.tok_stride + (int64_t)head * p.q.head_stride + 8 * hh;
 #pragma unroll
     for (int k = 0; k < 8; ++k) q[k] = *reinterpret_cast<const u32x4*>(x + 16 * k);
@@ -645,6 +660,7 @@ template <int D> __global__ __launch_bounds__(TILE_THREADS, 2) void attn_tiles_k
   float ref = -INFINITY, sum = 0.0f;
   const float scale = p.sm_scale * LOG2E;
 
+  // A stage lies in the LDS as K, then V; K comes a stage earlier.  Wave w brings tile w of both.
   const unsigned char* kbase = (const unsigned char*)p.k_pool + (int64_t)g * p.pool_head_stride * 2;
   const unsigned char* vbase = (const unsigned char*)p.v_pool + (int64_t)g * p.pool_head_stride * 2;
   const uint32_t row_bytes = (uint32_t)p.pool_tok_stride * 2;
@@ -652,161 +668,220 @@ template <int D> __global__ __launch_bounds__(TILE_THREADS, 2) void attn_tiles_k
   row_tile_src_offsets16(lane, row_bytes, src_off);
   Window win;
   win.first = -64;
-  // Copies of a stage: wave w brings tile w of K and of V.  t0: positions of the four tiles' first tokens
-  auto copy = [&](int stage, int buf, int (&t0)[4]) __attribute__((always_inline)) {
-    const int t = 4 * stage, e0 = t >> log_tpp, e3 = (t + 3) >> log_tpp;
-    if (e3 - win.first >= 64 || win.first < 0) win.fill(p, b, list, seen.entries, e0, lane, 2);
+  struct Stage { int t0[4]; uint64_t where; };   // positions of the tiles' first tokens; where this wave's tile lies in the pools
+  auto locate = [&](int stage) __attribute__((always_inline)) -> Stage {
+    Stage x;
+    if (stage >= end) return {{NO_TOKEN, NO_TOKEN, NO_TOKEN, NO_TOKEN}, 0};   // (its copies read the pool's first page, so that every stage has its copies)
+    const int t = 4 * stage, e0 = t >> log_tpp, e3 = (t + 3) >> log_tpp, tw = t + wave;
+    if (e3 - win.first >= 64) win.fill(p, b, list, seen.entries, e0, lane, 2);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int page = win.page((t + i) >> log_tpp), off = ((t + i) & ((1 << log_tpp) - 1)) << 4;
-      t0[i] = page < 0 ? NO_TOKEN : (page << p.log2_p) + off;
+      x.t0[i] = page < 0 ? NO_TOKEN : (page << p.log2_p) + off;
     }
-    const int tw = t + wave, off = (tw & ((1 << log_tpp) - 1)) << 4;
-    const uint64_t where = win.where(tw >> log_tpp) + (uint64_t)off * row_bytes;
-    const uint32_t dst = buf * 2 * STAGE_BYTES + wave * 4096;
-    copy_rows16_to_lds(kbase + where, src_off, dst);
-    copy_rows16_to_lds(vbase + where, src_off, dst + STAGE_BYTES);
+    x.where = win.where(tw >> log_tpp) + (uint64_t)((tw & ((1 << log_tpp) - 1)) << 4) * row_bytes;
+    return x;
+  };
+  auto copy_k = [&](const Stage& x, uint32_t at) __attribute__((always_inline)) { copy_rows16_to_lds(kbase + x.where, src_off, at + wave * 4096); };
+  auto copy_v = [&](const Stage& x, uint32_t at) __attribute__((always_inline)) { copy_rows16_to_lds(vbase + x.where, src_off, at + STAGE_BYTES + wave * 4096); };
+
+  uint32_t n_at, t_at;
+  {
+    uint32_t na[8], tt[8];
+    row_tile_addrs(lq, hh, 0, na);
+    row_tile_tr_addrs(lane, STAGE_BYTES, tt);
+    n_at = na[0]; t_at = tt[0];
+  }
+  // (the others of row_tile_addrs, row_tile_tr_addrs differ in bits: one instruction each, out of the compiler's sight, as kept they would not fit the registers)
+  auto with_bits = [](uint32_t x, const uint32_t bits) __attribute__((always_inline)) {
+    if (bits) asm volatile("v_xor_b32 %0, %1, %2" : "=v"(x) : "i"(bits), "v"(x));
+    return x;
   };
 
-  uint32_t na[8], tt[8];
-  row_tile_addrs(lq, hh, 0, na);
-  row_tile_tr_addrs(lane, STAGE_BYTES, tt);
-
-  // half a stage: 32 tokens from LDS offset `at`, whose tiles begin at positions ta and tb
-  auto unit = [&](const uint32_t at, const int ta, const int tb, const bool masked, int number) __attribute__((always_inline)) {
-    f32x16 st;
+  // One step of the pipeline, a unit being half a stage (32 tokens): the matrix instructions of S_{u+1} = K_{u+1} Q^T (8) and of O += V_u P_u (16) between slices
+  // of the softmax of S_u, in slots that are kept in order; operands come from the LDS in eight groups of two, two groups ahead.
+  u32x4 fr[3][2];
+  auto fetch = [&](uint32_t k_at, uint32_t v_at, int gr) __attribute__((always_inline)) {   // groups 0 .. 3: K; 4 .. 7: V of dim blocks 2 (gr % 2) + 0, 1
 #pragma unroll
-    for (int x = 0; x < 16; ++x) st[x] = 0.f;
+    for (int i = 0; i < 2; ++i) {
+      const int j = 2 * (gr & 1) + i;
+      if (gr < 4) fr[gr % 3][i] = lds_at<u32x4>(with_bits(k_at, (2 * gr + i) << 5));
+      else fr[gr % 3][i] = column_frag(with_bits(v_at, j << 6) + 4096 * ((gr >> 1) & 1), with_bits(v_at, j << 6 | 32) + 4096 * ((gr >> 1) & 1) + 2048);
+    }
+  };
+  float from = 0.0f;            // the reference, 0 while it is -infinity
+  // before a unit's weights: what a row does not see is -infinity, and the reference moves if a weight would pass 2^9
+  auto refer = [&](f32x16& s, bool masked, int ta, int tb) __attribute__((always_inline)) {
+    if (masked) {
+      const int l = lane_again(), mine = s0_pos + min(w0 + (l & 31), r_last) / p.G - 4 * (l >> 5);   // this row's position, less the lane's first token
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      st = mfma32(__builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(smem + (na[k] + at))), __builtin_bit_cast(bf16x8, q[k]), st);
-    float z[16], all;
-    auto position = [&](int x) { return (x < 8 ? ta : tb) + 8 * ((x >> 2) & 1) + 4 * hh + (x & 3); };
-    auto weights = [&](float from) __attribute__((always_inline)) {
+      for (int x = 0; x < 16; ++x) s[x] = (x < 8 ? ta : tb) + 8 * ((x >> 2) & 1) + (x & 3) <= mine ? s[x] : -INFINITY;
+    }
+    float top = s[0];
 #pragma unroll
-      for (int x = 0; x < 16; ++x) z[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[x], scale, -from));
-      if (masked) {
-#pragma unroll
-        for (int x = 0; x < 16; ++x) z[x] = position(x) <= pos ? z[x] : 0.0f;
-      }
-      all = (((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]))) + (((z[8] + z[9]) + (z[10] + z[11])) + ((z[12] + z[13]) + (z[14] + z[15])));
-    };
-    weights(ref);
-    if (__any(!(all <= MOST))) {   // (a row's first tokens: its reference is -infinity)
-      float top = -INFINITY;
-#pragma unroll
-      for (int x = 0; x < 16; ++x) top = fmaxf(top, !masked || position(x) <= pos ? st[x] * scale : -INFINITY);
+    for (int x = 1; x < 16; ++x) top = fmaxf(top, s[x]);
+    top *= scale;
+    if (__any(top > ref + 9.0f)) {
       const float to = fmaxf(ref, half_max(top));
       const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref - to);
       ref = to;
+      from = to == -INFINITY ? 0.0f : to;
       sum *= f;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int x = 0; x < 16; ++x) acc[j][x] *= f;
-      weights(to == -INFINITY ? 0.0f : to);   // (all that was seen may be -infinity: no weight)
     }
-    sum += all;
-    u32x4 pf[2][2];                // [16 tokens][term]
+  };
+  // k_buf, v_buf: LDS offsets of K of unit u + 1 and V of unit u; (ta, tb): positions of unit u's tiles
+  auto step = [&](uint32_t k_buf, uint32_t v_buf, f32x16& s_in, f32x16& s_out, bool masked, int ta, int tb) __attribute__((always_inline)) {
+    const uint32_t k_at = n_at + k_buf, v_at = t_at + v_buf;
+    u32x4 pr[2][2];              // [16 tokens][term]
+    auto weigh = [&](int e) __attribute__((always_inline)) {   // a pair of logits
+      float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s_in[2 * e], scale, -from)), y = __builtin_amdgcn_exp2f(__builtin_fmaf(s_in[2 * e + 1], scale, -from));
+      sum += x + y;
+      const uint32_t w = pack2_bf16(x, y);
+      less(x, y, w);
+      pr[e >> 2][0][e & 3] = w;
+      pr[e >> 2][1][e & 3] = pack2_bf16(x, y);
+    };
+    fetch(k_at, v_at, 0);
+    fetch(k_at, v_at, 1);
+    refer(s_in, masked, ta, tb);
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int gr = 0; gr < 8; ++gr) {
+      if (gr < 6) fetch(k_at, v_at, gr + 2);
+      // lgkmcnt: what was fetched after this group (two operations for a group of K, four for one of V)
+      if (gr < 2) __builtin_amdgcn_s_waitcnt(0xC47F);
+      else if (gr == 2) __builtin_amdgcn_s_waitcnt(0xC67F);
+      else if (gr < 6) __builtin_amdgcn_s_waitcnt(0xC87F);
+      else if (gr == 6) __builtin_amdgcn_s_waitcnt(0xC47F);
+      else __builtin_amdgcn_s_waitcnt(0xC07F);
+      __builtin_amdgcn_sched_barrier(0);   // keep the fetch ahead of this group's matrix instructions
+      if (gr < 4) {
+        if (gr == 0) {
+          f32x16 zero;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float &x = z[8 * u + 2 * e], &y = z[8 * u + 2 * e + 1];
-          const uint32_t w = pack2_bf16(x, y);
-          if (t == 0) less(x, y, w);
-          pf[u][t][e] = w;
+          for (int x = 0; x < 16; ++x) zero[x] = 0.f;
+          s_out = mfma32(__builtin_bit_cast(bf16x8, fr[0][0]), __builtin_bit_cast(bf16x8, q[0]), zero);
+        } else {
+          s_out = mfma32(__builtin_bit_cast(bf16x8, fr[gr % 3][0]), __builtin_bit_cast(bf16x8, q[2 * gr]), s_out);
         }
-    // Tokens that not every row sees.  Their V is zero where nothing of it is seen (it may be anything), and so are their values that are not
-    // finite: a weight of zero does not stop those, so the rows that do see them get them below.
-    bool wild = false;
+        weigh(gr);
+        __builtin_amdgcn_sched_barrier(0);
+        s_out = mfma32(__builtin_bit_cast(bf16x8, fr[gr % 3][1]), __builtin_bit_cast(bf16x8, q[2 * gr + 1]), s_out);
+        __builtin_amdgcn_sched_barrier(0);
+      } else {
+        const int j = 2 * (gr & 1), u = (gr >> 1) & 1;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+        for (int t = 1; t >= 0; --t) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        u32x4 v = row_tile_tr_frag(smem, tt[2 * j], tt[2 * j + 1], at + 4096 * u);
-        if (masked) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int t = (u ? tb : ta) + 8 * (e >> 1) + 4 * hh + 2 * (e & 1);
-            uint32_t w = v[e];
-            const bool lo = wild16(w, 0), hi = wild16(w, 1), lo_part = t > min_pos, hi_part = t + 1 > min_pos, lo_un = t > max_pos, hi_un = t + 1 > max_pos;
-            wild |= (lo_part && !lo_un && lo) || (hi_part && !hi_un && hi);
-            w = lo_part && (lo_un || lo) ? w & 0xffff0000u : w;
-            w = hi_part && (hi_un || hi) ? w & 0x0000ffffu : w;
-            v[e] = w;
-          }
-        }
-#pragma unroll
-        for (int t = 1; t >= 0; --t) acc[j] = mfma32(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pf[u][t]), acc[j]);
-      }
-    if (masked && __any(wild)) {   // a lane holds dims 32 j + 8 (x / 4) + 4 hh + x % 4 of its row in acc[j][x]
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int base = u ? tb : ta, tile = number + u, e = tile >> log_tpp, off = (tile & ((1 << log_tpp) - 1)) << 4;
-        if (base >= NO_TOKEN) continue;
-        const unsigned char* page = vbase + (int64_t)page_of(p, b, list ? list[e] : e) * p.pool_page_stride * 2;
-        for (int t = 0; t < 16; ++t) {
-          if (base + t <= min_pos || base + t > max_pos) continue;
-          const bf16_t* v = reinterpret_cast<const bf16_t*>(page + (int64_t)(off + t) * row_bytes) + 4 * hh;
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int x = 0; x < 16; ++x) {
-              const float y = bf16_to_f32(v[32 * j + 8 * (x >> 2) + (x & 3)]);
-              if (wild32(__float_as_uint(y)) && base + t <= pos) acc[j][x] += y;
-            }
+          for (int i = 0; i < 2; ++i) acc[j + i] = mfma32(__builtin_bit_cast(bf16x8, fr[gr % 3][i]), __builtin_bit_cast(bf16x8, pr[u][t]), acc[j + i]);
+          if (u == 0) weigh(4 + 2 * (gr & 1) + (1 - t));
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
     }
   };
-
-  int t0[2][4];
-  if (first < end) copy(first, 0, t0[0]);
-  for (int stage = first; stage < end; stage += 2) {
+  auto beyond = [&](const Stage& x, int from_pos) { return max(max(x.t0[0], x.t0[1]), max(x.t0[2], x.t0[3])) + 15 > from_pos; };   // whether it goes past a position
+  // Tokens of a stage that not every row of the workgroup sees: their V becomes zero where no row sees it (it may be anything), and so do their
+  // values that are not finite: a weight of zero does not stop those, so the rows that do see them get them at the end of the stage.
+  const int block_min = s.pos + r0 / p.G;
+  volatile int* const wild_seen = reinterpret_cast<volatile int*>(smem + 4 * STAGE_BYTES);
+  auto tame = [&](const Stage& x, uint32_t v_at) __attribute__((always_inline)) {
+    const int tid = 64 * wave + lane_again(), r = tid >> 2, i = r >> 4, t = (i == 0 ? x.t0[0] : i == 1 ? x.t0[1] : i == 2 ? x.t0[2] : x.t0[3]) + (r & 15);
+    bool wild = false;
+    if (t > block_min) {
+      uint4* at = reinterpret_cast<uint4*>(smem + v_at + STAGE_BYTES + r * 256 + (tid & 3) * 64);
+      for (int c = 0; c < 4; ++c) {
+        uint4 v = at[c];
+        uint32_t* w = reinterpret_cast<uint32_t*>(&v);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      if (stage + k >= end) break;
-      // this stage's copies have landed, and every wave is done with the other buffer
-      wait_copies<0>();
-      __syncthreads();
-      if (stage + k + 1 < end) copy(stage + k + 1, 1 - k, t0[1 - k]);
-      if (has_rows) {
-        const int last = max(max(t0[k][0], t0[k][1]), max(t0[k][2], t0[k][3]));
-        const uint32_t at = k * 2 * STAGE_BYTES;
-        if (last + 15 > min_pos) {
-          unit(at, t0[k][0], t0[k][1], true, 4 * (stage + k));
-          unit(at + 8192, t0[k][2], t0[k][3], true, 4 * (stage + k) + 2);
-        } else {
-          unit(at, t0[k][0], t0[k][1], false, 0);
-          unit(at + 8192, t0[k][2], t0[k][3], false, 0);
+        for (int e = 0; e < 4; ++e) {
+          const bool lo = wild16(w[e], 0), hi = wild16(w[e], 1);
+          wild |= t <= block_pos && (lo || hi);
+          w[e] = t > block_pos ? 0 : w[e] & (lo ? 0xffff0000u : ~0u) & (hi ? 0x0000ffffu : ~0u);
         }
+        at[c] = v;
+      }
+    }
+    if (wild) *wild_seen = 1;
+    __syncthreads();
+  };
+  f32x16 sA, sB;
+  Stage cur = locate(first), next = locate(first + 1);
+  if (first < end) {
+    if (threadIdx.x == 0) *wild_seen = 0;
+    copy_k(cur, 0);
+    copy_v(cur, 0);
+    copy_k(next, 2 * STAGE_BYTES);
+    wait_copies<8>();
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < 16; ++x) sA[x] = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sA = mfma32(__builtin_bit_cast(bf16x8, lds_at<u32x4>(with_bits(n_at, k << 5))), __builtin_bit_cast(bf16x8, q[k]), sA);
+  }
+  // Copies complete in order, four of a wave for K and four for V; each has a stage of time.  (A wave without rows works on the last row.)
+  uint32_t at = 0;               // LDS offset of this stage; the other one's: at ^ 2 STAGE_BYTES
+  for (int stage = first; stage < end; ++stage) {
+    wait_copies<4>();            // V of this stage has landed, and every wave is done with the one before
+    __syncthreads();
+    copy_v(next, at ^ 2 * STAGE_BYTES);
+    if (beyond(cur, block_min)) tame(cur, at);
+    const bool masked = beyond(cur, min_pos);
+    step(at + 8192, at, sA, sB, masked, cur.t0[0], cur.t0[1]);
+    const Stage after = locate(stage + 2);
+    wait_copies<4>();            // K of the next stage has landed, and every wave is done with this one's
+    __syncthreads();
+    copy_k(after, at);
+    step(at ^ 2 * STAGE_BYTES, at + 8192, sB, sA, masked, cur.t0[2], cur.t0[3]);
+    cur = next;
+    next = after;
+    at ^= 2 * STAGE_BYTES;
+  }
+
+  wait_copies<0>();              // (the last ones, which nobody reads, before the LDS is another's)
+  const int l = lane_again(), lr = l & 31, half = l >> 5, row = min(w0 + lr, r_last), token = row / p.G, head = g * p.G + (row - token * p.G), pos = s.pos + token;
+  if (first < end && *wild_seen) {   // a lane holds dims 32 j + 8 (x / 4) + 4 hh + x % 4 of its row in acc[j][x]
+    for (int tile = min(4 * end, seen.tiles) - 1; tile >= 4 * first; --tile) {
+      const int e = tile >> log_tpp, off = (tile & ((1 << log_tpp) - 1)) << 4, page = list ? list[e] : e;
+      const int phys = page >= 0 && page < (p.max_len + p.P - 1) >> p.log2_p ? page_of(p, b, page) : -1;
+      if (phys < 0) continue;
+      const int t0 = (page << p.log2_p) + off;
+      if (t0 + 15 <= block_min) break;
+      for (int t = max(0, block_min + 1 - t0); t < 16 && t0 + t <= block_pos; ++t) {
+        const bf16_t* v = reinterpret_cast<const bf16_t*>(vbase + (int64_t)phys * p.pool_page_stride * 2 + (int64_t)(off + t) * row_bytes) + 4 * half;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int x = 0; x < 16; ++x) {
+            const float y = bf16_to_f32(v[32 * j + 8 * (x >> 2) + (x & 3)]);
+            if (wild32(__float_as_uint(y)) && t0 + t <= pos) acc[j][x] += y;
+          }
       }
     }
   }
-
   sum = half_sum(sum);
-  if (w0 + lq > w_last || !has_rows) return;
+  if (w0 >= n_rows || w0 + lr > w_last) return;
   if (item.count > 1) {
-    const int64_t to = (int64_t)blockIdx.x * TILE_ROWS + 32 * wave + lq;
+    const int64_t to = (int64_t)blockIdx.x * TILE_ROWS + 32 * wave + lr;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int x = 0; x < 16; x += 4)
-        *reinterpret_cast<float4*>(a.part + to * D + 32 * j + 2 * x + 4 * hh) = make_float4(acc[j][x], acc[j][x + 1], acc[j][x + 2], acc[j][x + 3]);
-    if (hh == 0) *reinterpret_cast<float2*>(a.part_ml + to * 2) = make_float2(ref, sum);
+        *reinterpret_cast<float4*>(a.part + to * D + 32 * j + 2 * x + 4 * half) = make_float4(acc[j][x], acc[j][x + 1], acc[j][x + 2], acc[j][x + 3]);
+    if (half == 0) *reinterpret_cast<float2*>(a.part_ml + to * 2) = make_float2(ref, sum);
     return;
   }
   const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
-  bf16_t* dst = (bf16_t*)p.q_out.data + (int64_t)(s.row + token) * p.q_out.tok_stride + (int64_t)head * p.q_out.head_stride + 4 * hh;
+  bf16_t* dst = (bf16_t*)p.q_out.data + (int64_t)(s.row + token) * p.q_out.tok_stride + (int64_t)head * p.q_out.head_stride + 4 * half;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
 #pragma unroll
     for (int x = 0; x < 16; x += 4)
       *reinterpret_cast<uint2*>(dst + 32 * j + 2 * x) = make_uint2(pack2_bf16(acc[j][x] * f, acc[j][x + 1] * f), pack2_bf16(acc[j][x + 2] * f, acc[j][x + 3] * f));
-  if (hh == 0) p.lse[(int64_t)head * p.n_rows + s.row + token] = sum == 0.0f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * LN2;
+  if (half == 0) p.lse[(int64_t)head * p.n_rows + s.row + token] = sum == 0.0f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
 // How a call is cut.
