@@ -67,6 +67,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t page_buffer(const unsigned cha
 struct AttnArgs {
   int block_rows, step;        // rows of a block; tokens that the work is counted in
   int split;                   // whether blocks may be cut
+  int even;                    // into equal shares of the longest
   int target, min_steps;       // workgroups to aim at; steps of a part at least
   int2* parts;                 // [sequence * Hkv + KV head]: its first workgroup, parts of each of its blocks
   float* part;                 // [workgroup][row of the block][D] sums
@@ -89,18 +90,30 @@ __device__ __forceinline__ Item item_at(const RowsParams& p, const AttnArgs& a, 
 #pragma unroll
   for (int i = 0; i < HELD; ++i) held[i] = 64 * i < n ? load_of(p, a, min(64 * i + lane, n - 1)) : Load{0, 1};
   float total = 0.0f;
+  int most = 1;
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
     if (64 * i + lane >= n) held[i].blocks = 0;
     total += (float)held[i].blocks * (float)held[i].steps;
+    most = max(most, held[i].blocks ? held[i].steps : 1);
   }
   for (int e = 64 * HELD + lane; e < n; e += 64) {
     const Load l = load_of(p, a, e);
     total += (float)l.blocks * (float)l.steps;
+    most = max(most, l.blocks ? l.steps : 1);
   }
 #pragma unroll
-  for (int w = 1; w < 64; w *= 2) total += __shfl_xor(total, w, 64);
-  const int per = a.split ? max(a.min_steps, (int)(total / (float)a.target) + 1) : 0x7fffffff;   // (the same sum in every wave)
+  for (int w = 1; w < 64; w *= 2) {
+    total += __shfl_xor(total, w, 64);
+    most = max(most, __shfl_xor(most, w, 64));
+  }
+  // Steps of a part (the same in every wave).  Tiles: an equal share of the longest, as many as fit one round of workgroups (224 blocks of 250 steps in
+  // 1, 2, 3, 4 parts: 427, 362, 378, 365 us; 112 of 512: 823, 437, 434, 365); else by the work alone, so that short parts even out.
+  int per = 0x7fffffff;
+  if (a.split) {
+    const int shares = max(1, (int)((float)a.target * (float)most / max(total, 1.0f) + 1e-3f));
+    per = max(a.min_steps, a.even ? (most + shares - 1) / shares : (int)(total / (float)a.target) + 1);
+  }
   int before = 0;
   for (int e0 = 0; e0 < n; e0 += 64) {
     Load l{0, 1};
@@ -903,9 +916,9 @@ Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   const int64_t each = (rows + c.block_rows - 1) / c.block_rows;
   int64_t blocks = ((int64_t)p.n_rows * p.G / c.block_rows + p.n_seqs) * p.Hkv;
   if (blocks > each * heads) blocks = each * heads;
-  c.min_steps = c.tiles ? 8 : 8;
-  c.split = steps > (c.tiles ? 16 : 16) && blocks < 4 * WGS;
-  c.target = WGS > 2 * blocks ? (int)(WGS - blocks) : WGS / 2 > blocks ? WGS / 2 : (int)blocks;
+  c.min_steps = 8;
+  c.split = steps > 16 && blocks <= 2 * WGS;   // (more fill the chip; parts of tiles take up to 66 KB a workgroup)
+  c.target = c.tiles ? WGS : WGS > 2 * blocks ? (int)(WGS - blocks) : WGS / 2 > blocks ? WGS / 2 : (int)blocks;
   const int64_t most = (steps + c.min_steps - 1) / c.min_steps;
   c.blocks = !c.split ? blocks : blocks * most < c.target + blocks ? blocks * most : c.target + blocks;
   c.waves = c.split ? 4 : 8;
@@ -924,7 +937,7 @@ size_t part_bytes(const RowsParams& p, const Plan& c) {
 }
 
 template <typename T, int D, typename K> hipError_t run(const RowsParams& p, const Plan& c, K kernel, int threads, size_t lds, DeviceOnce& once, void* ws, hipStream_t st) {
-  AttnArgs a{c.block_rows, c.step, c.split, c.target, c.min_steps, nullptr, nullptr, nullptr, (int)c.blocks};
+  AttnArgs a{c.block_rows, c.step, c.split, c.tiles, c.target, c.min_steps, nullptr, nullptr, nullptr, (int)c.blocks};
   if (c.split) {
     a.part = (float*)ws;
     a.part_ml = a.part + c.blocks * c.block_rows * D;
