@@ -614,9 +614,12 @@ __global__ __launch_bounds__(COMBINE_THREADS) void attn_combine_kernel(RowsParam
 // Four waves of 32 query rows each share stages of 64 tokens (four tiles of 16, each inside a page), which come into the LDS by direct copies a stage ahead.
 // With v_mfma_f32_32x32x16_bf16 and the row tiles of mfma_common.h: S^T = K Q^T from rows of K, O^T += V^T P^T from transposing reads of V, a lane
 // holds one query row.  The softmax as above.
+// A row tile in the LDS: rows of 2 D bytes, granule c (16 bytes) of row r at c ^ f(r).  Head dim 128: that of mfma_common.h.  Head dim 64: two rows share a
+// line of 256 bytes, f(r) = 4 ((r / 2) % 2) + (r / 4) % 4: 16 rows read at one granule, and the 4 rows x 64 bytes of a transposing read, use every bank once.
 constexpr int TILE_ROWS = 128, TILE_STAGE = 64, TILE_THREADS = 256;
-constexpr int STAGE_BYTES = TILE_STAGE * 256;               // of K, and of V
-constexpr int TILE_LDS = 4 * STAGE_BYTES + 16;              // K and V, two stages, a flag
+template <int D> constexpr int STAGE_BYTES = TILE_STAGE * 2 * D;            // of K, and of V
+template <int D> constexpr int TILE_LDS = 4 * STAGE_BYTES<D> + 16;          // K and V, two stages, a flag
+template <int D> __device__ __forceinline__ uint32_t swizzle(uint32_t r) { return D == 128 ? row_tile_f(r) : ((r >> 1) & 1) << 2 | ((r >> 2) & 3); }
 
 // the LDS at a byte
 template <typename V> __device__ __forceinline__ V lds_at(uint32_t at) { return *(const __attribute__((address_space(3))) V*)at; }
@@ -626,6 +629,8 @@ __device__ __forceinline__ u32x4 column_frag(uint32_t a0, uint32_t a1) {
   const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)a1));
   return __builtin_shufflevector(lo, hi, 0, 1, 2, 3);
 }
+// LDS operations of a group of operands: groups of K, then of V
+template <int D> constexpr int tile_ops(int group) { return group >= D / 16 ? 0 : group < D / 32 ? 2 : 4; }
 // The lane, asked for anew: what a loop full of operands does not need is not kept over it.
 __device__ __forceinline__ int lane_again() {
   int l;
@@ -635,7 +640,8 @@ __device__ __forceinline__ int lane_again() {
 
 template <int D> __global__ __launch_bounds__(TILE_THREADS, 2) void attn_tiles_kernel(RowsParams p, AttnArgs a) {
   extern __shared__ __align__(16) unsigned char smem[];
-  static_assert(D == 128, "rows of 256 bytes");
+  constexpr int STAGE = STAGE_BYTES<D>, TILE = 32 * D, HALF = 2 * TILE;    // bytes of a stage, of a tile of 16 tokens, of a unit of 32
+  constexpr int NK = D / 16, NJ = D / 32;                                  // steps of a product over the dims; blocks of 32 of them
   const int lane = threadIdx.x & 63, lq = lane & 31, hh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Item item = item_at(p, a, blockIdx.x, lane);
@@ -650,12 +656,12 @@ template <int D> __global__ __launch_bounds__(TILE_THREADS, 2) void attn_tiles_k
   const int min_pos = s.pos + min(w0, r_last) / p.G;
   const int s0_pos = s.pos;
 
-  u32x4 q[8];
+  u32x4 q[NK];
   {
     const int row = min(w0 + lq, r_last), token = row / p.G, head = g * p.G + (row - token * p.G);
     const bf16_t* x = (const bf16_t*)p.q.data + (int64_t)(s.row + token) * p.q.tok_stride + (int64_t)head * p.q.head_stride + 8 * hh;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) q[k] = *reinterpret_cast<const u32x4*>(x + 16 * k);
+    for (int k = 0; k < NK; ++k) q[k] = *reinterpret_cast<const u32x4*>(x + 16 * k);
   }
 
   const int log_tpp = p.log2_p - 4;
@@ -665,9 +671,9 @@ template <int D> __global__ __launch_bounds__(TILE_THREADS, 2) void attn_tiles_k
   const int each = (int)((uint32_t)n_stages / (uint32_t)item.count), more = n_stages - each * item.count;   // (one more for the first `more`)
   const int first = each * item.index + min(item.index, more), end = first + each + (item.index < more);
 
-  f32x16 acc[4];
+  f32x16 acc[NJ];
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+  for (int j = 0; j < NJ; ++j)
 #pragma unroll
     for (int x = 0; x < 16; ++x) acc[j][x] = 0.f;
   float ref = -INFINITY, sum = 0.0f;
@@ -677,8 +683,13 @@ template <int D> __global__ __launch_bounds__(TILE_THREADS, 2) void attn_tiles_k
   const unsigned char* kbase = (const unsigned char*)p.k_pool + (int64_t)g * p.pool_head_stride * 2;
   const unsigned char* vbase = (const unsigned char*)p.v_pool + (int64_t)g * p.pool_head_stride * 2;
   const uint32_t row_bytes = (uint32_t)p.pool_tok_stride * 2;
-  uint32_t src_off[4];
-  row_tile_src_offsets16(lane, row_bytes, src_off);
+  uint32_t src_off[NJ];          // of a lane's granules in a tile, a KiB of the LDS each
+#pragma unroll
+  for (int c = 0; c < NJ; ++c) {
+    constexpr int PER_ROW = D / 8;
+    const uint32_t r = (64 / PER_ROW) * c + lane / PER_ROW;
+    src_off[c] = r * row_bytes + (((lane % PER_ROW) ^ swizzle<D>(r)) << 4) - 1024 * c;
+  }
   Window win;
   win.first = -64;
   struct Stage { int t0[4]; uint64_t where; };   // positions of the tiles' first tokens; where this wave's tile lies in the pools
@@ -695,31 +706,39 @@ template <int D> __global__ __launch_bounds__(TILE_THREADS, 2) void attn_tiles_k
     x.where = win.where(tw >> log_tpp) + (uint64_t)((tw & ((1 << log_tpp) - 1)) << 4) * row_bytes;
     return x;
   };
-  auto copy_k = [&](const Stage& x, uint32_t at) __attribute__((always_inline)) { copy_rows16_to_lds(kbase + x.where, src_off, at + wave * 4096); };
-  auto copy_v = [&](const Stage& x, uint32_t at) __attribute__((always_inline)) { copy_rows16_to_lds(vbase + x.where, src_off, at + STAGE_BYTES + wave * 4096); };
+  auto copy_tile = [&](const unsigned char* src, uint32_t dst) __attribute__((always_inline)) {
+    if constexpr (D == 128) copy_rows16_to_lds(src, src_off, dst);
+    else copy_rows_to_lds(src, src_off[0], src_off[1], dst);
+  };
+  auto copy_k = [&](const Stage& x, uint32_t at) __attribute__((always_inline)) { copy_tile(kbase + x.where, at + wave * TILE); };
+  auto copy_v = [&](const Stage& x, uint32_t at) __attribute__((always_inline)) { copy_tile(vbase + x.where, at + STAGE + wave * TILE); };
 
+  // operands of a lane: granule 2 k + hh of its row of K (step k); of V, for dim block j, rows 4 hh + (lane % 16) / 4 (and + 8), four dims
   uint32_t n_at, t_at;
   {
-    uint32_t na[8], tt[8];
-    row_tile_addrs(lq, hh, 0, na);
-    row_tile_tr_addrs(lane, STAGE_BYTES, tt);
-    n_at = na[0]; t_at = tt[0];
+    const uint32_t L = lane & 15, gq = lane >> 4, r = 4 * (gq >> 1) + (L >> 2);
+    n_at = lq * (2 * D) + ((swizzle<D>(lq) ^ hh) << 4);
+    t_at = STAGE + r * (2 * D) + (((2 * (gq & 1) + ((L & 3) >> 1)) ^ swizzle<D>(r)) << 4) + 8 * (L & 1);
   }
-  // (the others of row_tile_addrs, row_tile_tr_addrs differ in bits: one instruction each, out of the compiler's sight, as kept they would not fit the registers)
+  // (the other steps', blocks' and rows' addresses differ in bits: one instruction each, out of the compiler's sight, as kept they would not fit the registers)
   auto with_bits = [](uint32_t x, const uint32_t bits) __attribute__((always_inline)) {
     if (bits) asm volatile("v_xor_b32 %0, %1, %2" : "=v"(x) : "i"(bits), "v"(x));
     return x;
   };
 
-  // One step of the pipeline, a unit being half a stage (32 tokens): the matrix instructions of S_{u+1} = K_{u+1} Q^T (8) and of O += V_u P_u (16) between slices
-  // of the softmax of S_u, in slots that are kept in order; operands come from the LDS in eight groups of two, two groups ahead.
+  // One step of the pipeline, a unit being half a stage (32 tokens): the matrix instructions of S_{u+1} = K_{u+1} Q^T (D / 16) and of O += V_u P_u (D / 8) between
+  // slices of the softmax of S_u, in slots that are kept in order; operands come from the LDS in groups of two, two groups ahead.
+  constexpr int GK = NK / 2, GV = NJ, GROUPS = GK + GV;   // groups of K, then of V
   u32x4 fr[3][2];
-  auto fetch = [&](uint32_t k_at, uint32_t v_at, int gr) __attribute__((always_inline)) {   // groups 0 .. 3: K; 4 .. 7: V of dim blocks 2 (gr % 2) + 0, 1
+  auto fetch = [&](uint32_t k_at, uint32_t v_at, int gr) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int j = 2 * (gr & 1) + i;
-      if (gr < 4) fr[gr % 3][i] = lds_at<u32x4>(with_bits(k_at, (2 * gr + i) << 5));
-      else fr[gr % 3][i] = column_frag(with_bits(v_at, j << 6) + 4096 * ((gr >> 1) & 1), with_bits(v_at, j << 6 | 32) + 4096 * ((gr >> 1) & 1) + 2048);
+      if (gr < GK) {
+        fr[gr % 3][i] = lds_at<u32x4>(with_bits(k_at, (2 * gr + i) << 5));
+      } else {
+        const int u = (gr - GK) / (NJ / 2), j = 2 * ((gr - GK) % (NJ / 2)) + i;
+        fr[gr % 3][i] = column_frag(with_bits(v_at, j << 6) + TILE * u, with_bits(v_at, j << 6 | 32) + TILE * u + TILE / 2);
+      }
     }
   };
   float from = 0.0f;            // the reference, 0 while it is -infinity
@@ -741,7 +760,7 @@ template <int D> __global__ __launch_bounds__(TILE_THREADS, 2) void attn_tiles_k
       from = to == -INFINITY ? 0.0f : to;
       sum *= f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int x = 0; x < 16; ++x) acc[j][x] *= f;
     }
@@ -761,52 +780,62 @@ template <int D> __global__ __launch_bounds__(TILE_THREADS, 2) void attn_tiles_k
     fetch(k_at, v_at, 0);
     fetch(k_at, v_at, 1);
     refer(s_in, masked, ta, tb);
-#pragma unroll
-    for (int gr = 0; gr < 8; ++gr) {
-      if (gr < 6) fetch(k_at, v_at, gr + 2);
-      // lgkmcnt: what was fetched after this group (two operations for a group of K, four for one of V)
-      if (gr < 2) __builtin_amdgcn_s_waitcnt(0xC47F);
-      else if (gr == 2) __builtin_amdgcn_s_waitcnt(0xC67F);
-      else if (gr < 6) __builtin_amdgcn_s_waitcnt(0xC87F);
-      else if (gr == 6) __builtin_amdgcn_s_waitcnt(0xC47F);
-      else __builtin_amdgcn_s_waitcnt(0xC07F);
+    auto group = [&](auto number) __attribute__((always_inline)) {
+      constexpr int gr = decltype(number)::value;
+      if constexpr (gr + 2 < GROUPS) fetch(k_at, v_at, gr + 2);
+      __builtin_amdgcn_s_waitcnt(0xC07F | (tile_ops<D>(gr + 1) + tile_ops<D>(gr + 2)) << 8);   // lgkmcnt: what was fetched after this group
       __builtin_amdgcn_sched_barrier(0);   // keep the fetch ahead of this group's matrix instructions
-      if (gr < 4) {
-        if (gr == 0) {
-          f32x16 zero;
+      if constexpr (gr < GK) {
 #pragma unroll
-          for (int x = 0; x < 16; ++x) zero[x] = 0.f;
-          s_out = mfma32(__builtin_bit_cast(bf16x8, fr[0][0]), __builtin_bit_cast(bf16x8, q[0]), zero);
-        } else {
-          s_out = mfma32(__builtin_bit_cast(bf16x8, fr[gr % 3][0]), __builtin_bit_cast(bf16x8, q[2 * gr]), s_out);
+        for (int i = 0; i < 2; ++i) {
+          if (gr == 0 && i == 0) {
+            f32x16 zero;
+#pragma unroll
+            for (int x = 0; x < 16; ++x) zero[x] = 0.f;
+            s_out = mfma32(__builtin_bit_cast(bf16x8, fr[0][0]), __builtin_bit_cast(bf16x8, q[0]), zero);
+          } else {
+            s_out = mfma32(__builtin_bit_cast(bf16x8, fr[gr % 3][i]), __builtin_bit_cast(bf16x8, q[2 * gr + i]), s_out);
+          }
+          if (GK == 2) weigh(2 * gr + i);
+          else if (i == 0) weigh(gr);
+          __builtin_amdgcn_sched_barrier(0);
         }
-        weigh(gr);
-        __builtin_amdgcn_sched_barrier(0);
-        s_out = mfma32(__builtin_bit_cast(bf16x8, fr[gr % 3][1]), __builtin_bit_cast(bf16x8, q[2 * gr + 1]), s_out);
-        __builtin_amdgcn_sched_barrier(0);
       } else {
-        const int j = 2 * (gr & 1), u = (gr >> 1) & 1;
+        constexpr int u = (gr - GK) / (NJ / 2), j = 2 * ((gr - GK) % (NJ / 2));
 #pragma unroll
         for (int t = 1; t >= 0; --t) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) acc[j + i] = mfma32(__builtin_bit_cast(bf16x8, fr[gr % 3][i]), __builtin_bit_cast(bf16x8, pr[u][t]), acc[j + i]);
-          if (u == 0) weigh(4 + 2 * (gr & 1) + (1 - t));
+          if (u == 0) {
+            if (NJ == 4) weigh(4 + j + (1 - t));
+            else { weigh(4 + 2 * (1 - t)); weigh(5 + 2 * (1 - t)); }
+          }
           __builtin_amdgcn_sched_barrier(0);
         }
       }
+    };
+    group(std::integral_constant<int, 0>{});
+    group(std::integral_constant<int, 1>{});
+    group(std::integral_constant<int, 2>{});
+    group(std::integral_constant<int, 3>{});
+    if constexpr (GROUPS == 8) {
+      group(std::integral_constant<int, 4>{});
+      group(std::integral_constant<int, 5>{});
+      group(std::integral_constant<int, 6>{});
+      group(std::integral_constant<int, 7>{});
     }
   };
   auto beyond = [&](const Stage& x, int from_pos) { return max(max(x.t0[0], x.t0[1]), max(x.t0[2], x.t0[3])) + 15 > from_pos; };   // whether it goes past a position
   // Tokens of a stage that not every row of the workgroup sees: their V becomes zero where no row sees it (it may be anything), and so do their
   // values that are not finite: a weight of zero does not stop those, so the rows that do see them get them at the end of the stage.
   const int block_min = s.pos + r0 / p.G;
-  volatile int* const wild_seen = reinterpret_cast<volatile int*>(smem + 4 * STAGE_BYTES);
+  volatile int* const wild_seen = reinterpret_cast<volatile int*>(smem + 4 * STAGE);
   auto tame = [&](const Stage& x, uint32_t v_at) __attribute__((always_inline)) {
     const int tid = 64 * wave + lane_again(), r = tid >> 2, i = r >> 4, t = (i == 0 ? x.t0[0] : i == 1 ? x.t0[1] : i == 2 ? x.t0[2] : x.t0[3]) + (r & 15);
     bool wild = false;
     if (t > block_min) {
-      uint4* at = reinterpret_cast<uint4*>(smem + v_at + STAGE_BYTES + r * 256 + (tid & 3) * 64);
-      for (int c = 0; c < 4; ++c) {
+      uint4* at = reinterpret_cast<uint4*>(smem + v_at + STAGE + r * (2 * D) + (tid & 3) * (D / 2));
+      for (int c = 0; c < D / 32; ++c) {
         uint4 v = at[c];
         uint32_t* w = reinterpret_cast<uint32_t*>(&v);
 #pragma unroll
@@ -827,31 +856,31 @@ template <int D> __global__ __launch_bounds__(TILE_THREADS, 2) void attn_tiles_k
     if (threadIdx.x == 0) *wild_seen = 0;
     copy_k(cur, 0);
     copy_v(cur, 0);
-    copy_k(next, 2 * STAGE_BYTES);
-    wait_copies<8>();
+    copy_k(next, 2 * STAGE);
+    wait_copies<2 * NJ>();
     __syncthreads();
 #pragma unroll
     for (int x = 0; x < 16; ++x) sA[x] = 0.f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) sA = mfma32(__builtin_bit_cast(bf16x8, lds_at<u32x4>(with_bits(n_at, k << 5))), __builtin_bit_cast(bf16x8, q[k]), sA);
+    for (int k = 0; k < NK; ++k) sA = mfma32(__builtin_bit_cast(bf16x8, lds_at<u32x4>(with_bits(n_at, k << 5))), __builtin_bit_cast(bf16x8, q[k]), sA);
   }
-  // Copies complete in order, four of a wave for K and four for V; each has a stage of time.  (A wave without rows works on the last row.)
-  uint32_t at = 0;               // LDS offset of this stage; the other one's: at ^ 2 STAGE_BYTES
+  // Copies complete in order, as many of a wave for K as for V; each has a stage of time.  (A wave without rows works on the last row.)
+  uint32_t at = 0;               // LDS offset of this stage; the other one's: at ^ 2 STAGE
   for (int stage = first; stage < end; ++stage) {
-    wait_copies<4>();            // V of this stage has landed, and every wave is done with the one before
+    wait_copies<NJ>();            // V of this stage has landed, and every wave is done with the one before
     __syncthreads();
-    copy_v(next, at ^ 2 * STAGE_BYTES);
+    copy_v(next, at ^ 2 * STAGE);
     if (beyond(cur, block_min)) tame(cur, at);
     const bool masked = beyond(cur, min_pos);
-    step(at + 8192, at, sA, sB, masked, cur.t0[0], cur.t0[1]);
+    step(at + HALF, at, sA, sB, masked, cur.t0[0], cur.t0[1]);
     const Stage after = locate(stage + 2);
-    wait_copies<4>();            // K of the next stage has landed, and every wave is done with this one's
+    wait_copies<NJ>();            // K of the next stage has landed, and every wave is done with this one's
     __syncthreads();
     copy_k(after, at);
-    step(at ^ 2 * STAGE_BYTES, at + 8192, sB, sA, masked, cur.t0[2], cur.t0[3]);
+    step(at ^ 2 * STAGE, at + HALF, sB, sA, masked, cur.t0[2], cur.t0[3]);
     cur = next;
     next = after;
-    at ^= 2 * STAGE_BYTES;
+    at ^= 2 * STAGE;
   }
 
   wait_copies<0>();              // (the last ones, which nobody reads, before the LDS is another's)
@@ -866,7 +895,7 @@ template <int D> __global__ __launch_bounds__(TILE_THREADS, 2) void attn_tiles_k
       for (int t = max(0, block_min + 1 - t0); t < 16 && t0 + t <= block_pos; ++t) {
         const bf16_t* v = reinterpret_cast<const bf16_t*>(vbase + (int64_t)phys * p.pool_page_stride * 2 + (int64_t)(off + t) * row_bytes) + 4 * half;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < NJ; ++j)
 #pragma unroll
           for (int x = 0; x < 16; ++x) {
             const float y = bf16_to_f32(v[32 * j + 8 * (x >> 2) + (x & 3)]);
@@ -880,7 +909,7 @@ template <int D> __global__ __launch_bounds__(TILE_THREADS, 2) void attn_tiles_k
   if (item.count > 1) {
     const int64_t to = (int64_t)blockIdx.x * TILE_ROWS + 32 * wave + lr;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int x = 0; x < 16; x += 4)
         *reinterpret_cast<float4*>(a.part + to * D + 32 * j + 2 * x + 4 * half) = make_float4(acc[j][x], acc[j][x + 1], acc[j][x + 2], acc[j][x + 3]);
@@ -890,7 +919,7 @@ template <int D> __global__ __launch_bounds__(TILE_THREADS, 2) void attn_tiles_k
   const float f = sum == 0.0f ? 0.0f : 1.0f / sum;
   bf16_t* dst = (bf16_t*)p.q_out.data + (int64_t)(s.row + token) * p.q_out.tok_stride + (int64_t)head * p.q_out.head_stride + 4 * half;
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+  for (int j = 0; j < NJ; ++j)
 #pragma unroll
     for (int x = 0; x < 16; x += 4)
       *reinterpret_cast<uint2*>(dst + 32 * j + 2 * x) = make_uint2(pack2_bf16(acc[j][x] * f, acc[j][x + 1] * f), pack2_bf16(acc[j][x + 2] * f, acc[j][x + 3] * f));
@@ -905,12 +934,15 @@ struct Plan {
 Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   Plan c{};
   const int64_t rows = (int64_t)p.max_rows * p.G, heads = (int64_t)p.n_seqs * p.Hkv;
-  c.tiles = is_bf16 && p.D == 128 && rows >= 64 && p.pool_tok_stride <= (1 << 24);   // (offsets of a lane in a tile: 32 bits)
+  int64_t tokens = p.max_len;
+  if (sel_stride >= 0 && (int64_t)sel_stride * p.P < tokens) tokens = (int64_t)sel_stride * p.P;
+  const int64_t reach = heads * tokens, held = p.num_phys * p.Hkv * p.P, cache_bytes = (reach < held ? reach : held) * 2 * p.D * (is_bf16 ? 2 : 4);
+  // Tiles once the caches are read by a second row block and that costs more than their start (one sequence of 4096 tokens, 84 rows: 22 us in six blocks,
+  // 26 in tiles; of 65,536, 21 rows: 51, 40; 16 of 4096, 35 rows: 67, 39).
+  c.tiles = is_bf16 && rows > 16 && ((rows + 15) / 16 - 1) * cache_bytes > (64ll << 20) && p.pool_tok_stride <= (1 << 24);   // (offsets of a lane in a tile: 32 bits)
   c.rt = rows <= 16 || p.D == 128 ? 1 : 2;
   c.block_rows = c.tiles ? TILE_ROWS : 16 * c.rt;
   c.step = c.tiles ? TILE_STAGE : 32;
-  int64_t tokens = p.max_len;
-  if (sel_stride >= 0 && (int64_t)sel_stride * p.P < tokens) tokens = (int64_t)sel_stride * p.P;
   const int64_t steps = (tokens + c.step - 1) / c.step;
   // blocks of rows of all sequences at most
   const int64_t each = (rows + c.block_rows - 1) / c.block_rows;
@@ -922,12 +954,11 @@ Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   const int64_t most = (steps + c.min_steps - 1) / c.min_steps;
   c.blocks = !c.split ? blocks : blocks * most < c.target + blocks ? blocks * most : c.target + blocks;
   c.waves = c.split ? 4 : 8;
-  const int64_t reach = heads * tokens, held = p.num_phys * p.Hkv * p.P;
-  c.stream = (reach < held ? reach : held) * 2 * p.D * (is_bf16 ? 2 : 4) > (256ll << 20);
+  c.stream = cache_bytes > (256ll << 20);
   return c;
 }
 // The sum of parts runs where c.split: a workgroup per row (before slices, which only a few rows have), or per eight (head dim 64: sixteen).
-bool combine_many(const RowsParams& p) { return (int64_t)p.max_rows * p.G > 64; }
+bool combine_many(const RowsParams& p) { return (int64_t)p.n_seqs * p.Hkv * p.max_rows * p.G > 4096; }   // (then a row has few parts)
 int64_t combine_blocks(const RowsParams& p, const Plan& c) {
   const int64_t rows = (int64_t)p.max_rows * p.G, heads = (int64_t)p.n_seqs * p.Hkv, at_once = 4 * COMBINE_THREADS / p.D;
   return combine_many(p) ? heads * ((rows + at_once - 1) / at_once) : heads * rows;
@@ -978,9 +1009,9 @@ template <typename T, int D, int RT> hipError_t run_rows(const RowsParams& p, co
 // (instantiated for one type and head dim per source file, which are compiled side by side)
 template <typename T, int D> hipError_t attn(const RowsParams& p, void* ws, hipStream_t st) {
   const Plan c = plan_of(p, sizeof(T) == 2, p.sel ? p.sel_stride : -1);
-  if constexpr (sizeof(T) == 2 && D == 128) {
+  if constexpr (sizeof(T) == 2) {
     static DeviceOnce once;
-    if (c.tiles) return run<T, D>(p, c, attn_tiles_kernel<D>, TILE_THREADS, TILE_LDS, once, ws, st);
+    if (c.tiles) return run<T, D>(p, c, attn_tiles_kernel<D>, TILE_THREADS, TILE_LDS<D>, once, ws, st);
   }
   if constexpr (D == 64) {
     if (c.rt == 2) return run_rows<T, D, 2>(p, c, ws, st);
