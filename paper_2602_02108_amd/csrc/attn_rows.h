@@ -61,6 +61,22 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t page_buffer(const unsigned cha
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base), 0, bytes, 0x00027000);
 }
 
+// Sums, maxima and running sums over the lanes of a wave: six steps between registers (lanes 1, 2, 4, 8 to the left inside rows of 16, then row by row).
+template <typename V, typename F> __device__ __forceinline__ V wave_upto(V x, V none, F f) {
+  auto moved = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
+    return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, x), decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
+  };
+  using std::integral_constant;
+  x = f(x, moved(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{}));   // row_shr:1
+  x = f(x, moved(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{}));
+  x = f(x, moved(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{}));
+  x = f(x, moved(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{}));
+  x = f(x, moved(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{}));   // row_bcast:15 into rows 1 and 3
+  x = f(x, moved(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{}));   // row_bcast:31 into rows 2 and 3
+  return x;
+}
+template <typename V> __device__ __forceinline__ V last_lane(V x) { return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63)); }
+
 // ---- how a call is cut --------------------------------------------------------------------------------------------------
 // (sequence, KV head) e has blocks of its rows, and every block is cut into the same number of parts, so that parts are of about equal work in the
 // whole call: counted on the device from the rows and lengths as they are.
@@ -74,21 +90,21 @@ struct AttnArgs {
   float* part_ml;              // [workgroup][row of the block][2]: reference, sum
   int blocks;                  // workgroups of the launch
 };
-struct Load { int blocks, steps; };   // of (sequence, KV head) e; steps: a bound of what its rows see
+struct Load { int blocks, steps; Seq s; };   // of (sequence, KV head) e; steps: a bound of what its rows see
 __device__ __forceinline__ Load load_of(const RowsParams& p, const AttnArgs& a, int e) {   // (no branch on a lane's values: a lane asks for several)
   const Seq s = seq_of(p, e / p.Hkv);
   const int64_t tokens = p.sel ? (int64_t)min(max(p.sel_count[e], 0), p.sel_stride) * p.P : s.len;
   const int steps = (int)((min(tokens, (int64_t)p.max_len) + a.step - 1) / a.step);
-  return {(int)(((int64_t)s.n * p.G + a.block_rows - 1) / a.block_rows), max(steps, 1)};
+  return {(int)(((int64_t)s.n * p.G + a.block_rows - 1) / a.block_rows), max(steps, 1), s};
 }
-struct Item { int e, block, first, index, count; };   // e, block of its rows, the block's first workgroup, this one of it, its number of parts
+struct Item { int e, block, first, index, count; Seq s; };   // e, block of its rows, the block's first workgroup, this one of it, its number of parts
 // Workgroup x's item, by every lane of a wave; e < 0: there are fewer.
 __device__ __forceinline__ Item item_at(const RowsParams& p, const AttnArgs& a, int x, int lane) {
   const int n = p.n_seqs * p.Hkv;
   constexpr int HELD = 4;   // of a lane, loaded together (256 in all; more are asked for again)
   Load held[HELD];
 #pragma unroll
-  for (int i = 0; i < HELD; ++i) held[i] = 64 * i < n ? load_of(p, a, min(64 * i + lane, n - 1)) : Load{0, 1};
+  for (int i = 0; i < HELD; ++i) held[i] = 64 * i < n ? load_of(p, a, min(64 * i + lane, n - 1)) : Load{0, 1, {}};
   float total = 0.0f;
   int most = 1;
 #pragma unroll
@@ -102,11 +118,8 @@ __device__ __forceinline__ Item item_at(const RowsParams& p, const AttnArgs& a, 
     total += (float)l.blocks * (float)l.steps;
     most = max(most, l.blocks ? l.steps : 1);
   }
-#pragma unroll
-  for (int w = 1; w < 64; w *= 2) {
-    total += __shfl_xor(total, w, 64);
-    most = max(most, __shfl_xor(most, w, 64));
-  }
+  total = last_lane(wave_upto(total, 0.0f, [](float a, float b) { return a + b; }));
+  most = last_lane(wave_upto(most, 1, [](int a, int b) { return max(a, b); }));
   // Steps of a part (the same in every wave).  Tiles: an equal share of the longest, as many as fit one round of workgroups (224 blocks of 250 steps in
   // 1, 2, 3, 4 parts: 427, 362, 378, 365 us; 112 of 512: 823, 437, 434, 365); else by the work alone, so that short parts even out.
   int per = 0x7fffffff;
@@ -116,7 +129,7 @@ __device__ __forceinline__ Item item_at(const RowsParams& p, const AttnArgs& a, 
   }
   int before = 0;
   for (int e0 = 0; e0 < n; e0 += 64) {
-    Load l{0, 1};
+    Load l{0, 1, {}};
     if (e0 >= 64 * HELD) {
       if (e0 + lane < n) l = load_of(p, a, e0 + lane);
     } else {
@@ -126,21 +139,17 @@ __device__ __forceinline__ Item item_at(const RowsParams& p, const AttnArgs& a, 
     }
     const int parts = a.split ? (int)(((uint32_t)l.steps + (uint32_t)per - 1) / (uint32_t)per) : 1;
     const int own = (int)min((int64_t)l.blocks * parts, (int64_t)1 << 24);   // (a launch holds fewer; row_starts may be anything)
-    int upto = own;
-#pragma unroll
-    for (int w = 1; w < 64; w *= 2) {
-      const int y = __shfl_up(upto, w, 64);
-      if (lane >= w) upto += y;
-    }
+    const int upto = wave_upto(own, 0, [](int a, int b) { return a + b; });
     const uint64_t past = __ballot(before + upto > x);
     if (past) {
       const int at = __builtin_ctzll(past), count = __builtin_amdgcn_readlane(parts, at), blocks = __builtin_amdgcn_readlane(l.blocks, at);
       const int start = before + __builtin_amdgcn_readlane(upto - own, at), nth = (x - start) / count, index = x - start - nth * count;
-      return {e0 + at, blocks - 1 - nth, x - index, index, count};   // (the last rows, which see the most, first)
+      return {e0 + at, blocks - 1 - nth, x - index, index, count,     // (the last rows, which see the most, first)
+              {__builtin_amdgcn_readlane(l.s.row, at), __builtin_amdgcn_readlane(l.s.n, at), __builtin_amdgcn_readlane(l.s.pos, at), 0}};
     }
     before += __builtin_amdgcn_readlane(upto, 63);
   }
-  return {-1, 0, 0, 0, 0};
+  return {-1, 0, 0, 0, 0, {}};
 }
 // What the sum of parts needs to know of e; by the workgroup of its last block's first part.
 __device__ __forceinline__ void note_parts(const RowsParams& p, const AttnArgs& a, const Item& it, int n_rows) {
@@ -238,7 +247,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_rows_kernel(RowsParams p, Attn
   const Item item = item_at(p, a, blockIdx.x, lane);
   if (item.e < 0) return;
   const int b = item.e / p.Hkv, g = item.e - b * p.Hkv;
-  const Seq s = seq_of(p, b);
+  const Seq s = item.s;
   const int n_rows = s.n * p.G;
   note_parts(p, a, item, n_rows);
   const int r0 = item.block * ROWS;
@@ -556,10 +565,9 @@ __global__ __launch_bounds__(COMBINE_THREADS) void attn_combine_kernel(RowsParam
   const int per_e = MANY ? (rows + GROUPS - 1) / GROUPS : rows;
   const int e = x / per_e, row = MANY ? (x - e * per_e) * GROUPS + grp : x - e * per_e;
   const int b = e / p.Hkv, g = e - b * p.Hkv;
-  const Seq s = seq_of(p, b);
-  if (row >= s.n * p.G) return;
   const int2 parts = a.parts[e];
-  if (parts.y <= 1) return;
+  const Seq s = seq_of(p, b);
+  if (row >= s.n * p.G || parts.y <= 1) return;   // (without rows, nobody wrote parts)
   const int block = row / a.block_rows, last = (s.n * p.G - 1) / a.block_rows;
   const int64_t first = parts.x + (int64_t)(last - block) * parts.y;
   if (first < 0 || first + parts.y > a.blocks) return;   // (rows beyond what the bounds allow have no workgroups)
@@ -647,7 +655,7 @@ template <int D> __global__ __launch_bounds__(TILE_THREADS, 2) void attn_tiles_k
   const Item item = item_at(p, a, blockIdx.x, lane);
   if (item.e < 0) return;
   const int b = item.e / p.Hkv, g = item.e - b * p.Hkv;
-  const Seq s = seq_of(p, b);
+  const Seq s = item.s;
   const int n_rows = s.n * p.G;
   note_parts(p, a, item, n_rows);
   const int r0 = item.block * TILE_ROWS, w0 = r0 + 32 * wave;
@@ -948,9 +956,9 @@ Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   const int64_t each = (rows + c.block_rows - 1) / c.block_rows;
   int64_t blocks = ((int64_t)p.n_rows * p.G / c.block_rows + p.n_seqs) * p.Hkv;
   if (blocks > each * heads) blocks = each * heads;
-  c.min_steps = 8;
+  c.min_steps = c.tiles ? 8 : 4;
   c.split = steps > 16 && blocks <= 2 * WGS;   // (more fill the chip; parts of tiles take up to 66 KB a workgroup)
-  c.target = c.tiles ? WGS : WGS > 2 * blocks ? (int)(WGS - blocks) : WGS / 2 > blocks ? WGS / 2 : (int)blocks;
+  c.target = (int)(c.tiles ? WGS : blocks < WGS ? WGS - blocks / 2 : blocks);   // (parts come out rounded up: half a part more for each block)
   const int64_t most = (steps + c.min_steps - 1) / c.min_steps;
   c.blocks = !c.split ? blocks : blocks * most < c.target + blocks ? blocks * most : c.target + blocks;
   c.waves = c.split ? 4 : 8;
