@@ -104,7 +104,7 @@ oomb_status oomb_page_copy(const oomb_copy_desc* d, void* const* pools, const in
   if (d->tok_stride != 0 && d->tok_stride < d->row_bytes) return OOMB_ERR_INVALID_ARG;
   if ((d->num_phys_pages > 1 && d->page_stride < d->row_bytes) || (d->n_heads > 1 && d->head_stride < d->row_bytes)) return OOMB_ERR_INVALID_ARG;
   if (d->num_phys_pages > (1 << 30) || d->max_copies > INT32_MAX || (int64_t)d->page_size * d->row_bytes > INT32_MAX - 65536) return OOMB_ERR_UNSUPPORTED;
-  if (d->max_copies > INT64_MAX / 128 / d->n_heads) return OOMB_ERR_UNSUPPORTED;
+  if (d->n_heads > 65535 / COPY_POOLS) return OOMB_ERR_UNSUPPORTED;
   for (int32_t i = 0; i < d->n_pools; ++i)
     if (!pools[i] || !aligned(pools[i], 16)) return OOMB_ERR_INVALID_ARG;
   if (d->max_copies == 0) return OOMB_OK;

@@ -2,6 +2,7 @@
 // moved to the front (compact).  Results do not depend on scheduling: free pages go out in ascending order, by ranks counted with prefix sums, and what is
 // added to a reference count is added as integers.
 #include "gen.h"
+#include "wave.h"
 
 namespace oomb {
 
@@ -30,12 +31,7 @@ __host__ __device__ ForkWs fork_ws(void* ws, int32_t n_seqs, int32_t n_out) {
 template <int THREADS> __device__ __forceinline__ int block_scan(int x, int* sums, int& total) {
   constexpr int WAVES = THREADS / 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int upto = x;
-#pragma unroll
-  for (int w = 1; w < 64; w *= 2) {
-    const int y = __shfl_up(upto, w, 64);
-    if (lane >= w) upto += y;
-  }
+  const int upto = wave_upto(x, 0, [](int a, int b) { return a + b; });
   __syncthreads();
   if (lane == 63) sums[wave] = upto;
   __syncthreads();
@@ -43,8 +39,9 @@ template <int THREADS> __device__ __forceinline__ int block_scan(int x, int* sum
   total = 0;
 #pragma unroll
   for (int w = 0; w < WAVES; ++w) {
-    before += w < wave ? sums[w] : 0;
-    total += sums[w];
+    const int y = sums[w];
+    before += w < wave ? y : 0;
+    total += y;
   }
   return before + upto - x;
 }
@@ -182,32 +179,33 @@ __global__ __launch_bounds__(ROW_THREADS) void fork_rows_kernel(ForkParams p, vo
 }
 
 // ---- copies ---------------------------------------------------------------------------------------------------------------
-// A workgroup takes one head of a page of one pool at a time, 16 bytes a thread, four loads in flight.
-__global__ __launch_bounds__(COPY_THREADS) void page_copy_kernel(CopyParams p, CopyPools pools, int n_pools) {
+// A workgroup takes one head of a page of one pool at a time, 16 bytes a thread, eight loads in flight.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__global__ __launch_bounds__(COPY_THREADS) void page_copy_kernel(CopyParams p, CopyPools pools) {
+  const int pool = blockIdx.y / p.n_heads, head = blockIdx.y - pool * p.n_heads;
   const int n = p.count ? min(max(*p.count, 0), p.n_copies) : p.n_copies;
-  const int64_t items = (int64_t)n * n_pools * p.n_heads;
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const int64_t x = item / p.n_heads;
-    const int head = (int)(item - x * p.n_heads), i = (int)(x / n_pools), pool = (int)(x - (int64_t)i * n_pools);
+  unsigned char* const base = pools.at[pool] + head * p.head_stride;
+  const bool whole = p.tok_stride == 0 || p.tok_stride == p.row_bytes;
+  const int row_units = p.row_bytes / 16;
+  for (int i = blockIdx.x; i < n; i += gridDim.x) {
     const int src = p.copies[3 * (int64_t)i], dst = p.copies[3 * (int64_t)i + 1], tokens = min(p.copies[3 * (int64_t)i + 2], p.page);
     if (src < 0 || src >= p.num_phys || dst < 0 || dst >= p.num_phys || src == dst || tokens <= 0) continue;
-    const unsigned char* from = pools.at[pool] + src * p.page_stride + head * p.head_stride;
-    unsigned char* to = pools.at[pool] + dst * p.page_stride + head * p.head_stride;
-    const bool whole = p.tok_stride == 0 || p.tok_stride == p.row_bytes;
-    const int row_units = p.row_bytes / 16, units = p.tok_stride == 0 ? row_units : tokens * row_units;
-    constexpr int AT_ONCE = 4;
+    const unsigned char* from = base + src * p.page_stride;
+    unsigned char* to = base + dst * p.page_stride;
+    const int units = p.tok_stride == 0 ? row_units : tokens * row_units;
+    constexpr int AT_ONCE = 8;
     for (int u0 = threadIdx.x; u0 < units; u0 += AT_ONCE * COPY_THREADS) {
-      uint4 v[AT_ONCE];
+      u32x4 v[AT_ONCE];
       int64_t at[AT_ONCE];
 #pragma unroll
       for (int j = 0; j < AT_ONCE; ++j) {
         const int u = min(u0 + j * COPY_THREADS, units - 1);
         at[j] = whole ? (int64_t)u * 16 : (u / row_units) * p.tok_stride + (u % row_units) * 16;
-        v[j] = *reinterpret_cast<const uint4*>(from + at[j]);
+        if (u0 + j * COPY_THREADS < units) v[j] = *reinterpret_cast<const u32x4*>(from + at[j]);
       }
 #pragma unroll
       for (int j = 0; j < AT_ONCE; ++j)
-        if (u0 + j * COPY_THREADS < units) *reinterpret_cast<uint4*>(to + at[j]) = v[j];
+        if (u0 + j * COPY_THREADS < units) *reinterpret_cast<u32x4*>(to + at[j]) = v[j];
     }
   }
 }
@@ -316,12 +314,218 @@ __global__ __launch_bounds__(ROW_THREADS) void compact_rows_kernel(CompactParams
   }
 }
 
+// ---- few pages and sequences: a fork, or a compact, in one workgroup -------------------------------------------------------
+// The reference counts lie in the LDS, and what needs them there needs no second launch (a table of 64 rows of 34: 9 us in two, 6 in one).
+constexpr int SMALL_PAGES = 8192, SMALL_SEQS = 1024, SMALL_ENTRIES = 65536;
+constexpr int SMALL_EACH = SMALL_PAGES / PLAN_THREADS;
+// row of entry e of a table of `cols` columns: magic = ceil(2^32 / cols), exact below 2^16 entries
+__device__ __forceinline__ int row_of(int e, int cols, uint32_t magic) { return cols == 1 ? e : (int)__umulhi((uint32_t)e, magic); }
+
+__global__ __launch_bounds__(PLAN_THREADS) void fork_small_kernel(ForkParams p, uint32_t in_magic, uint32_t out_magic) {
+  extern __shared__ __align__(16) int room[];
+  __shared__ int sums[PLAN_THREADS / 64];
+  int* const count = room;                                  // [num_phys]
+  Child* const child = (Child*)(count + ((p.num_phys + 3) & ~3));   // [n_out]
+  Parent* const parent = (Parent*)(child + p.n_out);        // [n_seqs]
+  int* const first = (int*)(parent + p.n_seqs);             // [n_seqs]
+  int* const last = first + p.n_seqs;                       // [n_seqs] partly filled page
+  uint16_t* const free_pages = (uint16_t*)(last + p.n_seqs);   // [num_phys]
+  const int tid = threadIdx.x, P = 1 << p.log2_p, cap = p.cols << p.log2_p, out_cap = p.out_cols << p.log2_p;
+  // loads that wait for nothing
+  const int s_of = tid < p.n_out ? p.parents[tid] : -1, more = tid < p.n_out && p.grow ? max(p.grow[tid], 0) : 0;
+  const int len = tid < p.n_seqs ? min(max(p.lens[tid], 0), cap) : 0, was = min(len, out_cap);
+  const int each = (p.num_phys + PLAN_THREADS - 1) / PLAN_THREADS;
+  int refs[SMALL_EACH];
+#pragma unroll
+  for (int j = 0; j < SMALL_EACH; ++j)
+    if (j < each) refs[j] = tid * each + j < p.num_phys ? p.refs[tid * each + j] : 1;
+  const int page = was & (P - 1) ? valid(p, p.tables[(int64_t)tid * p.stride + (was >> p.log2_p)]) : -1;
+  if (tid < p.n_seqs) {
+    parent[tid] = {0, 0, (len + P - 1) >> p.log2_p, was >> p.log2_p};
+    first[tid] = 0x7fffffff;
+    last[tid] = page;
+  }
+  int n_free = 0;
+#pragma unroll
+  for (int j = 0; j < SMALL_EACH; ++j)
+    if (j < each) {
+      if (tid * each + j < p.num_phys) count[tid * each + j] = refs[j];
+      n_free += refs[j] == 0;
+    }
+  __syncthreads();
+  const bool of = s_of >= 0 && s_of < p.n_seqs;
+  if (of) {
+    atomicAdd(&parent[s_of].children, 1);
+    atomicMin(&first[s_of], tid);
+  }
+  int total_free;
+  int k = block_scan<PLAN_THREADS>(n_free, sums, total_free);
+#pragma unroll
+  for (int j = 0; j < SMALL_EACH; ++j)
+    if (j < each && refs[j] == 0) free_pages[k++] = (uint16_t)(tid * each + j);
+  if (tid < p.n_seqs) parent[tid].keeps = parent[tid].children > 0 && page >= 0 && count[page] <= 1;
+  Child c{0, 0, 0, 0};
+  int need = 0;
+  if (tid < p.n_out) {
+    if (of) {
+      const int l = last[s_of];
+      c.copied = l >= 0 && (first[s_of] != tid || count[l] > 1);
+      c.was = min(min(max(p.lens[s_of], 0), cap), out_cap);
+    }
+    if (of || s_of == OOMB_FORK_BEGINS) c.now = (int)min((int64_t)c.was + more, (int64_t)out_cap);
+    need = c.copied + ((c.now + P - 1) >> p.log2_p) - ((c.was + P - 1) >> p.log2_p);
+  }
+  int total;
+  c.first = block_scan<PLAN_THREADS>(need, sums, total);
+  if (tid < p.n_out) child[tid] = c;
+  __syncthreads();
+  if (tid < p.n_out) {
+    p.lens_out[tid] = c.now;
+    const bool copy = c.copied && c.first < total_free;
+    p.copies[3 * tid] = copy ? last[s_of] : -1;
+    p.copies[3 * tid + 1] = copy ? free_pages[c.first] : -1;
+    p.copies[3 * tid + 2] = copy ? c.was & (P - 1) : 0;
+  }
+  if (tid == 0) {
+    p.status[0] = min(total, total_free);
+    p.status[1] = total - min(total, total_free);
+  }
+  // the children's rows, then what the parents' rows counted; four entries of a thread at a time
+  constexpr int AT_ONCE = 4;
+  for (int e0 = tid; e0 < p.n_out * p.out_cols; e0 += AT_ONCE * PLAN_THREADS) {
+    int x[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int e = e0 + j * PLAN_THREADS, row = row_of(e, p.out_cols, out_magic), l = e - row * p.out_cols;
+      x[j] = -1;
+      if (e < p.n_out * p.out_cols) {
+        const Child h = child[row];
+        if (l < ((h.was + P - 1) >> p.log2_p) - h.copied) x[j] = valid(p, p.tables[(int64_t)p.parents[row] * p.stride + l]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int e = e0 + j * PLAN_THREADS, row = row_of(e, p.out_cols, out_magic), l = e - row * p.out_cols;
+      if (e >= p.n_out * p.out_cols) break;
+      const Child h = child[row];
+      const int kept = ((h.was + P - 1) >> p.log2_p) - h.copied;
+      if (l >= kept && l < (h.now + P - 1) >> p.log2_p && h.first + l - kept < total_free) {
+        x[j] = free_pages[h.first + l - kept];
+        atomicAdd(&count[x[j]], 1);
+      }
+      p.tables_out[(int64_t)row * p.out_stride + l] = x[j];
+    }
+  }
+  for (int e0 = tid; e0 < p.n_seqs * p.cols; e0 += AT_ONCE * PLAN_THREADS) {
+    int x[AT_ONCE], more_of[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int e = e0 + j * PLAN_THREADS, row = row_of(e, p.cols, in_magic), l = e - row * p.cols;
+      x[j] = -1;
+      more_of[j] = 0;
+      if (e < p.n_seqs * p.cols) {
+        const Parent r = parent[row];
+        more_of[j] = l >= r.pages ? 0 : (l < r.held ? r.children : l == r.held ? r.keeps : 0) - 1;
+        if (more_of[j]) x[j] = valid(p, p.tables[(int64_t)row * p.stride + l]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j)
+      if (x[j] >= 0) atomicAdd(&count[x[j]], more_of[j]);
+  }
+  __syncthreads();
+  for (int i = tid; i < p.num_phys; i += PLAN_THREADS) p.refs_out[i] = count[i];
+}
+
+__global__ __launch_bounds__(PLAN_THREADS) void compact_small_kernel(CompactParams p, uint32_t magic) {
+  extern __shared__ __align__(16) int room[];
+  __shared__ int sums[PLAN_THREADS / 64];
+  int* const count = room;                                  // [num_phys]
+  int* const becomes = count + p.num_phys;                  // [num_phys]: -1, itself, or num_phys + i if it is the i-th to move
+  uint16_t* const src = (uint16_t*)(becomes + p.num_phys);  // [num_phys / 2]
+  uint16_t* const dst = src + p.num_phys / 2;
+  const int tid = threadIdx.x, each = (p.num_phys + PLAN_THREADS - 1) / PLAN_THREADS;
+  int refs[SMALL_EACH], used = 0, n, low;
+#pragma unroll
+  for (int j = 0; j < SMALL_EACH; ++j)
+    if (j < each) refs[j] = tid * each + j < p.num_phys ? p.refs[tid * each + j] : 0;
+#pragma unroll
+  for (int j = 0; j < SMALL_EACH; ++j)
+    if (j < each) {
+      if (tid * each + j < p.num_phys) count[tid * each + j] = refs[j];
+      used += refs[j] > 0;
+    }
+  int rank = block_scan<PLAN_THREADS>(used, sums, n);
+  int below = 0;
+#pragma unroll
+  for (int j = 0; j < SMALL_EACH; ++j)
+    if (j < each) below += refs[j] > 0 && tid * each + j < n;
+  block_scan<PLAN_THREADS>(below, sums, low);
+#pragma unroll
+  for (int j = 0; j < SMALL_EACH; ++j) {
+    const int i = tid * each + j;
+    if (j >= each || i >= p.num_phys) break;
+    if (refs[j] > 0) {
+      becomes[i] = i < n ? i : p.num_phys + rank - low;
+      if (i >= n) src[rank - low] = (uint16_t)i;
+    } else {
+      becomes[i] = -1;
+      if (i < n) dst[i - rank] = (uint16_t)i;
+    }
+    rank += refs[j] > 0;
+  }
+  __syncthreads();
+  const int moves = n - low;
+  for (int i = tid; i < p.num_phys; i += PLAN_THREADS) {
+    const int b = becomes[i];
+    p.map[i] = b < p.num_phys ? b : dst[b - p.num_phys];
+    if (b >= 0 || i >= n) p.refs_out[i] = b == i ? count[i] : 0;   // (holes below n: with the moves)
+  }
+  for (int k = tid; k < moves; k += PLAN_THREADS) {
+    p.moves[3 * k] = src[k];
+    p.moves[3 * k + 1] = dst[k];
+    p.moves[3 * k + 2] = p.page;
+    p.refs_out[dst[k]] = count[src[k]];
+  }
+  if (tid == 0) {
+    p.status[0] = n;
+    p.status[1] = moves;
+  }
+  constexpr int AT_ONCE = 4;
+  for (int e0 = tid; e0 < p.n_seqs * p.cols; e0 += AT_ONCE * PLAN_THREADS) {
+    int x[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int e = e0 + j * PLAN_THREADS, row = row_of(e, p.cols, magic), l = e - row * p.cols;
+      x[j] = -1;
+      if (e < p.n_seqs * p.cols) {
+        const int len = min(max(p.lens[row], 0), p.cols << p.log2_p);
+        x[j] = p.tables[(int64_t)row * p.stride + l];
+        if (l >= (len + p.page - 1) >> p.log2_p) x[j] = -1;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int e = e0 + j * PLAN_THREADS, row = row_of(e, p.cols, magic), l = e - row * p.cols;
+      if (e >= p.n_seqs * p.cols) break;
+      int y = x[j] >= 0 && x[j] < p.num_phys ? becomes[x[j]] : -1;
+      if (y >= p.num_phys) y = dst[y - p.num_phys];
+      p.tables_out[(int64_t)row * p.out_stride + l] = y;
+    }
+  }
+}
+
 int pieces_of(int32_t cols) { return (cols + ROW_ENTRIES - 1) / ROW_ENTRIES; }
 int fork_pieces(const ForkParams& p) { return pieces_of(p.cols > p.out_cols ? p.cols : p.out_cols); }
 int compact_move_blocks(const CompactParams& p) {
   const int most = (p.num_phys / 2 + ROW_THREADS - 1) / ROW_THREADS;
   return most < 1 ? 1 : most < 64 ? most : 64;
 }
+
+bool few(int64_t num_phys, int64_t n_seqs, int64_t n_out, int64_t entries) {
+  return num_phys <= SMALL_PAGES && n_seqs <= SMALL_SEQS && n_out <= SMALL_SEQS && entries <= SMALL_ENTRIES;
+}
+uint32_t magic_of(int32_t cols) { return (uint32_t)(((1ull << 32) + cols - 1) / cols); }
 
 }  // namespace
 
@@ -330,6 +534,18 @@ size_t fork_workspace_bytes(int32_t n_seqs, int32_t n_out, int64_t num_phys) {
 }
 int64_t fork_blocks(const ForkParams& p) { return ((int64_t)p.n_out + p.n_seqs) * fork_pieces(p); }
 hipError_t launch_page_fork(const ForkParams& p, void* ws, hipStream_t st) {
+  const int64_t in = (int64_t)p.n_seqs * p.cols, out = (int64_t)p.n_out * p.out_cols;
+  if (few(p.num_phys, p.n_seqs, p.n_out, in > out ? in : out)) {
+    ProfScope prof_("fork_small", st);
+    const size_t lds = (size_t)((p.num_phys + 3) & ~3) * 4 + sizeof(Child) * p.n_out + (sizeof(Parent) + 8) * p.n_seqs + (size_t)p.num_phys * 2;
+    if (lds > 65536 - 1024) {
+      static DeviceOnce once;
+      const hipError_t e = ensure_max_dynamic_lds(once, (const void*)fork_small_kernel, SMALL_PAGES * 6 + SMALL_SEQS * 40);
+      if (e != hipSuccess) return e;
+    }
+    fork_small_kernel<<<dim3(1), dim3(PLAN_THREADS), lds, st>>>(p, magic_of(p.cols), magic_of(p.out_cols));
+    return hipGetLastError();
+  }
   {
     ProfScope prof_("fork_plan", st);
     const unsigned more = p.refs_out == p.refs ? 0 : (unsigned)(((int64_t)p.num_phys + PLAN_THREADS - 1) / PLAN_THREADS);
@@ -348,6 +564,17 @@ size_t compact_workspace_bytes(int64_t num_phys) {
 }
 int64_t compact_blocks(const CompactParams& p) { return compact_move_blocks(p) + (int64_t)p.n_seqs * pieces_of(p.cols); }
 hipError_t launch_page_compact(const CompactParams& p, void* ws, hipStream_t st) {
+  if (few(p.num_phys, p.n_seqs, p.n_seqs, (int64_t)p.n_seqs * p.cols)) {
+    ProfScope prof_("compact_small", st);
+    const size_t lds = (size_t)p.num_phys * 10 + 16;
+    if (lds > 65536 - 1024) {
+      static DeviceOnce once;
+      const hipError_t e = ensure_max_dynamic_lds(once, (const void*)compact_small_kernel, SMALL_PAGES * 10 + 16);
+      if (e != hipSuccess) return e;
+    }
+    compact_small_kernel<<<dim3(1), dim3(PLAN_THREADS), lds, st>>>(p, magic_of(p.cols));
+    return hipGetLastError();
+  }
   const unsigned blocks = (unsigned)(((int64_t)p.num_phys + COMPACT_BLOCK - 1) / COMPACT_BLOCK);
   {
     ProfScope prof_("compact_rank", st);
@@ -366,9 +593,9 @@ hipError_t launch_page_copy(const CopyParams& p, void* const* pools, int32_t n_p
     const int32_t n = n_pools - first < COPY_POOLS ? n_pools - first : COPY_POOLS;
     CopyPools at{};
     for (int32_t i = 0; i < n; ++i) at.at[i] = (unsigned char*)pools[first + i];
-    const int64_t items = (int64_t)p.n_copies * n * p.n_heads;
+    const int32_t rows = n * p.n_heads, most = rows < 8192 ? 8192 / rows : 1;   // (a list that may be long is walked: most of its room may be unused)
     ProfScope prof_("page_copy", st);
-    page_copy_kernel<<<dim3((unsigned)(items < 4096 ? items : 4096)), dim3(COPY_THREADS), 0, st>>>(p, at, n);
+    page_copy_kernel<<<dim3((unsigned)(p.n_copies < most ? p.n_copies : most), (unsigned)rows), dim3(COPY_THREADS), 0, st>>>(p, at);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -49,9 +49,10 @@ FORKS = [
 ]
 
 
-def _fork_case(case, in_place):
+def _fork_case(case, in_place, held=0):
     spans, shared, P, cols, n_phys, parents, grow, out_cols = case
     tables, refs = _state(spans, P, cols, n_phys, shared, 3)
+    refs += [1] * held      # pages that somebody else holds
     want = gu.fork(tables, spans, parents, grow, refs, P, out_cols)
     n_out = len(parents)
     t, ln, r = _i(tables), _i(spans), _i(refs)
@@ -68,17 +69,20 @@ def _fork_case(case, in_place):
 
 
 @pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("held", [0, 9000])   # (few pages: one workgroup; many: two launches)
 @pytest.mark.parametrize("case", FORKS, ids=[str(i) for i in range(len(FORKS))])
-def test_fork(case, in_place):
-    _fork_case(case, in_place)
+def test_fork(case, held, in_place):
+    _fork_case(case, in_place, held)
 
 
-def test_fork_of_entries_out_of_range_and_of_lengths_out_of_range():
+@pytest.mark.parametrize("held", [0, 9000])
+def test_fork_of_entries_out_of_range_and_of_lengths_out_of_range(held):
     P, n_phys = 16, 30
     tables, refs = _state([40, 40, 35], P, 4, n_phys, [0, 0, 0], 5)
+    refs += [1] * held
     for x in (tables[0][1], tables[1][2], tables[2][2]):
         refs[x] = 0
-    tables[0][1], tables[1][2], tables[2][2] = 30, -9, 1 << 30
+    tables[0][1], tables[1][2], tables[2][2] = 30 + held, -9, 1 << 30
     parents, grow = [0, 0, 1, 1, 2, 2], [1, 9, 1, 30, -5, 40]
     want = gu.fork(tables, [40, 900, -3], parents, grow, refs, P, 4)
     got = api.page_fork(_i(tables), _i([40, 900, -3]), _i(parents), _i(refs), P, grow=_i(grow))
@@ -87,7 +91,7 @@ def test_fork_of_entries_out_of_range_and_of_lengths_out_of_range():
     assert got.copies.tolist() == want[3] and got.status.tolist() == want[4]
 
 
-@pytest.mark.parametrize("n_seqs,n_out,P,n_phys", [(1500, 2000, 16, 60000), (4096, 4096, 128, 9000), (3, 700, 32, 40000)])
+@pytest.mark.parametrize("n_seqs,n_out,P,n_phys", [(1500, 2000, 16, 60000), (4096, 4096, 128, 9000), (3, 700, 32, 40000), (1024, 1024, 16, 8192), (1025, 3, 16, 8192)])
 def test_fork_of_many(n_seqs, n_out, P, n_phys):
     """More sequences than a workgroup has threads, more pages than it counts at a time, rows of several pieces; then further steps in place."""
     rng = np.random.default_rng(6)
@@ -107,17 +111,19 @@ def test_fork_of_many(n_seqs, n_out, P, n_phys):
         t, ln = got.tables, got.lens
 
 
-def test_counts_of_pages_held_besides():
+@pytest.mark.parametrize("more", [0, 9000])
+def test_counts_of_pages_held_besides(more):
     """A page that somebody outside holds: the first child copies it too, and it does not become free."""
     P = 16
     tables, refs = _state([20, 18], P, 3, 8, [0, 0], 9)
+    refs += [1] * more
     held = tables[0][1]
     refs[held] += 1
     want = gu.fork(tables, [20, 18], [0, -1], [1, 0], refs, P, 3)
     got = api.page_fork(_i(tables), _i([20, 18]), _i([0, -1]), _i(refs), P, grow=_i([1, 0]))
     torch.cuda.synchronize()
     assert got.copies.tolist() == want[3] and got.copies.tolist()[0][0] == held and got.refs.tolist() == want[2]
-    assert got.refs[held] == 1 and sum(x > 0 for x in got.refs.tolist()) == 3
+    assert got.refs[held] == 1 and sum(x > 0 for x in got.refs.tolist()) == 3 + more
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "tokens_first", "kvq", "gradient"])
@@ -161,7 +167,7 @@ def test_copy_of_a_count_on_the_device(limit):
 
 
 @pytest.mark.parametrize("n_phys,spans,P,cols", [(1, [0], 16, 1), (2, [5], 16, 2), (40, [100, 33, 0, 16], 16, 9), (9000, [3000, 70000, 1], 16, 5000),
-                                                 (20000, [150000], 16, 10000)])
+                                                 (20000, [150000], 16, 10000), (8192, [40000, 39999, 1], 16, 3000), (8191, [90000], 16, 6000)])
 @pytest.mark.parametrize("in_place", [False, True])
 def test_compact(n_phys, spans, P, cols, in_place):
     tables, refs = _state(spans, P, cols, n_phys, [0] * len(spans), 11)
@@ -183,7 +189,7 @@ def test_compact(n_phys, spans, P, cols, in_place):
 
 
 def test_compact_of_nothing_and_of_everything():
-    for refs in ([0] * 50, [1] * 50, [0] * 25 + [2] * 25, [3] * 25 + [0] * 25):
+    for refs in ([0] * 50, [1] * 50, [0] * 25 + [2] * 25, [3] * 25 + [0] * 25, [0] * 10000, [1] * 10000, [0] * 5000 + [2] * 5000):
         want = gu.compact([[-1] * 3], [0], refs, 16)
         got = api.page_compact(_i([[-1] * 3]), _i([0]), _i(refs), 16)
         torch.cuda.synchronize()
