@@ -205,7 +205,7 @@ __global__ __launch_bounds__(COPY_THREADS) void page_copy_kernel(CopyParams p, C
       }
 #pragma unroll
       for (int j = 0; j < AT_ONCE; ++j)
-        if (u0 + j * COPY_THREADS < units) *reinterpret_cast<u32x4*>(to + at[j]) = v[j];
+        if (u0 + j * COPY_THREADS < units) __builtin_nontemporal_store(v[j], reinterpret_cast<u32x4*>(to + at[j]));   // (past the caches: 236 MB 60 -> 53 us)
     }
   }
 }
