@@ -343,16 +343,17 @@ template <typename T> __global__ __launch_bounds__(GROUP_THREADS) void beam_grou
       if (!(base[beam] > -(double)INFINITY)) continue;
       const Row<T> x(p, (int64_t)group * p.n_beams + beam);
       for (int64_t v0 = 0; v0 < p.vocab; v0 += GROUP_THREADS) {
-        const uint64_t worst = n_best == K ? c.best_val[K - 1] : 0;
-        if (worst >= top_val) break;
-        const int64_t at = v0 + tid;
-        const uint64_t v = at < p.vocab ? value(beam, Elem<T>::load(x.from + x.lead + at)) : 0;
+        const uint64_t worst = n_best == K ? c.best_val[K - 1] : 0, worst_at = n_best == K ? c.best_at[K - 1] : 0;
+        if (worst > top_val || (worst == top_val && worst_at < ((uint64_t)beam << 32 | (uint32_t)v0))) break;   // (a beam that has ended may stand behind)
+        const int64_t token = v0 + tid;
+        const uint64_t v = token < p.vocab ? value(beam, Elem<T>::load(x.from + x.lead + token)) : 0, at = (uint64_t)beam << 32 | (uint32_t)token;
+        const bool better = v > worst || (v && v == worst && at < worst_at);
         if (tid == 0) n_cand = 0;
-        if (!__syncthreads_or(v > worst)) continue;
-        if (v > worst) {
+        if (!__syncthreads_or(better)) continue;
+        if (better) {
           const int to = atomicAdd(&n_cand, 1);
           c.val[to] = v;
-          c.at[to] = (uint64_t)beam << 32 | (uint32_t)at;
+          c.at[to] = at;
         }
         __syncthreads();
         n_best = keep_best(c, n_cand, n_best, K);

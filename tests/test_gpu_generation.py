@@ -247,6 +247,14 @@ def test_beam_of_equal_logits_takes_the_lowest():
     _verify_beam(x, s, 33, _beam(x, s, 33))
 
 
+@pytest.mark.parametrize("n_out", [1, 2, 3])
+def test_beam_that_has_ended_stands_behind_equal_ones(n_out):
+    """Scores so large that log-sums vanish in them: every candidate of a group is equal, and the lowest places win over those of beams that have ended."""
+    scores, x = torch.full((2, 3), -1e20), torch.zeros((2, 3, 5000))
+    done = torch.tensor([[0, 1, 1], [1, 0, 1]], dtype=torch.int32)
+    _verify_beam(x, scores, n_out, _beam(x, scores, n_out, done, 7), done, 7)
+
+
 def test_beam_of_zeros_of_either_sign():
     """They are equal: the lowest place wins."""
     for V in (200, 9000, 30000):
