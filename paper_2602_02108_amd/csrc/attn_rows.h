@@ -257,8 +257,8 @@ __global__ __launch_bounds__(64 * W, 2) void attn_rows_kernel(RowsParams p, Attn
   const int n_steps = (seen.tiles + TILES - 1) / TILES;
   const int parts = item.count * W, mine = item.index * W + wave;
   const int each = (int)((uint32_t)n_steps / (uint32_t)parts), more = n_steps - each * parts;   // (one more for the first `more`)
-  int u = each * mine + min(mine, more);
-  const int u_end = u + each + (mine < more);
+  const int u_first = each * mine + min(mine, more), u_end = u_first + each + (mine < more);
+  int u = u_first;
 
   f32x4 acc[RT][NJ];
   float ref[RT], sum[RT];
@@ -293,10 +293,11 @@ __global__ __launch_bounds__(64 * W, 2) void attn_rows_kernel(RowsParams p, Attn
     }
   };
 
-  auto one_step = [&](int number, Raw<T, D>& raw, const int (&t0)[TILES]) __attribute__((always_inline)) {
+  bool wild_seen = false;
+  auto one_step = [&](Raw<T, D>& raw, const int (&t0)[TILES]) __attribute__((always_inline)) {
     const bool masked = (TILES == 1 ? t0[0] : WIDE ? t0[TILES - 1] : max(t0[0], t0[TILES - 1])) + 15 > min_pos;
     // Tokens that not every row sees.  Their V is zero where nothing of it is seen (it may be anything), and so are their values that are not
-    // finite: a weight of zero does not stop those, so the rows that do see them get them below.
+    // finite: a weight of zero does not stop those, so the rows that do see them get them at the end.
     bool wild = false;
     if (masked) {
 #pragma unroll
@@ -422,34 +423,12 @@ __global__ __launch_bounds__(64 * W, 2) void attn_rows_kernel(RowsParams p, Attn
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) acc[rt][j] = mfma4(raw.v[0][r][j], __float_as_uint(z[rt][r]), acc[rt][j]);
     }
-
-    if (__any(wild)) {   // values that are not finite, to the rows that see them: lane (m, kg) holds dims D/4 kg + D/16 i + j of query m in acc[.][j][i]
-#pragma unroll
-      for (int i = 0; i < TILES; ++i) {
-        const int tile = TILES * number + i, e = tile >> log_tpp, off = (tile & ((1 << log_tpp) - 1)) << 4;
-        if (t0[i] >= NO_TOKEN) continue;
-        const unsigned char* page = vbase + (int64_t)page_of(p, b, list ? list[e] : e) * p.pool_page_stride * ES;
-        for (int t = 0; t < 16; ++t) {
-          const int at = t0[i] + t;
-          if (at <= min_pos || at > max_pos) continue;
-          const T* v = reinterpret_cast<const T*>(page + (int64_t)(off + t) * tok) + kg * (D / 4);
-#pragma unroll
-          for (int x = 0; x < 4; ++x)
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-              const float y = Elem<T>::load(v + NJ * x + j);
-              const bool bad = wild32(__float_as_uint(y));
-#pragma unroll
-              for (int rt = 0; rt < RT; ++rt)
-                if (bad && at <= pos[rt]) acc[rt][j][x] += y;
-            }
-        }
-      }
-    }
+    wild_seen |= wild;
   };
 
-  // steps in flight: a wave that waits for its next one idles its share of the memory's latency (about a microsecond)
-  constexpr int AHEAD = 2;
+  // steps in flight: a wave that waits for its next one idles its share of the memory's latency (about a microsecond); fp32 rows of 128 dims: two do not fit
+  // the registers (1 GB of cache, one row: two 195 us, one 180)
+  constexpr int AHEAD = sizeof(T) == 4 && D == 128 ? 1 : 2;
   Raw<T, D> raw[AHEAD];
   int t0[AHEAD][TILES];
   // The wait for a step lets every later fetch fly on, if the compiler can count them: the steady loop fetches without a condition,
@@ -462,7 +441,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_rows_kernel(RowsParams p, Attn
     for (; u + 2 * AHEAD <= u_end; u += AHEAD) {
 #pragma unroll
       for (int k = 0; k < AHEAD; ++k) {
-        one_step(u + k, raw[k], t0[k]);
+        one_step(raw[k], t0[k]);
         fetch(u + k + AHEAD, raw[k], t0[k]);
       }
     }
@@ -475,12 +454,32 @@ __global__ __launch_bounds__(64 * W, 2) void attn_rows_kernel(RowsParams p, Attn
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
       if (u + k >= u_end) break;
-      one_step(u + k, raw[k], t0[k]);
+      one_step(raw[k], t0[k]);
       if (u + k + AHEAD < u_end) fetch(u + k + AHEAD, raw[k], t0[k]);
     }
   }
 
   // lane (m, kg): query m, dims D/4 kg + D/16 i + j of acc[.][j][i]
+  if (__any(wild_seen)) {
+    for (int tile = min(TILES * u_end, seen.tiles) - 1; tile >= TILES * u_first; --tile) {
+      const int e = tile >> log_tpp, off = (tile & ((1 << log_tpp) - 1)) << 4, page = list ? list[e] : e;
+      const int phys = page >= 0 && page < (p.max_len + p.P - 1) >> p.log2_p ? page_of(p, b, page) : -1, start = (page << p.log2_p) + off;
+      if (phys < 0) continue;
+      if (start + 15 <= min_pos) break;
+      for (int t = max(0, min_pos + 1 - start); t < 16 && start + t <= max_pos; ++t) {
+        const T* v = reinterpret_cast<const T*>(vbase + (int64_t)phys * p.pool_page_stride * ES + (int64_t)(off + t) * tok) + kg * (D / 4);
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) {
+            const float y = Elem<T>::load(v + NJ * x + j);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+              if (wild32(__float_as_uint(y)) && start + t <= pos[rt]) acc[rt][j][x] += y;
+          }
+      }
+    }
+  }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     sum[rt] += __shfl_xor(sum[rt], 16, 64);
@@ -945,7 +944,8 @@ Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   c.split = steps > 16 && blocks <= 2 * WGS;   // (more fill the chip; parts of tiles take up to 66 KB a workgroup)
   c.target = (int)(c.tiles ? WGS : blocks < WGS ? WGS - blocks / 2 : blocks);   // (parts come out rounded up: half a part more for each block)
   const int64_t most = (steps + c.min_steps - 1) / c.min_steps;
-  c.blocks = !c.split ? blocks : blocks * most < c.target + blocks ? blocks * most : c.target + blocks;
+  const int64_t parts = c.target + blocks + 2;   // (what item_at comes to at most; two for its roundings)
+  c.blocks = !c.split ? blocks : blocks * most < parts ? blocks * most : parts;
   c.waves = c.split ? 4 : 8;
   c.stream = cache_bytes > (256ll << 20);
   return c;

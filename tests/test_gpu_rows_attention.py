@@ -190,6 +190,108 @@ def test_values_that_are_not_finite(dt, spans, Hq, Hkv, D):
     ru.check("O", np.where(np.isfinite(got), got, 0), np.where(np.isfinite(wo[live]), wo[live], 0), to[live])
 
 
+# Many bf16 rows over caches whose second reading costs something: (Hq, Hkv), D, P, spans, listed
+MANY = [
+    ((14, 2), 128, 16, [(300, 900), (40, 70), (1, 20)], False),      # whole waves without rows, pages of a tile
+    ((14, 2), 128, 128, [(301, 1300), (90, 60), (0, 30)], True),     # rows without a token; pages that end inside a stage
+    ((14, 2), 64, 32, [(300, 1500), (33, 1200)], False),
+    ((14, 2), 64, 128, [(299, 2100), (5, 5)], True),
+    ((6, 1), 128, 64, [(40, 50000)], False),                         # few rows, cut into parts
+    ((10, 1), 64, 16, [(23, 60001), (4, 9)], True),
+    ((3, 3), 128, 32, [(513, 1100), (513, 513), (129, 2000)], False),
+]
+MANY_IDS = [f"h{c[0][0]}-{c[0][1]}-d{c[1]}-p{c[2]}-{i}" for i, c in enumerate(MANY)]
+
+
+def _many(case, seed):
+    (Hq, Hkv), D, P, spans, listed = case
+    b = ru.Batch(spans, P, seed)
+    # (what makes a call one of many rows: the readings of the caches after the first, over 64 MB)
+    assert (-(-b.max_rows * (Hq // Hkv) // 16) - 1) * len(spans) * b.max_len * Hkv * 4 * D > (64 << 20) and \
+        (-(-b.max_rows * (Hq // Hkv) // 16) - 1) * b.n_phys * P * Hkv * 4 * D > (64 << 20)
+    rng = np.random.default_rng(seed)
+    lists = None
+    if listed:
+        lists = [[sorted(int(x) for x in rng.permutation(-(-t // P))[:-(-t // P) * 4 // 5]) for _ in range(Hkv)] for _, t in spans]
+    return b, lists, _queries(b, Hq, D, BF, seed + 1), [pu.random_pool(b, Hkv, D, BF, s) for s in (seed + 2, seed + 3)]
+
+
+@pytest.mark.parametrize("case", MANY, ids=MANY_IDS)
+def test_many_rows(case):
+    """Against the definition; then with pools of tokens before heads, and a workspace of anything: the same bits."""
+    b, lists, q, pools = _many(case, 40)
+    o, lse = _run(b, q, pools, 0.1, lists)
+    _verify(b, q, pools, 0.1, o, lse, lists)
+    strided = [x.permute(0, 2, 1, 3).contiguous().cuda().permute(0, 2, 1, 3) for x in pools]
+    o2, lse2 = _run(b, q, strided, 0.1, lists, workspace=torch.full((1 << 26,), 255, dtype=torch.uint8, device="cuda"))
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("case", MANY, ids=MANY_IDS)
+@pytest.mark.parametrize("order", ["rising", "falling", "spikes"])
+def test_many_rows_logits_far_apart(case, order):
+    b, lists, q, pools = _many(case, 50)
+    direction = torch.sign(q[0, 0].float())
+    for s, (_, t) in enumerate(b.spans):
+        pos = torch.arange(t, dtype=torch.float32)
+        size = {"rising": pos * 60 / t, "falling": (t - pos) * 60 / t, "spikes": torch.where(pos % 97 == 5, 30 + 30 * pos / t, 0.1)}[order]
+        pages = torch.from_numpy(b.tables[s].astype(np.int64))[torch.arange(t) // b.P]
+        pools[0][pages, :, torch.arange(t) % b.P] = (size[:, None, None] * direction).to(BF).expand(t, pools[0].shape[1], -1)
+    o, lse = _run(b, q, pools, 0.1, lists)
+    _verify(b, q, pools, 0.1, o, lse, lists)
+
+
+@pytest.mark.parametrize("case", MANY, ids=MANY_IDS)
+def test_many_rows_values_that_are_not_finite(case):
+    """As test_values_that_are_not_finite."""
+    b, lists, q, pools = _many(case, 60)
+    Hkv, P = pools[0].shape[1], b.P
+    n, t = b.spans[0]
+
+    def spoil(pool, s, pos, g, d, value):
+        pool[int(b.tables[s, pos // P]), g, pos % P, d] = value
+
+    last = pools[0].shape[3] - 1
+    for at, (pos, d, value) in enumerate([(t - n + 2, last, math.nan), (t - 1, 0, math.inf), (t - 3, 9, -math.inf), (t - 2, 40, math.nan), (t - n // 2, 33, math.inf),
+                                          (t - n // 2, 34, math.nan), (t - 17, 8, math.inf), (t - 16, 7, -math.inf)]):
+        spoil(pools[1], 0, pos, at % Hkv, d, value)
+    spoil(pools[1], 0, 3, Hkv - 1, 1, math.inf)          # seen by every row
+    spoil(pools[0], 0, t - 5, 0, 5, math.nan)
+    q[1, 0, 3] = math.nan
+    o, lse = _run(b, q, pools, 0.1, lists)
+    wo, wl, to, tl = pu.attend(b, q, *pools, 0.1, lists)
+    live = slice(0, b.rows)
+    got = o.cpu().double().numpy()[live]
+    assert np.isfinite(wo[live]).mean() > 0.5 and (~np.isfinite(wo[live])).any()
+    assert np.array_equal(np.isfinite(got), np.isfinite(wo[live]))
+    ru.check("LSE", lse.cpu().double().numpy()[:, live], wl[:, live], tl[:, live])
+    ru.check("O", np.where(np.isfinite(got), got, 0), np.where(np.isfinite(wo[live]), wo[live], 0), to[live])
+
+
+def test_many_rows_pages_that_the_pool_does_not_have():
+    b, _, q, pools = _many(MANY[1][:4] + (False,), 70)
+    bad = [1, 4, 9]
+    keep = b.tables.copy()
+    b.tables[0, bad] = [b.n_phys, -3, 1 << 30]
+    o, lse = _run(b, q, pools, 0.1)
+    b.tables = keep
+    lists = [[[l for l in range(-(-t // b.P)) if s or l not in bad] for _ in range(2)] for s, (_, t) in enumerate(b.spans)]
+    _verify(b, q, pools, 0.1, o, lse, lists)
+
+
+@pytest.mark.parametrize("dt,Hq,Hkv,D,P,spans", [
+    (F32, 14, 2, 128, 16, [(300, 900), (150, 700)]),     # parts of many rows
+    (F32, 16, 1, 64, 64, [(70, 3000), (1, 5000)]),
+    (BF, 16, 2, 64, 128, [(17, 3000), (9, 2000)]),
+])
+def test_parts_of_rows(dt, Hq, Hkv, D, P, spans):
+    b = ru.Batch(spans, P, 17)
+    q = _queries(b, Hq, D, dt, 13)
+    pools = [pu.random_pool(b, Hkv, D, dt, s) for s in (25, 26)]
+    o, lse = _run(b, q, pools, 0.1)
+    _verify(b, q, pools, 0.1, o, lse)
+
+
 def test_logits_of_minus_infinity_have_no_weight():
     P, D = 16, 64
     for dt in (BF, F32):
