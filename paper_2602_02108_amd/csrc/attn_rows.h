@@ -426,9 +426,9 @@ __global__ __launch_bounds__(64 * W, 2) void attn_rows_kernel(RowsParams p, Attn
     wild_seen |= wild;
   };
 
-  // steps in flight: a wave that waits for its next one idles its share of the memory's latency (about a microsecond); fp32 rows of 128 dims: two do not fit
-  // the registers (1 GB of cache, one row: two 195 us, one 180)
-  constexpr int AHEAD = sizeof(T) == 4 && D == 128 ? 1 : 2;
+  // steps in flight: a wave that waits for its next one idles its share of the memory's latency (about a microsecond); two of 128 dims do not fit the registers
+  // in fp32 (1 GB of cache, one row: two 195 us, one 180), nor beside two row tiles
+  constexpr int AHEAD = D == 128 && (sizeof(T) == 4 || RT == 2) ? 1 : 2;
   Raw<T, D> raw[AHEAD];
   int t0[AHEAD][TILES];
   // The wait for a step lets every later fetch fly on, if the compiler can count them: the steady loop fetches without a condition,
@@ -929,10 +929,14 @@ Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   int64_t tokens = p.max_len;
   if (sel_stride >= 0 && (int64_t)sel_stride * p.P < tokens) tokens = (int64_t)sel_stride * p.P;
   const int64_t reach = heads * tokens, held = p.num_phys * p.Hkv * p.P, cache_bytes = (reach < held ? reach : held) * 2 * p.D * (is_bf16 ? 2 : 4);
-  // Tiles once the caches are read by a second row block and that costs more than their start (one sequence of 4096 tokens, 84 rows: 22 us in six blocks,
-  // 26 in tiles; of 65,536, 21 rows: 51, 40; 16 of 4096, 35 rows: 67, 39).
-  c.tiles = is_bf16 && rows > 16 && ((rows + 15) / 16 - 1) * cache_bytes > (64ll << 20) && p.pool_tok_stride <= (1 << 24);   // (offsets of a lane in a tile: 32 bits)
-  c.rt = rows <= 16 || p.D == 128 ? 1 : 2;
+  // Readings of the caches after the first, in bytes, at 16 and at 32 rows a block.
+  const int64_t again_16 = ((rows + 15) / 16 - 1) * cache_bytes, again_32 = ((rows + 31) / 32 - 1) * cache_bytes;
+  // Tiles once the caches are read by a second block of 32 rows and that costs more than their start (one sequence, D 128, us without and with: 4 heads of 4096
+  // tokens, 35 rows 17, 16; of 65,536, 54, 40; 64 of 2048, one head, 64 rows 36, 31; 16 of 4096, D 64, one head, 96 rows 20, 21).
+  c.tiles = is_bf16 && rows > 32 && again_32 > (48ll << 20) && p.pool_tok_stride <= (1 << 24);   // (offsets of a lane in a tile: 32 bits)
+  // Two row tiles a wave where rows need them; at head dim 128 for bf16 and caches that are worth it, one step in flight instead of two (32 rows of one head, us
+  // with one and two: 4096 tokens 12, 14; 65,536, 25, 23; 28 rows of four heads over 500,000, in tiles 224, in two 167: 6.1 TB/s).
+  c.rt = rows > 16 && (p.D == 64 || (is_bf16 && again_16 > (16ll << 20))) ? 2 : 1;
   c.block_rows = c.tiles ? TILE_ROWS : 16 * c.rt;
   c.step = c.tiles ? TILE_STAGE : 32;
   const int64_t steps = (tokens + c.step - 1) / c.step;
@@ -991,7 +995,7 @@ template <typename T, int D, int RT, int W, bool WIDE, bool STREAM> hipError_t r
 }
 template <typename T, int D, int RT, int W> hipError_t run_rows(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
   if (sizeof(T) == 2 && p.P < 32) return run_rows<T, D, RT, W, sizeof(T) != 2, false>(p, c, ws, st);
-  if constexpr (RT == 1 && W == 4) {
+  if constexpr (W == 4) {
     if (c.stream) return run_rows<T, D, RT, W, true, true>(p, c, ws, st);
   }
   return run_rows<T, D, RT, W, true, false>(p, c, ws, st);
@@ -1006,7 +1010,7 @@ template <typename T, int D> hipError_t attn(const RowsParams& p, void* ws, hipS
     static DeviceOnce once;
     if (c.tiles) return run<T, D>(p, c, attn_tiles_kernel<D>, TILE_THREADS, TILE_LDS<D>, once, ws, st);
   }
-  if constexpr (D == 64) {
+  if constexpr (D == 64 || sizeof(T) == 2) {
     if (c.rt == 2) return run_rows<T, D, 2>(p, c, ws, st);
   }
   return run_rows<T, D, 1>(p, c, ws, st);

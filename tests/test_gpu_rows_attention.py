@@ -199,6 +199,8 @@ MANY = [
     ((6, 1), 128, 64, [(40, 50000)], False),                         # few rows, cut into parts
     ((10, 1), 64, 16, [(23, 60001), (4, 9)], True),
     ((3, 3), 128, 32, [(513, 1100), (513, 513), (129, 2000)], False),
+    ((28, 4), 128, 128, [(4, 9000), (1, 40)], False),                # two row tiles
+    ((8, 1), 128, 16, [(3, 40011), (4, 300)], True),
 ]
 MANY_IDS = [f"h{c[0][0]}-{c[0][1]}-d{c[1]}-p{c[2]}-{i}" for i, c in enumerate(MANY)]
 
@@ -206,9 +208,9 @@ MANY_IDS = [f"h{c[0][0]}-{c[0][1]}-d{c[1]}-p{c[2]}-{i}" for i, c in enumerate(MA
 def _many(case, seed):
     (Hq, Hkv), D, P, spans, listed = case
     b = ru.Batch(spans, P, seed)
-    # (what makes a call one of many rows: the readings of the caches after the first, over 64 MB)
-    assert (-(-b.max_rows * (Hq // Hkv) // 16) - 1) * len(spans) * b.max_len * Hkv * 4 * D > (64 << 20) and \
-        (-(-b.max_rows * (Hq // Hkv) // 16) - 1) * b.n_phys * P * Hkv * 4 * D > (64 << 20)
+    # (what makes a call one of many rows: bytes of the caches that are read again, at 32 rows a block, or at 16)
+    rows, held = b.max_rows * (Hq // Hkv), min(len(spans) * b.max_len, b.n_phys * P) * Hkv * 4 * D
+    assert (-(-rows // 32) - 1) * held > (48 << 20) if rows > 32 else (-(-rows // 16) - 1) * held > (16 << 20)
     rng = np.random.default_rng(seed)
     lists = None
     if listed:
