@@ -7,6 +7,10 @@
 // through the cells: the K-th best cell maximum is a bound that K candidates reach at least; only the few cells that reach it are read again, and the rank of
 // each of their values above the bound is counted.  Candidates are compared in 64 bits, ties go to the lowest w * vocab + v.
 // Where very many values are equal the bound does not sort them out; then a group is walked in order of its places, the K best so far in hand.
+//
+// What bounds it: the first kernel, the reading of the logits (256 rows of 130,999 bf16: 67 MB in 15 us, 4.5 TB/s; a maximum costs one instruction an element, where the
+// best of each slice kept on the way made both kernels 154 us instead of 25); the second, one workgroup a group and its chain of steps (cells, bound, values, ranks),
+// about 10 us for any vocabulary.
 #include <algorithm>
 #include <cfloat>
 
