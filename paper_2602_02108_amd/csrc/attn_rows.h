@@ -41,6 +41,7 @@ constexpr int NO_TOKEN = 0x7fffff00;     // position of the tokens of a tile tha
 constexpr int PAD = 4;                   // floats between the rows of a merge buffer: conflict-free for 16-byte accesses
 constexpr int COMBINE_THREADS = 256;
 constexpr int WGS = 512;                 // workgroups that a call is cut into
+constexpr int WAVES = 4;                 // that split the tokens of a block (100 sequences of 500 tokens: 23 us; eight, one workgroup a compute unit, 34; two the same, fp32 48 for 39)
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -76,7 +77,8 @@ struct AttnArgs {
   int split;                   // whether blocks may be cut
   int even;                    // into equal shares of the longest
   int target, min_steps;       // workgroups to aim at; steps of a part at least
-  int2* parts;                 // [sequence * Hkv + KV head]: its first workgroup, parts of each of its blocks
+  int planned;                 // whether attn_plan counts, for the whole call; else every workgroup does
+  int2* parts;                 // [sequence * Hkv + KV head]: its first workgroup, parts of each of its blocks; planned: one more, the workgroups of all
   float* part;                 // [workgroup][row of the block][D] sums
   float* part_ml;              // [workgroup][row of the block][2]: reference, sum
   int blocks;                  // workgroups of the launch
@@ -89,8 +91,38 @@ __device__ __forceinline__ Load load_of(const RowsParams& p, const AttnArgs& a, 
   return {(int)(((int64_t)s.n * p.G + a.block_rows - 1) / a.block_rows), max(steps, 1), s};
 }
 struct Item { int e, block, first, index, count; Seq s; };   // e, block of its rows, the block's first workgroup, this one of it, its number of parts
+// Steps of a part.  Tiles: an equal share of the longest, as many as fit one round of workgroups (224 blocks of 250 steps in
+// 1, 2, 3, 4 parts: 427, 362, 378, 365 us; 112 of 512: 823, 437, 434, 365); else by the work alone, so that short parts even out.
+__device__ __forceinline__ int steps_of_part(const AttnArgs& a, float total, int most) {
+  if (!a.split) return 0x7fffffff;
+  const int shares = max(1, (int)((float)a.target * (float)most / max(total, 1.0f) + 1e-3f));
+  return max(a.min_steps, a.even ? (most + shares - 1) / shares : (int)(total / (float)a.target) + 1);
+}
+__device__ __forceinline__ int parts_of(const AttnArgs& a, const Load& l, int per) { return a.split ? (int)(((uint32_t)l.steps + (uint32_t)per - 1) / (uint32_t)per) : 1; }
+__device__ __forceinline__ int workgroups_of(const Load& l, int parts) { return (int)min((int64_t)l.blocks * parts, (int64_t)1 << 24); }   // (a launch holds fewer; row_starts may be anything)
+
 // Workgroup x's item, by every lane of a wave; e < 0: there are fewer.
 __device__ __forceinline__ Item item_at(const RowsParams& p, const AttnArgs& a, int x, int lane) {
+  if (a.planned) {   // the last e that begins at x or before
+    const int n = p.n_seqs * p.Hkv;
+    if (x >= a.parts[n].x) return {-1, 0, 0, 0, 0, {}};
+    int e = 0;
+    for (int size = n; size > 1;) {
+      const int stride = (size + 63) >> 6;
+      const uint64_t upto = __ballot(lane * stride < size && a.parts[min(e + lane * stride, n - 1)].x <= x);
+      const int last = max(__popcll(upto) - 1, 0);
+      e += last * stride;
+      size = min(stride, size - last * stride);
+    }
+    e = __builtin_amdgcn_readfirstlane(e);
+    const int2 at = a.parts[e];
+    const Load l = load_of(p, a, e);
+    const int count = __builtin_amdgcn_readfirstlane(max(at.y, 1)), nth = __builtin_amdgcn_readfirstlane((x - at.x) / count), blocks = __builtin_amdgcn_readfirstlane(l.blocks);
+    if (nth < 0 || nth >= blocks) return {-1, 0, 0, 0, 0, {}};
+    const int index = __builtin_amdgcn_readfirstlane(x - at.x) - nth * count;
+    return {e, blocks - 1 - nth, x - index, index, count,
+            {__builtin_amdgcn_readfirstlane(l.s.row), __builtin_amdgcn_readfirstlane(l.s.n), __builtin_amdgcn_readfirstlane(l.s.pos), 0}};
+  }
   const int n = p.n_seqs * p.Hkv;
   constexpr int HELD = 4;   // of a lane, loaded together (256 in all; more are asked for again)
   Load held[HELD];
@@ -111,13 +143,7 @@ __device__ __forceinline__ Item item_at(const RowsParams& p, const AttnArgs& a, 
   }
   total = last_lane(wave_upto(total, 0.0f, [](float a, float b) { return a + b; }));
   most = last_lane(wave_upto(most, 1, [](int a, int b) { return max(a, b); }));
-  // Steps of a part (the same in every wave).  Tiles: an equal share of the longest, as many as fit one round of workgroups (224 blocks of 250 steps in
-  // 1, 2, 3, 4 parts: 427, 362, 378, 365 us; 112 of 512: 823, 437, 434, 365); else by the work alone, so that short parts even out.
-  int per = 0x7fffffff;
-  if (a.split) {
-    const int shares = max(1, (int)((float)a.target * (float)most / max(total, 1.0f) + 1e-3f));
-    per = max(a.min_steps, a.even ? (most + shares - 1) / shares : (int)(total / (float)a.target) + 1);
-  }
+  const int per = steps_of_part(a, total, most);   // (the same in every wave)
   int before = 0;
   for (int e0 = 0; e0 < n; e0 += 64) {
     Load l{0, 1, {}};
@@ -128,8 +154,7 @@ __device__ __forceinline__ Item item_at(const RowsParams& p, const AttnArgs& a, 
       for (int i = 0; i < HELD; ++i)
         if (e0 == 64 * i) l = held[i];
     }
-    const int parts = a.split ? (int)(((uint32_t)l.steps + (uint32_t)per - 1) / (uint32_t)per) : 1;
-    const int own = (int)min((int64_t)l.blocks * parts, (int64_t)1 << 24);   // (a launch holds fewer; row_starts may be anything)
+    const int parts = parts_of(a, l, per), own = workgroups_of(l, parts);
     const int upto = wave_upto(own, 0, [](int a, int b) { return a + b; });
     const uint64_t past = __ballot(before + upto > x);
     if (past) {
@@ -144,7 +169,72 @@ __device__ __forceinline__ Item item_at(const RowsParams& p, const AttnArgs& a, 
 }
 // What the sum of parts needs to know of e; by the workgroup of its last block's first part.
 __device__ __forceinline__ void note_parts(const RowsParams& p, const AttnArgs& a, const Item& it, int n_rows) {
-  if (a.split && it.index == 0 && it.block == (n_rows - 1) / a.block_rows && threadIdx.x == 0) a.parts[it.e] = make_int2(it.first, it.count);
+  if (a.split && !a.planned && it.index == 0 && it.block == (n_rows - 1) / a.block_rows && threadIdx.x == 0) a.parts[it.e] = make_int2(it.first, it.count);
+}
+
+// The same for the whole call, by one workgroup, where there are many sequences (counted by each workgroup, 1024 sequences of 2048 tokens, four KV heads, took
+// 1117 us instead of 654).
+constexpr int PLAN_THREADS = 1024, PLAN_EACH = 4, PLANNED = 512;   // more (sequence, KV head) than this
+__global__ __launch_bounds__(PLAN_THREADS) void attn_plan_kernel(RowsParams p, AttnArgs a) {
+  __shared__ float sums[PLAN_THREADS / 64];
+  __shared__ int most_of[PLAN_THREADS / 64], ends[PLAN_THREADS / 64];
+  const int n = p.n_seqs * p.Hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  float total = 0.0f;
+  int most = 1;
+  Load l[PLAN_EACH];
+  auto load = [&](int e0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < PLAN_EACH; ++j) {
+      const int e = e0 + PLAN_EACH * tid + j;
+      l[j] = load_of(p, a, min(e, n - 1));
+      if (e >= n) l[j].blocks = 0;
+    }
+  };
+  if (a.split) {
+    for (int e0 = 0; e0 < n; e0 += PLAN_EACH * PLAN_THREADS) {
+      load(e0);
+#pragma unroll
+      for (int j = 0; j < PLAN_EACH; ++j) {
+        total += (float)l[j].blocks * (float)l[j].steps;
+        most = max(most, l[j].blocks ? l[j].steps : 1);
+      }
+    }
+    total = wave_upto(total, 0.0f, [](float a, float b) { return a + b; });
+    most = wave_upto(most, 1, [](int a, int b) { return max(a, b); });
+    if (lane == 63) { sums[wave] = total; most_of[wave] = most; }
+    __syncthreads();
+    total = 0.0f;
+    most = 1;
+    for (int w = 0; w < PLAN_THREADS / 64; ++w) { total += sums[w]; most = max(most, most_of[w]); }
+  }
+  const int per = steps_of_part(a, total, most);
+  int before = 0;
+  for (int e0 = 0; e0 < n; e0 += PLAN_EACH * PLAN_THREADS) {
+    load(e0);
+    int parts[PLAN_EACH], own[PLAN_EACH], mine = 0;
+#pragma unroll
+    for (int j = 0; j < PLAN_EACH; ++j) {
+      parts[j] = parts_of(a, l[j], per);
+      own[j] = workgroups_of(l[j], parts[j]);
+      mine += own[j];
+    }
+    const int upto = wave_upto(mine, 0, [](int a, int b) { return a + b; });
+    __syncthreads();
+    if (lane == 63) ends[wave] = upto;
+    __syncthreads();
+    int at = before + upto - mine;
+    for (int w = 0; w < PLAN_THREADS / 64; ++w) {
+      at += w < wave ? ends[w] : 0;
+      before += ends[w];
+    }
+#pragma unroll
+    for (int j = 0; j < PLAN_EACH; ++j) {
+      const int e = e0 + PLAN_EACH * tid + j;
+      if (e < n) a.parts[e] = make_int2(at, parts[j]);
+      at += own[j];
+    }
+  }
+  if (tid == 0) a.parts[n] = make_int2(before, 0);
 }
 
 // The tiles of 16 tokens that a row at max_pos sees: all up to it, or the listed ones of pages that begin at or before it.
@@ -228,11 +318,11 @@ template <int RT, int NC> __device__ __forceinline__ void queries_landed(u32x4 (
 }
 
 // WIDE: pages of 32 tokens and more, a step lies in one (fp32: always).  STREAM: the cache is read past the caches.
-template <typename T, int D, int RT, int W, bool WIDE, bool STREAM>
-__global__ __launch_bounds__(64 * W, 2) void attn_rows_kernel(RowsParams p, AttnArgs a) {
+template <typename T, int D, int RT, bool WIDE, bool STREAM>
+__global__ __launch_bounds__(64 * WAVES, 2) void attn_rows_kernel(RowsParams p, AttnArgs a) {
   extern __shared__ __align__(16) float merge[];
   using S = Shape<T, D>;
-  constexpr int TILES = S::TILES, KC = S::KC, VW = S::VW, NJ = S::NJ, NZ = S::NZ, ES = S::ES, ROWS = 16 * RT;
+  constexpr int W = WAVES, TILES = S::TILES, KC = S::KC, VW = S::VW, NJ = S::NJ, NZ = S::NZ, ES = S::ES, ROWS = 16 * RT;
   const int lane = threadIdx.x & 63, m = lane & 15, kg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Item item = item_at(p, a, blockIdx.x, lane);
@@ -929,7 +1019,7 @@ template <int D> __global__ __launch_bounds__(TILE_THREADS, 2) void attn_tiles_k
 
 // How a call is cut.
 struct Plan {
-  int tiles, rt, waves, stream, split, block_rows, step, target, min_steps;
+  int tiles, rt, stream, split, planned, block_rows, step, target, min_steps;
   int64_t blocks;   // workgroups at most
 };
 Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
@@ -954,12 +1044,12 @@ Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   int64_t blocks = ((int64_t)p.n_rows * p.G / c.block_rows + p.n_seqs) * p.Hkv;
   if (blocks > each * heads) blocks = each * heads;
   c.min_steps = c.tiles ? 8 : 4;
-  c.split = steps > 16 && blocks <= 2 * WGS;   // (more fill the chip; parts of tiles take up to 66 KB a workgroup)
+  c.planned = heads > PLANNED;
+  c.split = steps > 16 && blocks <= (c.planned && !c.tiles ? 16 * WGS : 2 * WGS);   // (more fill the chip; parts of tiles take up to 66 KB a workgroup, others 8 or 16)
   c.target = (int)(c.tiles ? WGS : blocks < WGS ? WGS - blocks / 2 : blocks);   // (parts come out rounded up: half a part more for each block)
   const int64_t most = (steps + c.min_steps - 1) / c.min_steps;
   const int64_t parts = c.target + blocks + 2;   // (what item_at comes to at most; two for its roundings)
   c.blocks = !c.split ? blocks : blocks * most < parts ? blocks * most : parts;
-  c.waves = c.split ? 4 : 8;
   c.stream = cache_bytes > (256ll << 20);
   return c;
 }
@@ -970,15 +1060,21 @@ int64_t combine_blocks(const RowsParams& p, const Plan& c) {
   return combine_many(p) ? heads * ((rows + at_once - 1) / at_once) : heads * rows;
 }
 size_t part_bytes(const RowsParams& p, const Plan& c) {
-  return !c.split ? 0 : (size_t)c.blocks * c.block_rows * (p.D + 2) * sizeof(float) + (size_t)p.n_seqs * p.Hkv * sizeof(int2);
+  return (c.split ? (size_t)c.blocks * c.block_rows * (p.D + 2) * sizeof(float) : 0) + (c.split || c.planned ? ((size_t)p.n_seqs * p.Hkv + 1) * sizeof(int2) : 0);
 }
 
 template <typename T, int D, typename K> hipError_t run(const RowsParams& p, const Plan& c, K kernel, int threads, size_t lds, DeviceOnce& once, void* ws, hipStream_t st) {
-  AttnArgs a{c.block_rows, c.step, c.split, c.tiles, c.target, c.min_steps, nullptr, nullptr, nullptr, (int)c.blocks};
+  AttnArgs a{c.block_rows, c.step, c.split, c.tiles, c.target, c.min_steps, c.planned, (int2*)ws, nullptr, nullptr, (int)c.blocks};
   if (c.split) {
     a.part = (float*)ws;
     a.part_ml = a.part + c.blocks * c.block_rows * D;
     a.parts = (int2*)(a.part_ml + c.blocks * c.block_rows * 2);
+  }
+  if (c.planned) {
+    ProfScope prof_("attn_plan", st);
+    attn_plan_kernel<<<dim3(1), dim3(PLAN_THREADS), 0, st>>>(p, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
   {
     ProfScope prof_(c.tiles ? "attn_tiles" : "attn_rows", st);
@@ -998,19 +1094,13 @@ template <typename T, int D, typename K> hipError_t run(const RowsParams& p, con
   else attn_combine_kernel<T, D, D, false><<<dim3((unsigned)wgs), dim3(COMBINE_THREADS), 0, st>>>(p, a, rows);
   return hipGetLastError();
 }
-template <typename T, int D, int RT, int W, bool WIDE, bool STREAM> hipError_t run_rows(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
+template <typename T, int D, int RT, bool WIDE, bool STREAM> hipError_t run_rows(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
   static DeviceOnce once;
-  return run<T, D>(p, c, attn_rows_kernel<T, D, RT, W, WIDE, STREAM>, 64 * W, (size_t)(W * 16 * (D + PAD) + W * 16 * 2) * sizeof(float), once, ws, st);
-}
-template <typename T, int D, int RT, int W> hipError_t run_rows(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
-  if (sizeof(T) == 2 && p.P < 32) return run_rows<T, D, RT, W, sizeof(T) != 2, false>(p, c, ws, st);
-  if constexpr (W == 4) {
-    if (c.stream) return run_rows<T, D, RT, W, true, true>(p, c, ws, st);
-  }
-  return run_rows<T, D, RT, W, true, false>(p, c, ws, st);
+  return run<T, D>(p, c, attn_rows_kernel<T, D, RT, WIDE, STREAM>, 64 * WAVES, (size_t)(WAVES * 16 * (D + PAD) + WAVES * 16 * 2) * sizeof(float), once, ws, st);
 }
 template <typename T, int D, int RT> hipError_t run_rows(const RowsParams& p, const Plan& c, void* ws, hipStream_t st) {
-  return c.waves == 8 ? run_rows<T, D, RT, 8>(p, c, ws, st) : run_rows<T, D, RT, 4>(p, c, ws, st);
+  if (sizeof(T) == 2 && p.P < 32) return run_rows<T, D, RT, sizeof(T) != 2, false>(p, c, ws, st);
+  return c.stream ? run_rows<T, D, RT, true, true>(p, c, ws, st) : run_rows<T, D, RT, true, false>(p, c, ws, st);
 }
 // (instantiated for one type and head dim per source file, which are compiled side by side)
 template <typename T, int D> hipError_t attn(const RowsParams& p, void* ws, hipStream_t st) {

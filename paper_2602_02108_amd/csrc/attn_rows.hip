@@ -6,8 +6,8 @@ namespace oomb {
 size_t rows_attn_workspace_bytes(const RowsParams& p, bool is_bf16, int32_t sel_stride) { return part_bytes(p, plan_of(p, is_bf16, sel_stride)); }
 int64_t rows_attn_blocks(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   const Plan c = plan_of(p, is_bf16, sel_stride);
-  const int64_t attn = c.blocks * (c.tiles ? 1 : c.waves / 4), combine = c.split ? combine_blocks(p, c) : 0;   // (in workgroups of 256 threads)
-  return attn > combine ? attn : combine;
+  const int64_t combine = c.split ? combine_blocks(p, c) : 0;
+  return c.blocks > combine ? c.blocks : combine;
 }
 
 hipError_t launch_attn_rows(const RowsParams& p, bool is_bf16, void* ws, hipStream_t st) {

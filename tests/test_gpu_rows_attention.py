@@ -294,6 +294,59 @@ def test_parts_of_rows(dt, Hq, Hkv, D, P, spans):
     _verify(b, q, pools, 0.1, o, lse)
 
 
+def _spread(n, rows, tokens, seed):
+    """Spans of n sequences: lengths over their logarithm, some empty, some without rows, some of fewer tokens than rows."""
+    rng = np.random.default_rng(seed)
+    spans = []
+    for _ in range(n):
+        t = int(np.exp(rng.uniform(0, np.log(tokens + 1)))) if rng.random() < 0.95 else 0
+        spans.append((int(rng.integers(1, rows + 1)) if rng.random() < 0.9 else 0, t))
+    spans[n // 3], spans[-1] = (rows, tokens), (0, 3)
+    return spans
+
+
+@pytest.mark.parametrize("dt,Hq,Hkv,D,P,n,rows,tokens,listed", [
+    (BF, 4, 2, 128, 16, 140, 1, 3000, False),      # cut
+    (BF, 4, 2, 128, 16, 270, 1, 3000, False),      # more sequences and heads than a workgroup counts by itself
+    (BF, 6, 2, 64, 32, 300, 5, 900, True),
+    (F32, 4, 4, 128, 32, 170, 5, 900, True),
+    (F32, 4, 4, 64, 16, 70, 9, 1500, False),
+    (F32, 2, 2, 128, 64, 129, 40, 400, True),      # not cut
+    (BF, 2, 2, 64, 16, 2100, 1, 300, False),       # more than the planner takes at a time
+    (BF, 4, 2, 64, 16, 2500, 2, 700, True),
+    (BF, 8, 1, 128, 16, 4097, 1, 40, False),
+    (BF, 16, 8, 64, 16, 40, 200, 1200, False),     # in tiles
+])
+def test_many_sequences(dt, Hq, Hkv, D, P, n, rows, tokens, listed):
+    spans = _spread(n, rows, tokens, 3)
+    b = ru.Batch(spans, P, 18)
+    lists = None
+    if listed:
+        rng = np.random.default_rng(9)
+        lists = [[sorted(int(x) for x in rng.permutation(-(-t // P))[:rng.integers(0, -(-t // P) + 1)]) for _ in range(Hkv)] for _, t in spans]
+    q = _queries(b, Hq, D, dt, 14)
+    pools = [pu.random_pool(b, Hkv, D, dt, s) for s in (25, 26)]
+    o, lse = _run(b, q, pools, 0.1, lists)
+    _verify(b, q, pools, 0.1, o, lse, lists)
+    ws = torch.full((1 << 28,), 127, dtype=torch.uint8, device="cuda")
+    o2, lse2 = _run(b, q, pools, 0.1, lists, workspace=ws)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("B", [200, 300])
+def test_many_sequences_of_equal_rows_and_lengths(B):
+    """Without starts and lengths."""
+    Hq, Hkv, D, P, t = 4, 2, 64, 16, 40
+    b = ru.Batch([(2, t)] * B, P, 18, behind=0)
+    q = _queries(b, Hq, D, BF, 14)
+    pools = [pu.random_pool(b, Hkv, D, BF, s) for s in (25, 26)]
+    table = torch.tensor(b.tables, device="cuda")
+    desc = api.make_rows_desc(q.cuda(), pools[0].cuda(), table, t, 0.1, max_rows=2)
+    o, lse = api.paged_attn_fwd_rows(desc, q.cuda(), *(x.cuda() for x in pools), table)
+    torch.cuda.synchronize()
+    _verify(b, q, pools, 0.1, o, lse)
+
+
 def test_logits_of_minus_infinity_have_no_weight():
     P, D = 16, 64
     for dt in (BF, F32):
