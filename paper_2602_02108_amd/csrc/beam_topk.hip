@@ -22,11 +22,11 @@ namespace {
 
 constexpr int THREADS = 256;                    // of the first kernel
 constexpr int LOADS = 4;                        // of 16 bytes, of a thread at a time
-constexpr int MOST_LISTS = 256;                 // slices of a group's rows
-constexpr int MOST_SLICES = 64;
+constexpr int MOST_LISTS = 64;                  // slices of a group's rows (or one a row): the second kernel takes in 10 B/ns (one group of 8 x 130,999: 16 us, with 256 lists 41)
 constexpr int GROUP_THREADS = 1024;             // of the second
 constexpr int GROUP_WAVES = GROUP_THREADS / 64;
-constexpr int HELD = 16;                        // cells that a thread of it keeps in registers
+constexpr int HELD = MOST_LISTS * THREADS / GROUP_THREADS;   // cells of a thread of it
+static_assert(BEAM_MOST_BEAMS <= MOST_LISTS, "a row has a list at least");
 constexpr int CELLS = 4096;                     // that reach the first bound
 constexpr int HOLDERS = 1024;                   // of them, that reach the bound
 constexpr int ROOM = GROUP_THREADS;             // candidates that do
@@ -254,7 +254,6 @@ template <typename T> __global__ __launch_bounds__(GROUP_THREADS) void beam_grou
     keys[j] = 0;
     if (j * GROUP_THREADS < n_cells) mine = max(mine, keys[j] = cell(tid + j * GROUP_THREADS, held[j]));
   }
-  for (int i = tid + HELD * GROUP_THREADS; i < n_cells; i += GROUP_THREADS) mine = max(mine, cell(i, cells[i]));
   // A bound that K cells reach at least: of the maxima of 64 groups of threads (rows of 16 lanes) the K-th best, by one wave
   const uint32_t group_top = row_max(mine);
   if ((lane & 15) == 15) tops[tid / 16] = group_top;
@@ -277,7 +276,6 @@ template <typename T> __global__ __launch_bounds__(GROUP_THREADS) void beam_grou
 #pragma unroll
     for (int j = 0; j < HELD; ++j)
       if (j * GROUP_THREADS < n_cells) note(tid + j * GROUP_THREADS, keys[j]);
-    for (int i = tid + HELD * GROUP_THREADS; i < n_cells; i += GROUP_THREADS) note(i, cell(i, cells[i]));
   }
   __syncthreads();
   const int noted = n_cell;
@@ -378,7 +376,7 @@ struct Cut { int slices, tiles; };
 template <typename T> Cut cut_of(const BeamParams& p) {
   const int64_t rows = (int64_t)p.n_groups * p.n_beams;
   const int tiles = (int)(((int64_t)p.vocab + VEC<T> - 1 + TILE<T> - 1) / TILE<T>);   // (a row may begin anywhere in 16 bytes)
-  int most = std::min(MOST_SLICES, MOST_LISTS / p.n_beams);
+  int most = MOST_LISTS / p.n_beams;
   const int64_t wanted = (1024 + rows - 1) / rows;
   most = (int)std::min<int64_t>(most, std::max<int64_t>(1, wanted));
   const int each = (tiles + std::min(tiles, most) - 1) / std::min(tiles, most);

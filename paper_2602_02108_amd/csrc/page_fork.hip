@@ -4,8 +4,8 @@
 //
 // What bounds it: launches and loads that wait for each other (parent, length, page, count), so few pages take one workgroup that holds the counts in the
 // LDS (tables of 64 rows of 34: 6 us in one launch, 9 in two).  More pages: the plan (one workgroup, since every child's new pages follow from the needs of those
-// before it) reads the counts only as far as free pages are needed, the tables are written by the whole chip.  Copies: memory, 236 MB read
-// and written in about 45 us.
+// before it) reads the counts only as far as free pages are needed, of a large pool the whole chip lists them first; the tables are written by the whole chip.
+// Copies: memory, 236 MB read and written in about 45 us.
 #include "gen.h"
 #include "wave.h"
 
@@ -17,18 +17,22 @@ constexpr int PLAN_THREADS = 1024;
 constexpr int SCAN = 8;             // reference counts of a thread at a time
 constexpr int ROW_THREADS = 256, ROW_ENTRIES = 1024;   // of a workgroup that rewrites a part of a table's row
 constexpr int COPY_THREADS = 256;
-constexpr int COMPACT_THREADS = 1024, COMPACT_EACH = 4, COMPACT_BLOCK = COMPACT_THREADS * COMPACT_EACH;
+constexpr int COMPACT_THREADS = 1024, COMPACT_EACH = 4, COMPACT_BLOCK = COMPACT_THREADS * COMPACT_EACH;   // pages of a workgroup that counts
+constexpr int LARGE_POOL = 32768;   // a fork counts the free pages of more with many workgroups (150,000 pages, the free ones last: 10 us, by the plan alone 79)
+
+__host__ __device__ int page_blocks(int64_t num_phys) { return (int)((num_phys + COMPACT_BLOCK - 1) / COMPACT_BLOCK); }
 
 // What the plan leaves for the second kernel.
 struct Child { int32_t was, now, first, copied; };      // tokens before and after, its first new page among all, whether the partly filled page is copied
 struct Parent { int32_t children, keeps, pages, held; };   // whether a child keeps the partly filled page; entries that its row counts; full pages that children share
-struct ForkWs { int32_t* found; Child* child; Parent* parent; int32_t* free_pages; };
-__host__ __device__ ForkWs fork_ws(void* ws, int32_t n_seqs, int32_t n_out) {
+struct ForkWs { int32_t* found; Child* child; Parent* parent; int32_t *free_pages, *counts; };   // counts: free pages of each block of pages, in a large pool
+__host__ __device__ ForkWs fork_ws(void* ws, int32_t n_seqs, int32_t n_out, int32_t num_phys) {
   ForkWs w;
   w.found = (int32_t*)ws;
   w.child = (Child*)((char*)ws + 16);
   w.parent = (Parent*)(w.child + n_out);
   w.free_pages = (int32_t*)(w.parent + n_seqs);
+  w.counts = w.free_pages + num_phys;
   return w;
 }
 
@@ -53,15 +57,48 @@ template <int THREADS> __device__ __forceinline__ int block_scan(int x, int* sum
 
 __device__ __forceinline__ int valid(const ForkParams& p, int x) { return x >= 0 && x < p.num_phys ? x : -1; }
 
-// Workgroup 0 plans; the others (if the counts are kept in another place) copy the reference counts.
-__global__ __launch_bounds__(PLAN_THREADS) void fork_plan_kernel(ForkParams p, void* ws) {
-  const ForkWs w = fork_ws(ws, p.n_seqs, p.n_out);
+// The free pages of each block of a large pool; the counts in their other place, if they get one.
+__global__ __launch_bounds__(COMPACT_THREADS) void fork_count_kernel(ForkParams p, void* ws) {
+  __shared__ int sums[COMPACT_THREADS / 64];
+  const int64_t at = (int64_t)blockIdx.x * COMPACT_BLOCK + threadIdx.x * COMPACT_EACH;
+  int n = 0, total;
+#pragma unroll
+  for (int j = 0; j < COMPACT_EACH; ++j)
+    if (at + j < p.num_phys) {
+      const int r = p.refs[at + j];
+      n += r == 0;
+      if (p.refs_out != p.refs) p.refs_out[at + j] = r;
+    }
+  block_scan<COMPACT_THREADS>(n, sums, total);
+  if (threadIdx.x == 0) fork_ws(ws, p.n_seqs, p.n_out, p.num_phys).counts[blockIdx.x] = total;
+}
+
+// Workgroup 0 plans.  The others: in a large pool the free pages of a block each, ascending; else the reference counts in their other place, if they get one.
+__global__ __launch_bounds__(PLAN_THREADS) void fork_plan_kernel(ForkParams p, void* ws, int blocks) {   // blocks: of a large pool; else 0
+  const ForkWs w = fork_ws(ws, p.n_seqs, p.n_out, p.num_phys);
+  __shared__ int sums[PLAN_THREADS / 64];
+  if (blockIdx.x > 0 && blocks) {
+    const int block = blockIdx.x - 1;
+    int lower = 0, before, total;
+    for (int i = threadIdx.x; i < block; i += PLAN_THREADS) lower += w.counts[i];
+    block_scan<PLAN_THREADS>(lower, sums, before);
+    const int64_t at = (int64_t)block * COMPACT_BLOCK + threadIdx.x * COMPACT_EACH;
+    bool is[COMPACT_EACH];
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < COMPACT_EACH; ++j) n += is[j] = at + j < p.num_phys && p.refs[at + j] == 0;
+    int k = before + block_scan<PLAN_THREADS>(n, sums, total);
+#pragma unroll
+    for (int j = 0; j < COMPACT_EACH; ++j)
+      if (is[j]) w.free_pages[k++] = (int)(at + j);
+    return;
+  }
   if (blockIdx.x > 0) {
     const int64_t i = (int64_t)(blockIdx.x - 1) * PLAN_THREADS + threadIdx.x;
     if (i < p.num_phys) p.refs_out[i] = p.refs[i];
     return;
   }
-  __shared__ int children[FORK_MOST_SEQS], first[FORK_MOST_SEQS], sums[PLAN_THREADS / 64];
+  __shared__ int children[FORK_MOST_SEQS], first[FORK_MOST_SEQS];
   for (int s = threadIdx.x; s < p.n_seqs; s += PLAN_THREADS) { children[s] = 0; first[s] = 0x7fffffff; }
   __syncthreads();
   for (int b = threadIdx.x; b < p.n_out; b += PLAN_THREADS) {
@@ -111,7 +148,12 @@ __global__ __launch_bounds__(PLAN_THREADS) void fork_plan_kernel(ForkParams p, v
 
   // the free pages, ascending, as many as are needed
   int found = 0;
-  for (int64_t i0 = 0; i0 < p.num_phys && found < need_before; i0 += PLAN_THREADS * SCAN) {
+  if (blocks) {
+    int n = 0;
+    for (int i = threadIdx.x; i < blocks; i += PLAN_THREADS) n += w.counts[i];
+    block_scan<PLAN_THREADS>(n, sums, found);
+  }
+  for (int64_t i0 = 0; !blocks && i0 < p.num_phys && found < need_before; i0 += PLAN_THREADS * SCAN) {
     const int64_t at = i0 + (int64_t)threadIdx.x * SCAN;
     int r[SCAN];
 #pragma unroll
@@ -139,7 +181,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void fork_plan_kernel(ForkParams p, v
 
 // Workgroups of children write their rows, workgroups of parents take their references back.
 __global__ __launch_bounds__(ROW_THREADS) void fork_rows_kernel(ForkParams p, void* ws, int pieces) {
-  const ForkWs w = fork_ws(ws, p.n_seqs, p.n_out);
+  const ForkWs w = fork_ws(ws, p.n_seqs, p.n_out, p.num_phys);
   const int row = blockIdx.x / pieces, l0 = (blockIdx.x - row * pieces) * ROW_ENTRIES + threadIdx.x;
   const int P = 1 << p.log2_p;
   if (row < p.n_out) {
@@ -219,7 +261,7 @@ __global__ __launch_bounds__(COPY_THREADS) void page_copy_kernel(CopyParams p, C
 // n used pages; the i-th used page from n on moves to the i-th free page below n.
 struct CompactWs { int32_t* counts; int32_t* becomes; };   // used pages of each block; a page's new number: -1, itself, or num_phys + i if it is the i-th to move
 __host__ __device__ CompactWs compact_ws(void* ws, int32_t num_phys) {
-  const int32_t blocks = (num_phys + COMPACT_BLOCK - 1) / COMPACT_BLOCK;
+  const int32_t blocks = page_blocks(num_phys);
   return {(int32_t*)ws, (int32_t*)ws + ((blocks + 3) & ~3)};
 }
 __device__ __forceinline__ int used_of(const CompactParams& p, int64_t at, int64_t end, bool (&used)[COMPACT_EACH]) {
@@ -535,7 +577,7 @@ uint32_t magic_of(int32_t cols) { return (uint32_t)(((1ull << 32) + cols - 1) / 
 }  // namespace
 
 size_t fork_workspace_bytes(int32_t n_seqs, int32_t n_out, int64_t num_phys) {
-  return 16 + sizeof(Child) * (size_t)n_out + sizeof(Parent) * (size_t)n_seqs + sizeof(int32_t) * (size_t)num_phys;
+  return 16 + sizeof(Child) * (size_t)n_out + sizeof(Parent) * (size_t)n_seqs + sizeof(int32_t) * (size_t)(num_phys + page_blocks(num_phys));
 }
 int64_t fork_blocks(const ForkParams& p) { return ((int64_t)p.n_out + p.n_seqs) * fork_pieces(p); }
 hipError_t launch_page_fork(const ForkParams& p, void* ws, hipStream_t st) {
@@ -553,8 +595,14 @@ hipError_t launch_page_fork(const ForkParams& p, void* ws, hipStream_t st) {
   }
   {
     ProfScope prof_("fork_plan", st);
-    const unsigned more = p.refs_out == p.refs ? 0 : (unsigned)(((int64_t)p.num_phys + PLAN_THREADS - 1) / PLAN_THREADS);
-    fork_plan_kernel<<<dim3(1 + more), dim3(PLAN_THREADS), 0, st>>>(p, ws);
+    const int blocks = p.num_phys > LARGE_POOL ? page_blocks(p.num_phys) : 0;
+    if (blocks) {
+      fork_count_kernel<<<dim3((unsigned)blocks), dim3(COMPACT_THREADS), 0, st>>>(p, ws);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    const unsigned more = blocks ? (unsigned)blocks : p.refs_out == p.refs ? 0 : (unsigned)(((int64_t)p.num_phys + PLAN_THREADS - 1) / PLAN_THREADS);
+    fork_plan_kernel<<<dim3(1 + more), dim3(PLAN_THREADS), 0, st>>>(p, ws, blocks);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -564,7 +612,7 @@ hipError_t launch_page_fork(const ForkParams& p, void* ws, hipStream_t st) {
 }
 
 size_t compact_workspace_bytes(int64_t num_phys) {
-  const int64_t blocks = (num_phys + COMPACT_BLOCK - 1) / COMPACT_BLOCK;
+  const int64_t blocks = page_blocks(num_phys);
   return sizeof(int32_t) * (size_t)(((blocks + 3) & ~3) + num_phys);
 }
 int64_t compact_blocks(const CompactParams& p) { return compact_move_blocks(p) + (int64_t)p.n_seqs * pieces_of(p.cols); }
@@ -580,7 +628,7 @@ hipError_t launch_page_compact(const CompactParams& p, void* ws, hipStream_t st)
     compact_small_kernel<<<dim3(1), dim3(PLAN_THREADS), lds, st>>>(p, magic_of(p.cols));
     return hipGetLastError();
   }
-  const unsigned blocks = (unsigned)(((int64_t)p.num_phys + COMPACT_BLOCK - 1) / COMPACT_BLOCK);
+  const unsigned blocks = (unsigned)page_blocks(p.num_phys);
   {
     ProfScope prof_("compact_rank", st);
     compact_count_kernel<<<dim3(blocks), dim3(COMPACT_THREADS), 0, st>>>(p, ws);

@@ -111,6 +111,26 @@ def test_fork_of_many(n_seqs, n_out, P, n_phys):
         t, ln = got.tables, got.lens
 
 
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("n_phys,free", [(32768, 90), (32769, 90), (150001, 90), (150001, 2), (150001, 0), (70000, 9000)])
+def test_fork_of_large_pools(n_phys, free, in_place):
+    """The free pages are the last ones, or fewer than needed, or none; two of the counts are negative, which frees nothing."""
+    P, cols, n = 16, 8, 50
+    spans = [5 + i for i in range(n)]
+    tables = [[7 * i + l if l < -(-t // P) else -1 for l in range(cols)] for i, t in enumerate(spans)]
+    refs = [1] * (n_phys - free) + [0] * free
+    refs[n_phys // 2] = refs[n_phys - free - 1] = -1
+    parents, grow = [(3 * b) % n for b in range(n)], [1] * n
+    want = gu.fork(tables, spans, parents, grow, refs, P, cols)
+    r = _i(refs)
+    out = None if in_place else torch.full((n_phys,), 77, dtype=torch.int32, device="cuda")
+    got = api.page_fork(_i(tables), _i(spans), _i(parents), r, P, grow=_i(grow), refs_out=out)
+    torch.cuda.synchronize()
+    assert got.tables.tolist() == want[0] and got.lens.tolist() == want[1] and got.refs.tolist() == want[2]
+    assert got.copies.tolist() == want[3] and got.status.tolist() == want[4]
+    assert (got.refs is r) if in_place else r.tolist() == refs
+
+
 @pytest.mark.parametrize("more", [0, 9000])
 def test_counts_of_pages_held_besides(more):
     """A page that somebody outside holds: the first child copies it too, and it does not become free."""
