@@ -6,7 +6,8 @@
 // exponentials against it.  The second one, a workgroup per group, adds the sums, which makes candidates of different beams comparable, and looks for the K best
 // through the cells: the K-th best cell maximum is a bound that K candidates reach at least; only the few cells that reach it are read again, and the rank of
 // each of their values above the bound is counted.  Candidates are compared in 64 bits, ties go to the lowest w * vocab + v.
-// Where very many values are equal the bound does not sort them out; then a group is walked in order of its places, the K best so far in hand.
+// Where very many values are equal (logits masked with a finite value, fewer than K others) the bound does not sort them out; then those equal to it are taken
+// in order of their places.
 //
 // What bounds it: the first kernel, the reading of the logits (256 rows of 130,999 bf16: 67 MB in 15 us, 4.5 TB/s; a maximum costs one instruction an element, where the
 // best of each slice kept on the way made both kernels 154 us instead of 25); the second, one workgroup a group and its chain of steps (cells, bound, values, ranks),
@@ -27,8 +28,8 @@ constexpr int GROUP_THREADS = 1024;             // of the second
 constexpr int GROUP_WAVES = GROUP_THREADS / 64;
 constexpr int HELD = MOST_LISTS * THREADS / GROUP_THREADS;   // cells of a thread of it
 static_assert(BEAM_MOST_BEAMS <= MOST_LISTS, "a row has a list at least");
-constexpr int CELLS = 4096;                     // that reach the first bound
-constexpr int HOLDERS = 1024;                   // of them, that reach the bound
+constexpr int CELLS = 1024;                     // that reach the first bound (about 300 of equally distributed values at most)
+constexpr int HOLDERS = 256;                    // of them, that reach the bound
 constexpr int ROOM = GROUP_THREADS;             // candidates that do
 constexpr int PARTS = 8;                        // threads that count a rank together
 template <typename T> constexpr int VEC = 16 / (int)sizeof(T);
@@ -205,7 +206,7 @@ template <typename T> __global__ __launch_bounds__(GROUP_THREADS) void beam_grou
   __shared__ uint32_t holder[HOLDERS];
   __shared__ uint64_t ended_val[BEAM_MOST_BEAMS], ended_at[BEAM_MOST_BEAMS];
   __shared__ int n_cell, n_hold, n_cand;
-  __shared__ uint64_t top_val;
+  __shared__ uint8_t ties[BEAM_MOST_BEAMS];        // whether a beam has cells that equal the K-th best
   __shared__ __align__(16) Cands c;
   const float* cells = w.cells + (int64_t)group * n_cells;
   float held[HELD];                              // (on their way while the log-sums are formed; of a row that offers nothing they are not used)
@@ -213,7 +214,7 @@ template <typename T> __global__ __launch_bounds__(GROUP_THREADS) void beam_grou
   for (int j = 0; j < HELD; ++j)
     if (j * GROUP_THREADS < n_cells) held[j] = cells[min(tid + j * GROUP_THREADS, n_cells - 1)];
   if (tid < lists) beam_of[tid] = (uint8_t)(tid / slices);
-  if (tid == 0) { n_cell = n_hold = n_cand = 0; bound = 0; top_val = 0; }
+  if (tid == 0) { n_cell = n_hold = n_cand = 0; bound = 0; }
   __syncthreads();
   for (int beam = wave; beam < p.n_beams; beam += GROUP_WAVES) {
     const int64_t row = (int64_t)group * p.n_beams + beam;
@@ -333,32 +334,75 @@ template <typename T> __global__ __launch_bounds__(GROUP_THREADS) void beam_grou
     }
   }
   if (!found) {
-    // Very many equal values.  Every place in order, what is no better than the K-th best so far left out, until nothing better can come.
+    // Very many values are equal.  The K-th best cell in 64 bits: what reaches it stands in the cells that do, and if they are many, in the fewer than K above
+    // it and at the lowest places that equal it.
     if (tid < n_ended) { c.val[tid] = ended_val[tid]; c.at[tid] = ended_at[tid]; }
-    for (int i = tid; i < n_cells; i += GROUP_THREADS) {
-      const uint64_t v = value(beam_of[i / THREADS], cells[i]);
-      if (v) atomicMax((unsigned long long*)&top_val, (unsigned long long)v);
+    if (tid < p.n_beams) ties[tid] = 0;
+    n_best = keep_best(c, n_ended, 0, K);
+    if (tid == 0) n_hold = 0;
+    uint64_t top[HELD];
+#pragma unroll
+    for (int j = 0; j < HELD; ++j) {
+      const int i = tid + j * GROUP_THREADS;
+      top[j] = i < n_cells ? value(beam_of[i / THREADS], cells[i]) : 0;
+    }
+    uint64_t edge = 0;
+    int reach = 0;
+    for (int bit = 63; bit >= 0; --bit) {
+      const uint64_t to = edge | 1ull << bit;
+      int n = 0;
+#pragma unroll
+      for (int j = 0; j < HELD; ++j) n += __popcll(__ballot(top[j] >= to));
+      if (lane == 0) tops[(bit & 1) * GROUP_WAVES + wave] = n;
+      __syncthreads();
+      int all = 0;
+#pragma unroll
+      for (int w = 0; w < GROUP_WAVES; ++w) all += tops[(bit & 1) * GROUP_WAVES + w];
+      if (all >= K) { edge = to; reach = all; }
+    }
+    edge = max(edge, (uint64_t)1);               // (fewer than K cells hold anything: all of it)
+    const bool few = reach <= HOLDERS;
+#pragma unroll
+    for (int j = 0; j < HELD; ++j) {
+      if (top[j] > edge || (few && top[j] == edge)) holder[atomicAdd(&n_hold, 1)] = tid + j * GROUP_THREADS;
+      else if (top[j] == edge) ties[beam_of[(tid + j * GROUP_THREADS) / THREADS]] = 1;
     }
     __syncthreads();
-    n_best = keep_best(c, n_ended, 0, K);
+    auto offer = [&](uint64_t v, uint64_t at) __attribute__((always_inline)) {   // a candidate of each thread; 0: none
+      const uint64_t worst = n_best == K ? c.best_val[K - 1] : 0, worst_at = n_best == K ? c.best_at[K - 1] : 0;
+      const bool better = v > worst || (v && v == worst && at < worst_at);
+      if (tid == 0) n_cand = 0;
+      if (!__syncthreads_or(better)) return;
+      if (better) {
+        const int to = atomicAdd(&n_cand, 1);
+        c.val[to] = v;
+        c.at[to] = at;
+      }
+      __syncthreads();
+      n_best = keep_best(c, n_cand, n_best, K);
+    };
+    const int each = slice_tiles * LOADS * VEC<T>;
+    const int64_t n_held = (int64_t)n_hold * each;
+    for (int64_t e0 = 0; e0 < n_held; e0 += GROUP_THREADS) {
+      const int64_t e = min(e0 + tid, n_held - 1);
+      const int h = (int)(e / each), i = (int)(e - (int64_t)h * each), id = holder[h], list = id / THREADS, beam = beam_of[list];
+      const Row<T> x(p, (int64_t)group * p.n_beams + beam);
+      const int64_t at = place_of<T>(list - beam * slices, slice_tiles, i / VEC<T>, id % THREADS) + i % VEC<T>;
+      const uint64_t v = e0 + tid < n_held && at >= x.lead && at < x.end ? value(beam, Elem<T>::load(x.from + at)) : 0;
+      offer(v >= edge ? v : 0, (uint64_t)beam << 32 | (uint32_t)(at - x.lead));
+    }
     for (int beam = 0; beam < p.n_beams; ++beam) {
-      if (!(base[beam] > -(double)INFINITY)) continue;
+      if (!ties[beam]) continue;
       const Row<T> x(p, (int64_t)group * p.n_beams + beam);
       for (int64_t v0 = 0; v0 < p.vocab; v0 += GROUP_THREADS) {
-        const uint64_t worst = n_best == K ? c.best_val[K - 1] : 0, worst_at = n_best == K ? c.best_at[K - 1] : 0;
-        if (worst > top_val || (worst == top_val && worst_at < ((uint64_t)beam << 32 | (uint32_t)v0))) break;   // (a beam that has ended may stand behind)
-        const int64_t token = v0 + tid;
-        const uint64_t v = token < p.vocab ? value(beam, Elem<T>::load(x.from + x.lead + token)) : 0, at = (uint64_t)beam << 32 | (uint32_t)token;
-        const bool better = v > worst || (v && v == worst && at < worst_at);
-        if (tid == 0) n_cand = 0;
-        if (!__syncthreads_or(better)) continue;
-        if (better) {
-          const int to = atomicAdd(&n_cand, 1);
-          c.val[to] = v;
-          c.at[to] = at;
+        if (n_best == K && (c.best_val[K - 1] > edge || (c.best_val[K - 1] == edge && c.best_at[K - 1] < ((uint64_t)beam << 32 | (uint32_t)v0)))) break;
+        const int64_t at = x.lead + min(v0 + tid, (int64_t)p.vocab - 1);
+        uint64_t v = v0 + tid < p.vocab ? value(beam, Elem<T>::load(x.from + at)) : 0;
+        if (v == edge) {                         // (in a cell above the edge it has been offered)
+          const int slice = (int)(at / ((int64_t)slice_tiles * TILE<T>)), thread = (int)(at / VEC<T> % THREADS);
+          if (value(beam, cells[(beam * slices + slice) * THREADS + thread]) != edge) v = 0;
         }
-        __syncthreads();
-        n_best = keep_best(c, n_cand, n_best, K);
+        offer(v == edge ? v : 0, (uint64_t)beam << 32 | (uint32_t)(at - x.lead));
       }
     }
   }

@@ -267,6 +267,35 @@ def test_beam_of_equal_logits_takes_the_lowest():
     _verify_beam(x, s, 33, _beam(x, s, 33))
 
 
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("V", [300, 5000, 131072])
+@pytest.mark.parametrize("mask", [-1e4, "least"])
+def test_beam_of_logits_masked_with_a_finite_value(dt, V, mask):
+    """Fewer live tokens than candidates: the first masked ones, by score and place, fill up."""
+    gen = torch.Generator().manual_seed(V)
+    least = torch.finfo(dt).min if mask == "least" else mask
+    x = torch.full((4, 5, V), least).to(dt)
+    for g in range(4):
+        for w in range(5):
+            live = torch.randperm(V, generator=gen)[:int(torch.randint(1, 4, (1,), generator=gen))]
+            x[g, w, live] = (torch.randn(len(live), generator=gen) * 4).to(dt)
+    s = -20 * torch.rand((4, 5), generator=gen)
+    done = torch.zeros((4, 5), dtype=torch.int32)
+    done[1, 2] = done[3, 0] = done[3, 1] = 1
+    for n_out in (1, 16, 64):
+        _verify_beam(x, s, n_out, _beam(x, s, n_out, done, 1), done, 1)
+
+
+def test_beam_of_few_cells_with_many_values_above_equal_ones():
+    """More values above the common one than are ranked at a time, all in a few threads' places."""
+    V = 400000
+    v = torch.arange(V)
+    for many in (1, 7):
+        x = torch.where((v // 4) % 256 == 0, 1 + (v * many % 4001) / 4096.0, torch.tensor(0.25)).expand(1, 1, V).contiguous()
+        for n_out in (1, 50, 64):
+            _verify_beam(x, torch.zeros((1, 1)), n_out, _beam(x, torch.zeros((1, 1)), n_out))
+
+
 @pytest.mark.parametrize("n_out", [1, 2, 3])
 def test_beam_that_has_ended_stands_behind_equal_ones(n_out):
     """Scores so large that log-sums vanish in them: every candidate of a group is equal, and the lowest places win over those of beams that have ended."""
