@@ -20,7 +20,7 @@
 // What bounds it.  Few rows: the reading of the cache (28 heads over 4 of 128 dims, bf16, 1M tokens: 2.1 GB in 323 us, 6.6 TB/s, of which the join takes 6; fp32 5.5),
 // where it is short two launches and a chain of loads that wait for each other (lengths, page, rows; 1000 tokens 11 us).  So a wave keeps 32 KB in
 // flight, and the loop carries no LDS, no barrier and no exchange but the test of the weights.  Many rows read the cache again per block of rows: then
-// attn_tiles_kernel, below, shares a reading among 128 rows (three prompts of up to 2048 rows: 945 us here, 358 there); fp32 stays here, where the
+// attn_tiles_kernel, below, shares a reading among 128 rows (three prompts of up to 1021 rows: 945 us here, 342 there); fp32 stays here, where the
 // fp32 matrix instructions bound it (1024 rows over 16K tokens, 28 / 4 heads of 128: 2219 us, 105 TFLOP/s; the library's fp32 product 136).
 #pragma once
 #include <type_traits>
@@ -704,7 +704,7 @@ __global__ __launch_bounds__(COMBINE_THREADS) void attn_combine_kernel(RowsParam
 // holds one query row.  The softmax as above.
 // What bounds it: the matrix unit and the power it draws (4096 rows over 16K tokens, 28 / 4 heads of 128: 1175 us, 0.72 PFLOP/s, 1.08 with the weights' second
 // terms; a library product of 8192^3 1.21).  32 rows a wave and a stage of 64 tokens twice are what registers and LDS hold for two workgroups a compute unit.  First form,
-// softmax and products one after the other, 396 us for three prompts; in one pipeline with the accumulators where they are 358.
+// softmax and products one after the other, 396 us for three prompts; in one pipeline with the accumulators where they are 342.
 // A row tile in the LDS: rows of 2 D bytes, granule c (16 bytes) of row r at c ^ f(r).  Head dim 128: that of mfma_common.h.  Head dim 64: two rows share a
 // line of 256 bytes, f(r) = 4 ((r / 2) % 2) + (r / 4) % 4: 16 rows read at one granule, and the 4 rows x 64 bytes of a transposing read, use every bank once.
 constexpr int TILE_ROWS = 128, TILE_STAGE = 64, TILE_THREADS = 256;

@@ -347,6 +347,47 @@ def test_many_sequences_of_equal_rows_and_lengths(B):
     _verify(b, q, pools, 0.1, o, lse)
 
 
+def test_many_sequences_in_a_captured_step():
+    """Lengths, rows and tables that change between the replays: each of them the bits of an eager call, with the program's own work in between."""
+    P, Hq, Hkv, D, n, dt = 16, 4, 2, 64, 300, BF
+    spans = [_spread(n, 3, 900, s) for s in (1, 2, 3)]
+    batches = [ru.Batch(x, P, 5) for x in spans]
+    rows, cols, n_phys = max(b.n_rows for b in batches), 60, max(b.n_phys for b in batches)
+    gen = torch.Generator().manual_seed(3)
+    pools = [torch.randn((n_phys, Hkv, P, D), generator=gen).to(dt).cuda() for _ in range(2)]
+    q = torch.randn((rows, Hq, D), generator=gen).to(dt).cuda()
+    table, lens = torch.zeros((n, cols), dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")
+    starts = torch.zeros(n + 1, dtype=torch.int32, device="cuda")
+    desc = api.make_rows_desc(q, pools[0], table, cols * P, 0.1, max_rows=3)
+    ws = torch.empty(api.rows_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    o, lse = torch.zeros((rows, Hq, D), dtype=dt, device="cuda"), torch.zeros((Hq, rows), device="cuda")
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            api.paged_attn_fwd_rows(desc, q, *pools, table, o=o, lse=lse, workspace=ws, seq_lens=lens, row_starts=starts)
+    for i in (0, 1, 2, 1, 0):
+        b = batches[i]
+        table[:, :b.cols] = torch.tensor(b.tables, device="cuda")
+        lens.copy_(torch.tensor([t for _, t in b.spans], dtype=torch.int32))
+        starts.copy_(torch.tensor(b.starts, dtype=torch.int32))
+        o.fill_(5.0)
+        lse.fill_(5.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        o2, lse2 = torch.full_like(o, 5.0), torch.full_like(lse, 5.0)
+        api.paged_attn_fwd_rows(desc, q, *pools, table, o=o2, lse=lse2, seq_lens=lens, row_starts=starts)
+        torch.cuda.synchronize()
+        assert torch.equal(o, o2) and torch.equal(lse, lse2)
+        q_here = q.cpu()
+        wo, wl, to, tl = pu.attend(b, q_here[:b.n_rows], *(x.cpu() for x in pools), 0.1)
+        live = slice(0, b.rows)
+        ru.check("O", o.cpu().double().numpy()[live], wo[live], to[live])
+        ru.check("LSE", lse.cpu().double().numpy()[:, live], wl[:, live], tl[:, live])
+        assert (o[b.rows:] == 5.0).all()
+
+
 def test_logits_of_minus_infinity_have_no_weight():
     P, D = 16, 64
     for dt in (BF, F32):
