@@ -494,6 +494,33 @@ def test_pool_beyond_4_gib():
     ru.check("LSE", lse.cpu().double().numpy(), wl, tl)
 
 
+@pytest.mark.parametrize("rows", [1, 4])
+@pytest.mark.parametrize("dt,D,P", [(BF, 128, 16), (BF, 64, 16), (BF, 128, 128), (BF, 64, 32), (F32, 128, 16), (F32, 64, 64)])
+def test_pools_larger_than_the_caches(dt, D, P, rows):
+    """Pools and bounds of more than 256 MB, a few pages of which hold something."""
+    Hq, Hkv = 28, 4
+    b = ru.Batch([(rows, 700), (1, 33), (0, 20), (rows, 2000)], P, 9)
+    es = 2 if dt == BF else 4
+    n_phys = (300 << 20) // (Hkv * P * D * 2 * es)
+    small = [pu.random_pool(b, Hkv, D, dt, s) for s in (1, 2)]
+    where = torch.randperm(n_phys, generator=torch.Generator().manual_seed(5))[:b.n_phys]
+    pools = [torch.full((n_phys, Hkv, P, D), math.nan, dtype=dt, device="cuda") for _ in range(2)]
+    for pool, x in zip(pools, small):
+        pool[where.cuda()] = x.cuda()
+    q = _queries(b, Hq, D, dt, 8)
+    at = b.device()
+    max_len = 1 << 19
+    table = torch.full((len(b.spans), max_len // P), -1, dtype=torch.int32)
+    held = torch.tensor(b.tables)
+    table[:, :b.cols] = torch.where(held >= 0, where[held.clamp(min=0).long()].to(torch.int32), -1)
+    at["page_tables"] = table.cuda()
+    desc = api.make_rows_desc(q.cuda(), pools[0], at["page_tables"], max_len, 0.1, max_rows=rows)
+    o, lse = torch.full(q.shape, 5.0, dtype=dt, device="cuda"), torch.full((Hq, b.n_rows), 5.0, device="cuda")
+    api.paged_attn_fwd_rows(desc, q.cuda(), *pools, at.pop("page_tables"), o=o, lse=lse, **at)
+    torch.cuda.synchronize()
+    _verify(b, q, small, 0.1, o, lse)
+
+
 def test_workspaces_hold_anything_and_results_do_not_depend_on_the_stream():
     b = ru.Batch([(1, 5000), (0, 9), (1, 1), (1, 900)], 128, 14)
     q = _queries(b, 28, 128, BF, 15)
