@@ -77,6 +77,7 @@ struct AttnArgs {
   int split;                   // whether blocks may be cut
   int even;                    // into equal shares of the longest
   int target, min_steps;       // workgroups to aim at; steps of a part at least
+  int full;                    // whether the blocks fill the chip as they are: about equal ones are not cut
   int planned;                 // whether attn_plan counts, for the whole call; else every workgroup does
   int2* parts;                 // [sequence * Hkv + KV head]: its first workgroup, parts of each of its blocks; planned: one more, the workgroups of all
   float* part;                 // [workgroup][row of the block][D] sums
@@ -96,7 +97,8 @@ struct Item { int e, block, first, index, count; Seq s; };   // e, block of its 
 __device__ __forceinline__ int steps_of_part(const AttnArgs& a, float total, int most) {
   if (!a.split) return 0x7fffffff;
   const int shares = max(1, (int)((float)a.target * (float)most / max(total, 1.0f) + 1e-3f));
-  return max(a.min_steps, a.even ? (most + shares - 1) / shares : (int)(total / (float)a.target) + 1);
+  const int per = max(a.min_steps, a.even ? (most + shares - 1) / shares : (int)(total / (float)a.target) + 1);
+  return a.full && most <= 2 * per ? max(most, per) : per;
 }
 __device__ __forceinline__ int parts_of(const AttnArgs& a, const Load& l, int per) { return a.split ? (int)(((uint32_t)l.steps + (uint32_t)per - 1) / (uint32_t)per) : 1; }
 __device__ __forceinline__ int workgroups_of(const Load& l, int parts) { return (int)min((int64_t)l.blocks * parts, (int64_t)1 << 24); }   // (a launch holds fewer; row_starts may be anything)
@@ -1019,7 +1021,7 @@ template <int D> __global__ __launch_bounds__(TILE_THREADS, 2) void attn_tiles_k
 
 // How a call is cut.
 struct Plan {
-  int tiles, rt, stream, split, planned, block_rows, step, target, min_steps;
+  int tiles, rt, stream, split, planned, full, block_rows, step, target, min_steps;
   int64_t blocks;   // workgroups at most
 };
 Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
@@ -1046,7 +1048,10 @@ Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   c.min_steps = c.tiles ? 8 : 4;
   c.planned = heads > PLANNED;
   c.split = steps > 16 && blocks <= (c.planned && !c.tiles ? 16 * WGS : 2 * WGS);   // (more fill the chip; parts of tiles take up to 66 KB a workgroup, others 8 or 16)
-  c.target = (int)(c.tiles ? WGS : blocks < WGS ? WGS - blocks / 2 : blocks);   // (parts come out rounded up: half a part more for each block)
+  // Parts come out rounded up, half a part more for each block: one round of workgroups for few blocks (32 ragged sequences, 128 blocks: to 448, 704 workgroups 48.7, 53
+  // us), shorter parts that even out for many (512 of them: to 2048, 2304 in 599, 587 us), but equal ones stay whole (1024 of 2048 tokens: 666, in halves 737).
+  c.full = !c.tiles && blocks > WGS;
+  c.target = (int)(c.tiles ? WGS : c.full ? blocks + WGS / 2 : blocks < WGS ? WGS - blocks / 2 : blocks);
   const int64_t most = (steps + c.min_steps - 1) / c.min_steps;
   const int64_t parts = c.target + blocks + 2;   // (what item_at comes to at most; two for its roundings)
   c.blocks = !c.split ? blocks : blocks * most < parts ? blocks * most : parts;
@@ -1064,7 +1069,7 @@ size_t part_bytes(const RowsParams& p, const Plan& c) {
 }
 
 template <typename T, int D, typename K> hipError_t run(const RowsParams& p, const Plan& c, K kernel, int threads, size_t lds, DeviceOnce& once, void* ws, hipStream_t st) {
-  AttnArgs a{c.block_rows, c.step, c.split, c.tiles, c.target, c.min_steps, c.planned, (int2*)ws, nullptr, nullptr, (int)c.blocks};
+  AttnArgs a{c.block_rows, c.step, c.split, c.tiles, c.target, c.min_steps, c.full, c.planned, (int2*)ws, nullptr, nullptr, (int)c.blocks};
   if (c.split) {
     a.part = (float*)ws;
     a.part_ml = a.part + c.blocks * c.block_rows * D;
