@@ -187,20 +187,12 @@ __device__ int keep_best(Cands& c, int fresh, int n_best, int K) {
   return min(all, K);
 }
 
-// The largest of a row of 16 lanes, in its last lane.
-__device__ __forceinline__ uint32_t row_max(uint32_t x) {
-  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false));   // row_shr:1
-  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false));
-  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false));
-  return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false));
-}
-
 template <typename T> __global__ __launch_bounds__(GROUP_THREADS) void beam_group_kernel(BeamParams p, void* ws, int slices, int slice_tiles) {
   const int group = blockIdx.x, K = p.n_out, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lists = p.n_beams * slices, n_cells = lists * THREADS;
   const BeamWs w = beam_ws(ws, (int64_t)p.n_groups * p.n_beams * slices);
   __shared__ double base[BEAM_MOST_BEAMS];       // score less log-sum; -infinity: the row offers nothing
   __shared__ uint8_t beam_of[MOST_LISTS];
-  __shared__ uint32_t tops[GROUP_THREADS / 16 + 1], bound;
+  __shared__ uint32_t tops[GROUP_THREADS], first_bound, bound;
   __shared__ __align__(16) uint32_t cell_key[CELLS + 8 * PARTS];
   __shared__ uint32_t cell_id[CELLS];
   __shared__ uint32_t holder[HOLDERS];
@@ -255,19 +247,22 @@ template <typename T> __global__ __launch_bounds__(GROUP_THREADS) void beam_grou
     keys[j] = 0;
     if (j * GROUP_THREADS < n_cells) mine = max(mine, keys[j] = cell(tid + j * GROUP_THREADS, held[j]));
   }
-  // A bound that K cells reach at least: of the maxima of 64 groups of threads (rows of 16 lanes) the K-th best, by one wave
-  const uint32_t group_top = row_max(mine);
-  if ((lane & 15) == 15) tops[tid / 16] = group_top;
+  // A bound that K cells reach at least: of the maxima of 64 groups of threads (of each lane over the waves: short rows fill the first threads of a list) the K-th
+  // best, by one wave
+  tops[tid] = mine;
   __syncthreads();
   if (wave == 0) {
-    const uint32_t key = (tops[lane] & ~63u) | (63 - lane);   // (no two alike; what the last bits held is let in)
+#pragma unroll
+    for (int w = 1; w < GROUP_WAVES; ++w) mine = max(mine, tops[64 * w + lane]);
+    const uint32_t key = (mine & ~63u) | (63 - lane);   // (no two alike; what the last bits held is let in)
     int rank = 0;
 #pragma unroll
     for (int i = 0; i < 64; ++i) rank += (uint32_t)__builtin_amdgcn_readlane(key, i) > key;
-    if (rank == K - 1) tops[64] = max(key & ~63u, 1u);
+    if (rank == K - 1) first_bound = max(key & ~63u, 1u);
+    mine = tops[lane];
   }
   __syncthreads();
-  const uint32_t limit = tops[64];
+  const uint32_t limit = first_bound;
   auto note = [&](int i, uint32_t key) __attribute__((always_inline)) {
     if (key < limit) return;
     const int to = atomicAdd(&n_cell, 1);
