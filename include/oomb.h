@@ -576,8 +576,8 @@ oomb_status oomb_page_copy(const oomb_copy_desc* desc, void* const* pools, const
  *   parents, tokens [n_groups][n_out] int32, scores_out [n_groups][n_out] float (not in the memory of scores): parents are rows of all groups,
  *          group * n_beams + w, as oomb_page_fork takes them
  * A logit of -infinity is never taken.  A beam whose score, or whose log-sum (a logit of +infinity or NaN, nothing but -infinity), is not finite offers nothing;
- * where candidates run out: -1, -1, -infinity.  Exponentials in fp32, their sums across threads and the candidates in 64 bits: two candidates of different beams
- * that lie within about 2^-22 of each other may change places.  n_out and n_beams up to 64.
+ * where candidates run out: -1, -1, -infinity.  Exponentials and sums of up to 32 of them in fp32, longer sums and the candidates in 64 bits: a beam's log-sum is off by
+ * 2^-18 at most, for every vocab, so two candidates of different beams that lie within 2^-17 of each other may change places.  n_out and n_beams up to 64.
  */
 typedef struct {
   int32_t n_groups, n_beams, vocab, n_out;

@@ -351,6 +351,31 @@ def test_beam_rows_of_any_alignment(dt, pad, offset):
     _verify_beam(x.cpu().view(groups, W, V), s, 12, _beam(x, s, 12))
 
 
+@pytest.mark.parametrize("dt", [F32, BF])
+@pytest.mark.parametrize("kind", ["equal", "rising"])
+def test_beam_log_sums_of_very_long_rows(kind, dt):
+    """More beams than half the lists, so that a thread walks hundreds of tiles of a row, and logits whose roundings do not average out: equal ones below the
+    best one of every thread, or ones that rise a little from tile to tile.  Log-sums are off by 2^-18 at most: an exponential of a difference d of up to 32 takes half a step
+    of d (2^-20), half a step of d log2(e) times ln 2 (2^-19 ln 2) and a step of the result (2^-23), a sum of 32 of them nine roundings (9 * 2^-24), together
+    3.1 * 2^-20; terms further below are 2^23 e^-32 of a sum at most; and everything beyond is in 64 bits.  Then one rounding to float."""
+    W, V = 33, 4000004
+    x = torch.empty((W, V), dtype=dt, device="cuda")
+    tile = torch.arange(V, device="cuda") // (4096 if dt == F32 else 8192)
+    for w in range(W):
+        if kind == "equal":
+            x[w] = -(3 + w / 11.0)
+            x[w, :2048] = 0.0
+        else:
+            x[w] = (tile * 2.0 ** -10 * (0.5 + w / 8.0)).to(dt)
+        x[w, V - 1 - 1000 * w] = 8.0 if kind == "equal" else float(x[w, -1]) + 12
+    want = np.array([float(x[w].max().double() - torch.logsumexp(x[w].double(), 0)) for w in range(W)])
+    order = np.argsort(-want, kind="stable")
+    got = _beam(x, torch.zeros((1, W)), W)
+    assert np.array_equal(np.sort(got[0][0]), np.arange(W)) and np.array_equal(got[1][0], V - 1 - 1000 * got[0][0])
+    assert (np.abs(got[2][0] - want[got[0][0]]) <= 2.0 ** -18 + 2.0 ** -24 * np.abs(want[got[0][0]])).all()
+    assert (np.abs(want[got[0][0]] - want[order]) <= 2.0 ** -17).all()      # (closer ones may change places)
+
+
 def test_beam_workspaces_hold_anything_on_any_stream():
     x, s = _logits((4, 3, 30000), BF, 51).cuda(), torch.zeros((4, 3))
     need = api.beam_workspace_bytes(x, 4, 7)
