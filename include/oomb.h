@@ -532,6 +532,9 @@ oomb_status oomb_paged_attn_fwd_rows(const oomb_rows_desc* desc, const oomb_seqs
  *   lens_out [n_out] (may be seq_lens), refs_out [num_phys_pages] (may be refs)
  *   copies [n_out][3]  {source, destination, tokens}, or {-1, -1, 0} where nothing is to be copied
  *   status [2]         pages taken, and pages that were missing: their entries are -1 (what is appended there is dropped and not attended)
+ * What a caller keeps by sequence follows the parents by the caller's own gather, before the append: the page means (kbar_cache [n_seqs]... of the appends), texts, who has
+ * ended.  A hypothesis that has ended needs no pages: with OOMB_FORK_NONE for its parent its rows do not exist.  Rows that are appended without room for
+ * them (grow) go over their sequence's last tokens, in pages that others may share.
  * n_seqs and n_out up to 4096, page_size a power of two.
  *
  * oomb_page_compact: the n used pages (refs > 0) move to the places 0 .. n - 1: the i-th used page from n on goes to the i-th free page below n.
@@ -572,7 +575,7 @@ oomb_status oomb_page_copy(const oomb_copy_desc* desc, void* const* pools, const
  * descending, ties to the lowest w * vocab + v.
  *   logits [n_groups * n_beams][vocab] of dtype, rows row_stride elements apart, aligned to their elements
  *   scores [n_groups][n_beams] float;  done [n_groups][n_beams] int32 or NULL: a beam that has ended offers one candidate, pad_token at its score, and its
- *          logits are not read
+ *          logits are not read; that of the next step is the parents', and 1 where a token ends its text
  *   parents, tokens [n_groups][n_out] int32, scores_out [n_groups][n_out] float (not in the memory of scores): parents are rows of all groups,
  *          group * n_beams + w, as oomb_page_fork takes them
  * A logit of -infinity is never taken.  A beam whose score, or whose log-sum (a logit of +infinity or NaN, nothing but -infinity), is not finite offers nothing;

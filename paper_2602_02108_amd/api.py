@@ -932,7 +932,8 @@ def page_fork_workspace_bytes(n_seqs: int, n_out: int, n_phys: int) -> int:
 def page_fork(page_tables, seq_lens, parents, refs, page_size: int, grow=None, tables_out=None, lens_out=None, refs_out=None, copies=None, status=None,
               workspace=None) -> PageFork:
     """oomb_page_fork: the sequences of the next step, one per entry of parents (a sequence, FORK_BEGINS or FORK_NONE), each with room for
-    grow more tokens.  refs is updated in place unless refs_out is given.  page_copy(pools, result.copies) then copies the partly filled pages."""
+    grow more tokens.  refs is updated in place unless refs_out is given.  page_copy(pools, result.copies) then copies the partly filled pages.
+    What the caller keeps by sequence (page means, texts, who has ended) it gathers by parents itself."""
     for name, t, dims in (("page_tables", page_tables, 2), ("seq_lens", seq_lens, 1), ("parents", parents, 1), ("refs", refs, 1)):
         if not isinstance(t, torch.Tensor) or t.dim() != dims:
             raise OombError(ERR_INVALID_ARG, f"oomb_page_fork: {name} must be a tensor of {dims} dims")
@@ -1028,7 +1029,8 @@ def beam_workspace_bytes(logits, groups: int, n_out: int) -> int:
 
 def beam_topk(logits, scores, n_out: int, done=None, pad_token: int = 0, parents=None, tokens=None, scores_out=None, workspace=None):
     """oomb_beam_topk: of every group the n_out best continuations of its beams.  logits [groups * beams][vocab] or [groups][beams][vocab]; scores
-    [groups][beams] float32; done [groups][beams] int32.  Returns (parents [groups][n_out] int32 rows of logits, tokens int32, scores float32)."""
+    [groups][beams] float32; done [groups][beams] int32 (of the next step: the parents', and 1 where a token ends its
+    text).  Returns (parents [groups][n_out] int32 rows of logits, tokens int32, scores float32)."""
     if not isinstance(scores, torch.Tensor) or scores.dim() != 2 or not isinstance(logits, torch.Tensor):
         raise OombError(ERR_INVALID_ARG, "oomb_beam_topk: scores must be float32 [groups][beams]")
     groups, dev = int(scores.shape[0]), logits.device

@@ -535,3 +535,117 @@ def test_beam_search_over_a_paged_cache(dt, D, P, graph):
         for x in row[:-(-t // P)]:
             count[x] += 1
     assert count == refs.tolist()
+
+
+def _search_plain_that_ends(toy, prompts, W, steps, rope, eos, pad):
+    """_search_plain whose texts end: one that holds eos stays as it is and goes on with pad."""
+    out = []
+    for prompt in prompts:
+        beams = [(0.0, list(prompt), False)]
+        for _ in range(steps):
+            cand = []
+            for i, (s, text, over) in enumerate(beams):
+                if over:
+                    cand.append((-s, i, pad))
+                    continue
+                x = toy.next_logits(text, rope)
+                x = x - torch.logsumexp(x, 0)
+                cand += [(-(s + float(x[v])), i, v) for v in range(toy.V)]
+            beams = [(-c, beams[i][1] + [v], beams[i][2] or v == eos) for c, i, v in sorted(cand)[:W]]
+        out.append(beams)
+    return out
+
+
+@pytest.mark.parametrize("D,eos,steps,graph", [(64, 7, 12, False), (64, 7, 12, True), (128, 6, 6, False), (128, 6, 6, True)])
+def test_beam_search_whose_texts_end(D, eos, steps, graph):
+    """The loop of a program: who has ended, the texts and the page means follow the parents; hypotheses that have ended hold no pages, their rows do not exist, and their
+    logits are NaN.  Some end and are beaten later, and some texts end in all their hypotheses.  (Candidates next to each other at the edge are 2e-3 apart at least.)"""
+    W, V, Hq, Hkv, P, pad, cols, n_phys = 4, 40, 4, 2, 16, 11, 6, 90
+    prompts = [[3, 1, 4, 1, 5, 9, 2, 6, 5, 3, 5, 8, 9, 7, 9, 3, 2], [2, 7], [1] * 31]
+    n = len(prompts)
+    B = n * W
+    cpu, gpu = Toy(V, Hq, Hkv, D, F32, "cpu"), Toy(V, Hq, Hkv, D, F32, "cuda")
+    rope = api.rope_tables(cols * P, D)
+    pools = [torch.full((n_phys, Hkv, P, D), math.nan, device="cuda") for _ in range(2)]
+    refs = torch.zeros(n_phys, dtype=torch.int32, device="cuda")
+    scale = 1.0 / math.sqrt(D)
+    start = api.page_fork(_i([[-1] * cols]), _i([0]), _i([api.FORK_BEGINS] * n), refs, P, grow=_i([len(p) for p in prompts]))
+    q, k, v = gpu.rows(_i(sum(prompts, [])))
+    starts = _i([0] + list(np.cumsum([len(p) for p in prompts])))
+    first_means = torch.zeros((n, cols, Hkv, D), device="cuda")
+    desc = api.make_rows_desc(q, pools[0], start.tables, cols * P, scale, max_rows=31)
+    y = api.kv_append_rope(desc, k, v, start.tables, *pools, q=q, rope=rope, kbar_cache=first_means, seq_lens=start.lens, row_starts=starts)
+    o, _ = api.paged_attn_fwd_rows(desc, y, *pools, start.tables, seq_lens=start.lens, row_starts=starts)
+    logits = torch.full((B, V), math.nan, device="cuda")
+    logits[::W] = gpu.logits(o[starts[1:].long() - 1])
+    scores = torch.full((n, W), -math.inf, device="cuda")
+    scores[:, 0] = 0.0
+    done = torch.zeros((n, W), dtype=torch.int32, device="cuda")
+    tables = torch.full((B, cols), -1, dtype=torch.int32, device="cuda")
+    lens = torch.zeros(B, dtype=torch.int32, device="cuda")
+    tables[::W], lens[::W] = start.tables, start.lens
+    means = torch.zeros((B, cols, Hkv, D), device="cuda")
+    means[::W] = first_means
+    texts = torch.zeros((B, steps), dtype=torch.int32, device="cuda")
+    missing, at = torch.zeros((), dtype=torch.int32, device="cuda"), torch.zeros((1, 1), dtype=torch.int64, device="cuda")
+    ones = _i([1] * B)
+
+    def step():
+        parents, tokens, best = api.beam_topk(logits, scores, W, done=done, pad_token=pad)
+        rows = parents.flatten()
+        came = rows.clamp(min=0)
+        over = done.flatten()[came] | (tokens.flatten() == eos)
+        new = api.page_fork(tables, lens, torch.where(over != 0, api.FORK_NONE, rows), refs, P, grow=ones)
+        api.page_copy(pools, new.copies)
+        missing.add_(new.status[1])
+        means.copy_(means[came])
+        q, k, v = gpu.rows(tokens.flatten())
+        desc = api.make_rows_desc(q, pools[0], new.tables, cols * P, scale, max_rows=1)
+        y = api.kv_append_rope(desc, k, v, new.tables, *pools, q=q, rope=rope, kbar_cache=means, seq_lens=new.lens)
+        o, _ = api.paged_attn_fwd_rows(desc, y, *pools, new.tables, seq_lens=new.lens)
+        logits.copy_(torch.where(over[:, None] != 0, math.nan, gpu.logits(o)))
+        scores.copy_(best)
+        done.copy_(over.view(n, W))
+        tables.copy_(new.tables)
+        lens.copy_(new.lens)
+        texts.copy_(texts[came])
+        texts.scatter_(1, at.expand(B, 1), tokens.view(-1, 1))
+
+    if graph:
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            gpu.logits(torch.zeros((B, Hq, D), device="cuda"))     # (the library's handles and workspaces exist before the capture)
+            side.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                step()
+        torch.cuda.synchronize()
+    for i in range(steps):
+        at.fill_(i)
+        if graph:
+            g.replay()
+        else:
+            step()
+        torch.cuda.synchronize()
+    assert int(missing) == 0
+    want = _search_plain_that_ends(cpu, prompts, W, steps, rope, eos, pad)
+    over = [[b[2] for b in beams] for beams in want]
+    assert any(all(x) for x in over) and not all(all(x) for x in over)
+    assert done.tolist() == [[int(x) for x in y] for y in over]
+    got, got_scores = texts.cpu().view(n, W, steps), scores.cpu()
+    for i, prompt in enumerate(prompts):
+        for w in range(W):
+            assert got[i, w].tolist() == want[i][w][1][len(prompt):], (i, w)
+            assert abs(float(got_scores[i, w]) - want[i][w][0]) < 1e-4 * steps      # (as above: under 1e-4 a step)
+    # pages of ended hypotheses are free, the others counted; the means are those of the pages' keys
+    assert lens.tolist() == [0 if over[b // W][b % W] else len(prompts[b // W]) + steps for b in range(B)]
+    count = [0] * n_phys
+    for b, (row, t) in enumerate(zip(tables.tolist(), lens.tolist())):
+        for x in row[:-(-t // P)]:
+            count[x] += 1
+        for l in range(t // P):
+            keys = pools[0][row[l]].double()
+            tol = P * 2.0 ** -24 * keys.abs().mean(1)                               # (sums of P in fp32)
+            assert ((means[b, l].double() - keys.mean(1)).abs() <= tol).all()
+    assert count == refs.tolist()
