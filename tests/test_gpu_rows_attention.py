@@ -333,6 +333,52 @@ def test_many_sequences(dt, Hq, Hkv, D, P, n, rows, tokens, listed):
     assert torch.equal(o, o2) and torch.equal(lse, lse2)
 
 
+def _path(b, Hq, Hkv, D, dt):
+    """How a call over every page goes, by its sizes: what runs it, who counts it, how it is cut; and the workspace that follows, which the library is asked for."""
+    es, rows, heads = dt.itemsize, b.max_rows * (Hq // Hkv), len(b.spans) * Hkv
+    cache = min(heads * b.max_len, b.n_phys * Hkv * b.P) * 2 * D * es
+    tiles = dt == BF and rows > 32 and (-(-rows // 32) - 1) * cache > (48 << 20)
+    rt = 2 if rows > 16 and (D == 64 or (dt == BF and (-(-rows // 16) - 1) * cache > (16 << 20))) else 1
+    block, step, least = (128, 64, 8) if tiles else (16 * rt, 32, 4)
+    blocks = min((b.n_rows * (Hq // Hkv) // block + len(b.spans)) * Hkv, -(-rows // block) * heads)
+    steps, planned = -(-b.max_len // step), heads > 512
+    split = steps > 16 and blocks <= (8192 if planned and not tiles else 1024)
+    full = not tiles and blocks > 512
+    target = 512 if tiles else blocks + 256 if full else 512 - blocks // 2 if blocks < 512 else blocks
+    wgs = min(blocks * -(-steps // least), target + blocks + 2)
+    loads = [(-(-n * (Hq // Hkv) // block) * Hkv, max(1, -(-t // step))) for n, t in b.spans]
+    total, most = sum(x * y for x, y in loads), max(y for x, y in loads if x)
+    per = max(least, -(-most // max(1, int(target * most / total))) if tiles else total // target + 1)
+    cut = split and most > (2 * per if full else per)
+    return ("tiles" if tiles else f"rows{rt}", "planned" if planned else "full" if full else "counted", "cut" if cut else "split" if split else "whole"), \
+        (wgs * block * (D + 2) * 4 if split else 0) + ((heads + 1) * 8 if split or planned else 0)
+
+
+@pytest.mark.parametrize("dt,Hq,Hkv,D,P,spans,path", [
+    (BF, 16, 8, 64, 16, _spread(80, 60, 1500, 5), ("tiles", "planned", "cut")),
+    (BF, 16, 8, 128, 32, _spread(80, 55, 1300, 6), ("tiles", "planned", "cut")),
+    (BF, 16, 8, 64, 16, _spread(90, 200, 1200, 7), ("tiles", "planned", "whole")),
+    (BF, 16, 8, 128, 16, [(40, 250)] * 70, ("tiles", "planned", "whole")),
+    (BF, 14, 1, 128, 64, [(10, 300)] * 520, ("tiles", "planned", "whole")),
+    (F32, 8, 4, 64, 16, _spread(40, 100, 1500, 8), ("rows2", "full", "cut")),
+    (F32, 8, 4, 64, 32, [(60, 700)] * 35, ("rows2", "full", "split")),          # about equal: its parts are whole blocks
+    (F32, 4, 2, 128, 16, _spread(60, 70, 1500, 9), ("rows1", "full", "cut")),
+    (BF, 4, 2, 64, 16, _spread(100, 70, 700, 10), ("rows2", "full", "cut")),
+], ids=lambda x: "-".join(x) if isinstance(x, tuple) else None)
+def test_many_sequences_by_every_path(dt, Hq, Hkv, D, P, spans, path):
+    b = ru.Batch(spans, P, 19)
+    got, need = _path(b, Hq, Hkv, D, dt)
+    assert got == path
+    q = _queries(b, Hq, D, dt, 15)
+    pools = [pu.random_pool(b, Hkv, D, dt, s) for s in (27, 28)]
+    table = torch.empty((len(spans), b.cols), dtype=torch.int32)
+    assert api.rows_workspace_bytes(api.make_rows_desc(q, pools[0], table, b.max_len, 0.1, max_rows=b.max_rows)) == need
+    o, lse = _run(b, q, pools, 0.1)
+    _verify(b, q, pools, 0.1, o, lse)
+    o2, lse2 = _run(b, q, pools, 0.1, workspace=torch.full((need,), 127, dtype=torch.uint8, device="cuda") if need else None)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
 @pytest.mark.parametrize("B", [200, 300])
 def test_many_sequences_of_equal_rows_and_lengths(B):
     """Without starts and lengths."""
