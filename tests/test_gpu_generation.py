@@ -256,6 +256,19 @@ def test_beam(case):
     _verify_beam(x, scores, n_out, _beam(x, scores, n_out, done, 3), done, 3)
 
 
+@pytest.mark.parametrize("dt", [F32, BF])
+@pytest.mark.parametrize("V", [3, 60, 240, 256, 500])
+def test_beam_of_short_rows_and_many_beams(V, dt):
+    """Rows that fill fewer lanes than candidates are asked for: a first bound that nothing sets, and more cells than its list holds."""
+    for W in (5, 17, 64):
+        x = _logits((3, W, V), dt, 25)
+        scores = -10.0 * torch.rand((3, W), generator=torch.Generator().manual_seed(26))
+        done = (torch.rand((3, W), generator=torch.Generator().manual_seed(27)) < 0.3).to(torch.int32)
+        for n_out in (1, 33, 64):
+            _verify_beam(x, scores, n_out, _beam(x, scores, n_out))
+            _verify_beam(x, scores, n_out, _beam(x, scores, n_out, done, 2), done, 2)
+
+
 def test_beam_of_equal_logits_takes_the_lowest():
     for V, dt in ((9000, BF), (5000, F32), (300, BF)):
         for W in (1, 3):
