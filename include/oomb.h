@@ -505,6 +505,7 @@ oomb_status oomb_paged_attn_fwd_kvq(const oomb_rows_desc* desc, const oomb_seqs*
  * fills), as oomb_paged_attn_fwd_kvq over its own: the same rows, lists, outputs and empty rows.  A page of one KV head spans less than 2 GiB.  bf16 rows:
  * weights in two bf16 terms (2^-16 of a weight); fp32 rows: products in fp32.  Sums in fp32.  What is not seen may hold anything.  Of what is seen, a NaN in K makes
  * its rows NaN; an infinity or a NaN in V makes that dim of its rows infinite or NaN, and of no other.
+ * One kernel takes a whole call, by max_rows: pieces of prompts and single tokens over long caches take less time in a call each.
  * Results do not depend on scheduling.  Workspace: oomb_rows_workspace_bytes(desc, sel_stride), as above.
  */
 size_t oomb_rows_workspace_bytes(const oomb_rows_desc* desc, int32_t sel_stride);

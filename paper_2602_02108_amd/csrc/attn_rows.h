@@ -20,7 +20,7 @@
 // What bounds it.  Few rows: the reading of the cache (28 heads over 4 of 128 dims, bf16, 1M tokens: 2.1 GB in 323 us, 6.6 TB/s, of which the join takes 6; fp32 5.5),
 // where it is short two launches and a chain of loads that wait for each other (lengths, page, rows; 1000 tokens 11 us).  So a wave keeps 32 KB in
 // flight, and the loop carries no LDS, no barrier and no exchange but the test of the weights.  Many rows read the cache again per block of rows: then
-// attn_tiles_kernel, below, shares a reading among 128 rows (three prompts of up to 1021 rows: 945 us here, 342 there); fp32 stays here, where the
+// attn_tiles_kernel, below, shares a reading among 128 rows (three prompts of up to 1021 rows: 945 us here, 342 to 350 there); fp32 stays here, where the
 // fp32 matrix instructions bound it (1024 rows over 16K tokens, 28 / 4 heads of 128: 2219 us, 105 TFLOP/s; the library's fp32 product 136).
 #pragma once
 #include <type_traits>
@@ -706,7 +706,7 @@ __global__ __launch_bounds__(COMBINE_THREADS) void attn_combine_kernel(RowsParam
 // holds one query row.  The softmax as above.
 // What bounds it: the matrix unit and the power it draws (4096 rows over 16K tokens, 28 / 4 heads of 128: 1175 us, 0.72 PFLOP/s, 1.08 with the weights' second
 // terms; a library product of 8192^3 1.21).  32 rows a wave and a stage of 64 tokens twice are what registers and LDS hold for two workgroups a compute unit.  First form,
-// softmax and products one after the other, 396 us for three prompts; in one pipeline with the accumulators where they are 342.
+// softmax and products one after the other, 396 us for three prompts; in one pipeline with the accumulators where they are 342 to 350.
 // A row tile in the LDS: rows of 2 D bytes, granule c (16 bytes) of row r at c ^ f(r).  Head dim 128: that of mfma_common.h.  Head dim 64: two rows share a
 // line of 256 bytes, f(r) = 4 ((r / 2) % 2) + (r / 4) % 4: 16 rows read at one granule, and the 4 rows x 64 bytes of a transposing read, use every bank once.
 constexpr int TILE_ROWS = 128, TILE_STAGE = 64, TILE_THREADS = 256;
@@ -1034,6 +1034,8 @@ Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   const int64_t again_16 = ((rows + 15) / 16 - 1) * cache_bytes, again_32 = ((rows + 31) / 32 - 1) * cache_bytes;
   // Tiles once the caches are read by a second block of 32 rows and that costs more than their start (one sequence, D 128, us without and with: 4 heads of 4096
   // tokens, 35 rows 17, 16; of 65,536, 54, 40; 64 of 2048, one head, 64 rows 36, 31; 16 of 4096, D 64, one head, 96 rows 20, 21).
+  // It goes by the most rows of a sequence, for the whole call: single tokens beside a prompt's piece go in tiles too, seven rows in place of 128 (31 of up to 32K tokens and a
+  // piece of 1000 rows: 610 us; in two calls 107 and 340).
   c.tiles = is_bf16 && rows > 32 && again_32 > (48ll << 20) && p.pool_tok_stride <= (1 << 24);   // (offsets of a lane in a tile: 32 bits)
   // Two row tiles a wave where rows need them; at head dim 128 for bf16 and caches that are worth it, one step in flight instead of two (32 rows of one head, us
   // with one and two: 4096 tokens 12, 14; 65,536, 25, 23; 28 rows of four heads over 500,000, in tiles 224, in two 167: 6.1 TB/s).
@@ -1055,6 +1057,8 @@ Plan plan_of(const RowsParams& p, bool is_bf16, int32_t sel_stride) {
   const int64_t most = (steps + c.min_steps - 1) / c.min_steps;
   const int64_t parts = c.target + blocks + 2;   // (what item_at comes to at most; two for its roundings)
   c.blocks = !c.split ? blocks : blocks * most < parts ? blocks * most : parts;
+  // Measured where a byte is read once (single tokens); rows that read the caches again, prompts in fp32, lose by it (1000 rows, 28 / 4 heads of 128 dims, 336 MB: 23.2 ms,
+  // through the caches 11.5; 14 / 2 of 64 dims, 338 MB: 12.1, 10.6; 1000 rows of 2000 tokens in a pool of 600 MB: 0.226, 0.220).
   c.stream = cache_bytes > (256ll << 20);
   return c;
 }

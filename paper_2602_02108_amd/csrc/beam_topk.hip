@@ -6,12 +6,14 @@
 // exponentials against it.  The second one, a workgroup per group, adds the sums, which makes candidates of different beams comparable, and looks for the K best
 // through the cells: the K-th best cell maximum is a bound that K candidates reach at least; only the few cells that reach it are read again, and the rank of
 // each of their values above the bound is counted.  Candidates are compared in 64 bits, ties go to the lowest w * vocab + v.
-// Where very many values are equal (logits masked with a finite value, fewer than K others) the bound does not sort them out; then those equal to it are taken
-// in order of their places.
+// Where very many values are equal (logits masked with a finite value, fewer than K others) the bound does not sort them out; then the K-th best cell is found in 64
+// bits, and those equal to it are taken in order of their places.  Rows that fill fewer than K lanes (vocab / 4 in fp32, / 8 in bf16) have no first bound: with more than
+// CELLS of them their group goes that way too (64 beams of 240 in fp32, 64 best: 60 us; of 1200: 21).
 //
-// What bounds it: the first kernel, the reading of the logits (256 rows of 130,999 bf16: 67 MB in 15 us, 4.5 TB/s; a maximum costs one instruction an element, where the
-// best of each slice kept on the way made both kernels 154 us instead of 25); the second, one workgroup a group and its chain of steps (cells, bound, values, ranks),
-// about 10 us for any vocabulary.
+// What bounds it: the first kernel, the reading of the logits (256 rows of 130,999 bf16: 67 MB in 15.4 us, 4.4 TB/s; a maximum costs one instruction an element, where the
+// best of each slice kept on the way made both kernels 154 us instead of 25); the second, one workgroup a group and its chain of steps (cells, bound, values, ranks):
+// 8.7 us for one group of 4 x 32,000, 10.3 for 8 x 130,999, 10.7 for 32 such.  A cell that is read again holds vocab / (256 slices) values, which counts where many beams leave
+// one slice a row: 34 us for 64 x 200,001 (fp32; the first kernel as many), 243 for 33 x 4,000,004 (beside 810).
 #include <algorithm>
 #include <cfloat>
 
@@ -23,12 +25,12 @@ namespace {
 
 constexpr int THREADS = 256;                    // of the first kernel
 constexpr int LOADS = 4;                        // of 16 bytes, of a thread at a time
-constexpr int MOST_LISTS = 64;                  // slices of a group's rows (or one a row): the second kernel takes in 10 B/ns (one group of 8 x 130,999: 16 us, with 256 lists 41)
+constexpr int MOST_LISTS = 64;                  // slices of a group's rows (or one a row): the second kernel takes in 10 B/ns (one group of 8 x 130,999 in fp32, both kernels: 16 us, with 256 lists 41)
 constexpr int GROUP_THREADS = 1024;             // of the second
 constexpr int GROUP_WAVES = GROUP_THREADS / 64;
 constexpr int HELD = MOST_LISTS * THREADS / GROUP_THREADS;   // cells of a thread of it
 static_assert(BEAM_MOST_BEAMS <= MOST_LISTS, "a row has a list at least");
-constexpr int CELLS = 1024;                     // that reach the first bound (about 300 of equally distributed values at most)
+constexpr int CELLS = 1024;                     // that reach the first bound (about 300 of equally distributed values at most, where there is one)
 constexpr int HOLDERS = 256;                    // of them, that reach the bound
 constexpr int ROOM = GROUP_THREADS;             // candidates that do
 constexpr int PARTS = 8;                        // threads that count a rank together
@@ -344,7 +346,7 @@ template <typename T> __global__ __launch_bounds__(GROUP_THREADS) void beam_grou
     }
   }
   if (!found) {
-    // Very many values are equal.  The K-th best cell in 64 bits: what reaches it stands in the cells that do, and if they are many, in the fewer than K above
+    // Very many values are equal, or very many cells have no first bound.  The K-th best cell in 64 bits: what reaches it stands in the cells that do, and if they are many, in the fewer than K above
     // it and at the lowest places that equal it.
     if (tid < n_ended) { c.val[tid] = ended_val[tid]; c.at[tid] = ended_at[tid]; }
     if (tid < p.n_beams) ties[tid] = 0;

@@ -5,7 +5,7 @@
 // What bounds it: launches and loads that wait for each other (parent, length, page, count), so few pages take one workgroup that holds the counts in the
 // LDS (tables of 64 rows of 34: 6 us in one launch, 9 in two).  More pages: the plan (one workgroup, since every child's new pages follow from the needs of those
 // before it) reads the counts only as far as free pages are needed, of a large pool the whole chip lists them first; the tables are written by the whole chip.
-// Copies: memory, 236 MB read and written in about 45 us.
+// Copies: memory, 236 MB read and written in 45 to 49 us (of the same pools again, partly out of the caches, 35).
 #include "gen.h"
 #include "wave.h"
 
@@ -252,7 +252,7 @@ __global__ __launch_bounds__(COPY_THREADS) void page_copy_kernel(CopyParams p, C
       }
 #pragma unroll
       for (int j = 0; j < AT_ONCE; ++j)
-        if (u0 + j * COPY_THREADS < units) __builtin_nontemporal_store(v[j], reinterpret_cast<u32x4*>(to + at[j]));   // (past the caches: 236 MB 60 -> 53 us)
+        if (u0 + j * COPY_THREADS < units) __builtin_nontemporal_store(v[j], reinterpret_cast<u32x4*>(to + at[j]));   // (past the caches: a compact and its copies of 236 MB 60 -> 53 us)
     }
   }
 }
